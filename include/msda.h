@@ -76,8 +76,9 @@ typedef enum {
     MSDA_ERROR_LAUNCH_FAILED = 3  /* the HIP runtime reported an error when the kernels were enqueued */
 } msda_status_t;
 
-/* Element type of value, out and grad_out. */
-typedef enum { MSDA_F32 = 0, MSDA_F16 = 1 } msda_dtype_t;
+/* Element type of value, out and grad_out. MSDA_BF16 (bfloat16) is a type of the layer operators at the
+ * end of this header; the deformable attention entry points take MSDA_F32 and MSDA_F16. */
+typedef enum { MSDA_F32 = 0, MSDA_F16 = 1, MSDA_BF16 = 2 } msda_dtype_t;
 
 /*
  * Validate a problem description without touching any device: sizes, dtype and the level table.
@@ -277,6 +278,139 @@ msda_status_t msda_backward_fused(const void* value, const int64_t* spatial_shap
                                   float* grad_logits, void* workspace, size_t workspace_bytes,
                                   int64_t N, int64_t S, int64_t M, int64_t D, int64_t Lq, int64_t L,
                                   int64_t P, int dtype, void* stream);
+
+/*
+ * Layer operators: what a transformer layer runs beside the deformable attention above. Ownership,
+ * execution and errors are those stated at the head of this header: device pointers owned by the
+ * caller, work enqueued on `stream` alone, nothing allocated and no state kept, outputs overwritten
+ * entirely. Activations are MSDA_F32, MSDA_F16 or MSDA_BF16 (`dtype`); all else is fp32. Arithmetic is
+ * fp32 (matrix products of 16-bit operands with fp32 sums), every result is rounded to nearest-even
+ * once, and all results are reproducible bit for bit (no atomics).
+ */
+
+/*
+ * Layer normalization of rows of C channels, with an optional residual addition before it:
+ *   s = x + residual                          (fp32; residual may be NULL: s = x)
+ *   mean = sum_c s / C,  rstd = (sum_c (s - mean)^2 / C + eps)^(-1/2)
+ *   out = (s - mean) * rstd * weight + bias   (weight NULL: 1; bias NULL: 0)
+ *   x, residual, out [rows, C] dtype;  weight, bias [C] fp32
+ *   sum              [rows, C] dtype or NULL: s rounded to dtype (out is formed from the unrounded s)
+ *   mean, rstd       [rows] fp32 or NULL: kept for the backward pass
+ * Pointers need the alignment of their elements; 16-byte aligned tensors whose C is a multiple of 16
+ * bytes are read in 16-byte pieces. rows == 0 is a successful no-op. eps must be finite and >= 0.
+ * C > MSDA_LAYERNORM_MAX_C is MSDA_ERROR_NOT_SUPPORTED.
+ */
+#define MSDA_LAYERNORM_MAX_C 16384
+msda_status_t msda_layernorm_forward(const void* x, const void* residual, const float* weight,
+                                     const float* bias, void* out, void* sum, float* mean, float* rstd,
+                                     int64_t rows, int64_t C, float eps, int dtype, void* stream);
+
+/* Workspace bytes of msda_layernorm_backward where a weight or bias gradient is wanted (host-only). */
+msda_status_t msda_layernorm_backward_workspace_size(int64_t rows, int64_t C, int dtype, size_t* bytes);
+
+/*
+ * Backward pass of msda_layernorm_forward, from its inputs x and residual and its mean and rstd:
+ *   xh = (s - mean) * rstd,  g = grad_out * weight
+ *   grad_x = rstd * (g - mean_c(g) - xh * mean_c(g * xh)) + grad_sum
+ *   grad_weight = sum_rows grad_out * xh,  grad_bias = sum_rows grad_out
+ *   grad_out, grad_x [rows, C] dtype; grad_x is the gradient of x and of residual alike
+ *   grad_sum         [rows, C] dtype or NULL: the gradient that reaches s past the norm (through `sum`)
+ *   grad_weight, grad_bias [C] fp32, each may be NULL (not computed)
+ * workspace: DEVICE scratch of msda_layernorm_backward_workspace_size bytes, 16-byte aligned; not
+ * looked at when both grad_weight and grad_bias are NULL. A smaller one is MSDA_ERROR_INVALID_VALUE.
+ * rows == 0 still zeroes grad_weight and grad_bias.
+ */
+msda_status_t msda_layernorm_backward(const void* x, const void* residual, const float* weight,
+                                      const void* grad_out, const void* grad_sum, const float* mean,
+                                      const float* rstd, void* grad_x, float* grad_weight,
+                                      float* grad_bias, void* workspace, size_t workspace_bytes,
+                                      int64_t rows, int64_t C, int dtype, void* stream);
+
+/*
+ * Rotary positions of A axes (time, height, width; or the x, y of a reference point): the first 2R
+ * channels of every head are R pairs, and pair i of a token at position pos is turned by
+ *   angle_i = sum_a pos[a] * freqs[a, i]      (formed in fp64: exact for far positions)
+ *   (xa, xb) -> (xa cos - xb sin, xa sin + xb cos)
+ * Channels 2i and 2i+1 are pair i if `interleaved` is nonzero, else channels i and R+i; channels from
+ * 2R on are copied. An axis that does not turn a pair has frequency 0 there.
+ *   x, out [N, T, M, D] dtype, the channels contiguous; x_stride and out_stride are HOST arrays of the
+ *          three strides (batch item, token, head) in elements, or NULL: contiguous
+ *   pos    [pos_items, T, A] fp32, pos_items = N, or 1: the same positions in every batch item
+ *   freqs  [A, R] fp32
+ * out == x with the same strides rotates in place; otherwise they must not overlap. An output stride
+ * of 0 over more than one entry is MSDA_ERROR_INVALID_VALUE. 1 <= A <= 4, 0 <= 2R <= D;
+ * D > MSDA_ROTARY_MAX_D or M * D > 65536 is MSDA_ERROR_NOT_SUPPORTED. N * T == 0 is a no-op.
+ */
+#define MSDA_ROTARY_MAX_D 1024
+msda_status_t msda_rotary_forward(const void* x, const int64_t* x_stride, const float* pos,
+                                  const float* freqs, void* out, const int64_t* out_stride, int64_t N,
+                                  int64_t T, int64_t M, int64_t D, int64_t A, int64_t R,
+                                  int64_t pos_items, int interleaved, int dtype, void* stream);
+
+/* Backward pass: grad_x is grad_out turned by -angle (the rotation's transpose); arguments as above. */
+msda_status_t msda_rotary_backward(const void* grad_out, const int64_t* grad_out_stride, const float* pos,
+                                   const float* freqs, void* grad_x, const int64_t* grad_x_stride, int64_t N,
+                                   int64_t T, int64_t M, int64_t D, int64_t A, int64_t R,
+                                   int64_t pos_items, int interleaved, int dtype, void* stream);
+
+/*
+ * Dense attention of Lq queries over Lk keys with capped scores, a bias by distance and masks given by
+ * rules (no mask tensor is read). Query head m reads key head m / (M / Mkv).
+ *   z_ij = cap(scale * q_i . k_j) - slopes[m] * |q_pos_i - k_pos_j|      cap(s) = softcap * tanh(s / softcap)
+ *   lse_i = log sum_j exp(z_ij),  out_i = sum_j exp(z_ij - lse_i) v_j     over the keys j that i sees
+ * Query i of batch item n sees key j if both hold:
+ *   documents: no tables; or q_doc[n,i] >= 0 and k_doc[n,j] >= 0 and (q_doc[n,i] == k_doc[n,j] or
+ *              j < prefix[n])
+ *   order:     not causal; or j <= i + Lk - Lq (the last query sees every key); or j < prefix[n]
+ * so a document of -1 is padding, and the first prefix[n] keys are common to all. A query that sees no
+ * key (or whose scores are all minus infinity) gets out = 0 and lse = -inf, and passes no gradient. What a
+ * query does not see has no effect on it, infinities and NaN included.
+ */
+typedef struct {
+    int64_t N, Lq, Lk, M, Mkv, D; /* M a multiple of Mkv; 1 <= D <= MSDA_ATTENTION_MAX_D              */
+    int dtype;                    /* of q, k, v, out and the gradients                                */
+    int causal;                   /* nonzero: the order rule above; needs Lk >= Lq                    */
+    float scale;                  /* finite, > 0                                                      */
+    float softcap;                /* finite, >= 0; 0: scores are not capped                           */
+    int64_t q_stride[3];          /* strides of q [N, Lq, M, D] in elements: batch item, token, head; */
+    int64_t k_stride[3];          /* the channels are contiguous. Likewise k [N, Lk, Mkv, D]          */
+    int64_t v_stride[3];          /* and v [N, Lk, Mkv, D]                                            */
+    const float* slopes;          /* DEVICE [M] fp32 or NULL: no bias; constants, they get no gradient */
+    const float* q_pos;           /* DEVICE [N, Lq, 2] fp32 and [N, Lk, 2] fp32, with slopes: the     */
+    const float* k_pos;           /* places between which the (Euclidean) distance is taken           */
+    const int32_t* q_doc;         /* DEVICE [N, Lq] and [N, Lk], both or neither                      */
+    const int32_t* k_doc;
+    const int32_t* prefix;        /* DEVICE [N] or NULL: no common keys                               */
+} msda_attention_t;
+#define MSDA_ATTENTION_MAX_D 128
+
+/* Workspace bytes of msda_attention_forward (backward == 0) or msda_attention_backward: host-only, from
+ * the sizes, dtype and which tables are given. */
+msda_status_t msda_attention_workspace_size(const msda_attention_t* a, int backward, size_t* bytes);
+
+/*
+ * Forward pass: out [N, Lq, M, D] dtype (contiguous) and lse [N, M, Lq] fp32 (NULL: not written; the
+ * backward pass needs it). Few queries over many keys are split over the keys and joined, so a single
+ * token against a long cache fills the GPU. workspace: DEVICE scratch of at least
+ * msda_attention_workspace_size bytes, 16-byte aligned (may be NULL if that is 0), used by nothing
+ * else until the enqueued work completes; a smaller one is MSDA_ERROR_INVALID_VALUE. Pointers need the
+ * alignment of their elements; tensors whose base, strides and rows are multiples of 16 bytes are
+ * read in 16-byte pieces. Out is 16-byte aligned. N * Lq == 0 is a no-op; Lk == 0 writes out = 0, lse = -inf.
+ */
+msda_status_t msda_attention_forward(const msda_attention_t* a, const void* q, const void* k, const void* v,
+                                     void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/*
+ * Backward pass, from the forward's inputs, out and lse: grad_q [N, Lq, M, D], grad_k and grad_v
+ * [N, Lk, Mkv, D] (dtype, contiguous, 16-byte aligned, summed over the query heads that share a key head).
+ * out and grad_out are contiguous and 16-byte aligned. N == 0 is a no-op; with Lq == 0 or Lk == 0 the gradients that exist
+ * are zeroed.
+ */
+msda_status_t msda_attention_backward(const msda_attention_t* a, const void* q, const void* k, const void* v,
+                                      const void* out, const float* lse, const void* grad_out, void* grad_q,
+                                      void* grad_k, void* grad_v, void* workspace, size_t workspace_bytes,
+                                      void* stream);
 
 /* Static name of a status code ("MSDA_SUCCESS", ...); any int is accepted, and a value that is no
  * msda_status_t gives "MSDA_UNKNOWN_STATUS". */

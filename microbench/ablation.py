@@ -29,6 +29,7 @@ BUILD = os.path.join(HERE, "_build")
 CSRC = os.path.join(ROOT, "paper_2505_14022_amd", "csrc")
 PRODUCT = os.path.join(ROOT, "paper_2505_14022_amd", "_lib", "libmsda.so")
 sys.path.insert(0, ROOT)
+from paper_2505_14022_amd.build import SOURCES  # noqa: E402
 
 # variant -> (macro, what it replaces, workloads it is measured at)
 VARIANTS = {
@@ -62,8 +63,6 @@ VARIANTS = {
 }
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Xclang", "-target-feature",
          "-Xclang", "-packed-fp32-ops", "-munsafe-fp-atomics"]
-SOURCES = ["msda_api.cpp", "msda_arrange.cpp", "msda_fwd.hip", "msda_bwd.hip", "msda_bwd_value.hip",
-           "msda_prologue.hip", "msda_noalloc.hip"]
 PASSES = {
     "sq": ["SQ_WAVES", "SQ_WAVE_CYCLES", "SQ_BUSY_CYCLES", "SQ_INSTS_VALU", "SQ_INSTS_LDS", "SQ_LDS_BANK_CONFLICT",
            "SQ_WAIT_INST_ANY", "SQ_ACTIVE_INST_VALU", "GRBM_GUI_ACTIVE"],

@@ -9,12 +9,13 @@
 
 #include "msda.h"
 #include "msda_internal.h"
+#include "msda_layer.h"
 
 static_assert(MSDA_NOALLOC_SCRATCH_BYTES == msda::kStaticScratchBytes, "static scratch size in msda.h");
 
-namespace {
+static thread_local char g_last_error[512] = "";
 
-thread_local char g_last_error[512] = "";
+namespace msda {
 
 msda_status_t fail(msda_status_t st, const char* fmt, ...) {
     va_list ap;
@@ -28,6 +29,13 @@ msda_status_t ok() {
     g_last_error[0] = '\0';
     return MSDA_SUCCESS;
 }
+
+}  // namespace msda
+
+namespace {
+
+using msda::fail;
+using msda::ok;
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 

@@ -1,0 +1,90 @@
+// Internal interface between the layer operators' C ABI (msda_layer_api.cpp) and their HIP kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "msda.h"
+
+namespace msda {
+
+// Errors of all entry points (msda_api.cpp): fail() keeps the message for msda_last_error().
+msda_status_t fail(msda_status_t st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+msda_status_t ok();
+
+inline bool is_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline int dtype_size(int dtype) { return dtype == MSDA_F32 ? 4 : 2; }
+
+// ---------------------------------------------------------------- layer norm
+
+struct NormParams {
+    const void *x, *residual;   // [rows, C] dtype; residual may be null
+    const float *weight, *bias; // [C] or null
+    void *out, *sum;            // forward; sum may be null
+    const void *grad_out, *grad_sum;  // backward; grad_sum may be null
+    void* grad_x;
+    float *mean, *rstd;         // [rows]; may be null in the forward
+    float* partial;             // backward: [2][blocks][C] partial sums of grad_weight and grad_bias, or null
+    float *grad_weight, *grad_bias;   // may be null
+    int64_t rows;
+    int C, blocks;
+    float eps;
+    bool vec;                   // rows are whole 16-byte pieces, 16-byte aligned
+};
+
+// Workgroups of the backward kernel, each with a row of partial sums.
+int norm_backward_blocks(int64_t rows, int64_t C, int dtype);
+hipError_t launch_layernorm_forward(const NormParams& p, int dtype, hipStream_t stream);
+hipError_t launch_layernorm_backward(const NormParams& p, int dtype, hipStream_t stream);
+
+// ---------------------------------------------------------------- rotary positions
+
+struct RotaryParams {
+    const void* x;
+    void* out;
+    const float *pos, *freqs;
+    int64_t xs[3], os[3];       // strides in elements: batch item, token, head
+    int64_t T, pos_item;        // pos_item: elements between the positions of two batch items (0: shared)
+    int N, M, D, A, R;
+    bool interleaved, vec;      // vec: 16-byte pieces of pairs and of copied channels
+    float sign;                 // 1 forward, -1 backward
+};
+hipError_t launch_rotary(const RotaryParams& p, int dtype, hipStream_t stream);
+
+// ---------------------------------------------------------------- dense attention
+
+// The query heads that share a key head are packed: "row" r of a slab (batch item, key head) is query
+// r / G of query head kv * G + r % G, so that shared keys are read once for all of them and a single token
+// of G heads fills G rows of a matrix product.
+struct AttnParams {
+    const void *q, *k, *v, *o, *grad_out;  // o: the forward's result (backward)
+    void *out, *grad_q, *grad_k, *grad_v;
+    float* lse;                  // [N, M, Lq]; written by the forward (or null), read by the backward
+    float* delta;                // [N, M, Lq]: sum over channels of grad_out * o (backward)
+    const float *slopes, *q_pos, *k_pos;
+    const int *q_doc, *k_doc, *prefix;
+    int4 *k_ranges, *row_ranges;  // documents of each key tile [N, k_tiles] and row tile [N, row_tiles]
+    float* part;                  // partial results of the splits, or null with one split
+    int64_t qs[3], ks[3], vs[3];  // strides in elements: batch item, token, head
+    int N, Lq, Lk, M, Mkv, G, D;
+    int R;                        // rows of a slab: Lq * G
+    int k_tiles, row_tiles, blocks, splits;
+    int causal;
+    float scale, softcap;
+    bool q_vec, k_vec, v_vec, out_vec;  // read (or written) in 16-byte pieces
+};
+
+// How a call is cut up: waves per workgroup, workgroups per slab, splits of the other axis. Workgroups own
+// rows (forward, grad_q) or keys (grad_k and grad_v).
+struct AttnPlan {
+    int waves, blocks, splits;
+};
+AttnPlan attn_plan(const AttnParams& p, int dtype, bool own_keys);
+int attn_tile(int dtype);                            // keys or rows per tile in LDS
+int attn_channels(int D);                            // channels that the kernels hold: 32, 64 or 128
+hipError_t launch_attn_ranges(const AttnParams& p, int dtype, bool rows, hipStream_t stream);
+hipError_t launch_attn_forward(const AttnParams& p, int dtype, int waves, hipStream_t stream);
+hipError_t launch_attn_grad_q(const AttnParams& p, int dtype, int waves, hipStream_t stream);
+hipError_t launch_attn_grad_kv(const AttnParams& p, int dtype, int waves, hipStream_t stream);
+
+}  // namespace msda

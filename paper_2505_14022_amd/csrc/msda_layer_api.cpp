@@ -1,0 +1,436 @@
+// C ABI of the layer operators (layer norm, rotary positions, dense attention): argument checks and
+// launch (host code only).
+#include <math.h>
+#include <stdint.h>
+
+#include <hip/hip_runtime.h>
+
+#include "msda.h"
+#include "msda_layer.h"
+
+using msda::dtype_size;
+using msda::fail;
+using msda::is_aligned;
+using msda::ok;
+
+namespace {
+
+constexpr int64_t kMaxInt = 0x7fffffff;
+
+msda_status_t check_dtype(int dtype) {
+    if (dtype != MSDA_F32 && dtype != MSDA_F16 && dtype != MSDA_BF16)
+        return fail(MSDA_ERROR_INVALID_VALUE, "unknown dtype %d (expected MSDA_F32=0, MSDA_F16=1 or MSDA_BF16=2)", dtype);
+    return MSDA_SUCCESS;
+}
+
+msda_status_t check_norm(int64_t rows, int64_t C, int dtype) {
+    msda_status_t st = check_dtype(dtype);
+    if (st != MSDA_SUCCESS) return st;
+    if (rows < 0 || C < 1)
+        return fail(MSDA_ERROR_INVALID_VALUE, "rows=%lld must be >= 0 and C=%lld >= 1", (long long)rows, (long long)C);
+    if (C > MSDA_LAYERNORM_MAX_C)
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "C=%lld channels exceeds MSDA_LAYERNORM_MAX_C=%d", (long long)C,
+                    MSDA_LAYERNORM_MAX_C);
+    if (rows > (INT64_MAX >> 4) / C)
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "rows=%lld of C=%lld channels is too large", (long long)rows, (long long)C);
+    return MSDA_SUCCESS;
+}
+
+// Whether every given row tensor is read in 16-byte pieces.
+template <typename... P>
+bool norm_pieces(int64_t C, int dtype, P... ptr) {
+    return (C * dtype_size(dtype)) % 16 == 0 && (... && is_aligned(ptr, 16));
+}
+
+size_t norm_workspace(int64_t rows, int64_t C, int dtype) {
+    return rows == 0 ? 0 : (size_t)2 * msda::norm_backward_blocks(rows, C, dtype) * C * sizeof(float);
+}
+
+}  // namespace
+
+extern "C" {
+
+msda_status_t msda_layernorm_forward(const void* x, const void* residual, const float* weight, const float* bias,
+                                     void* out, void* sum, float* mean, float* rstd, int64_t rows, int64_t C,
+                                     float eps, int dtype, void* stream) {
+    msda_status_t st = check_norm(rows, C, dtype);
+    if (st != MSDA_SUCCESS) return st;
+    if (!(eps >= 0.f) || isinf(eps))
+        return fail(MSDA_ERROR_INVALID_VALUE, "eps=%g must be finite and >= 0", (double)eps);
+    if (rows == 0) return ok();
+    if (!x || !out) return fail(MSDA_ERROR_INVALID_VALUE, "x and out must be non-null");
+    const int es = dtype_size(dtype);
+    if (!is_aligned(x, es) || !is_aligned(residual, es) || !is_aligned(out, es) || !is_aligned(sum, es) ||
+        !is_aligned(weight, 4) || !is_aligned(bias, 4) || !is_aligned(mean, 4) || !is_aligned(rstd, 4))
+        return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: tensors need the alignment of their elements");
+    msda::NormParams p = {};
+    p.x = x;
+    p.residual = residual;
+    p.weight = weight;
+    p.bias = bias;
+    p.out = out;
+    p.sum = sum;
+    p.mean = mean;
+    p.rstd = rstd;
+    p.rows = rows;
+    p.C = (int)C;
+    p.eps = eps;
+    p.vec = norm_pieces(C, dtype, x, residual, (const void*)out, (const void*)sum);
+    hipError_t e = msda::launch_layernorm_forward(p, dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "layer norm launch: %s", hipGetErrorString(e));
+    return ok();
+}
+
+msda_status_t msda_layernorm_backward_workspace_size(int64_t rows, int64_t C, int dtype, size_t* bytes) {
+    if (!bytes) return fail(MSDA_ERROR_INVALID_VALUE, "bytes must be non-null");
+    *bytes = 0;
+    msda_status_t st = check_norm(rows, C, dtype);
+    if (st != MSDA_SUCCESS) return st;
+    *bytes = norm_workspace(rows, C, dtype);
+    return ok();
+}
+
+msda_status_t msda_layernorm_backward(const void* x, const void* residual, const float* weight, const void* grad_out,
+                                      const void* grad_sum, const float* mean, const float* rstd, void* grad_x,
+                                      float* grad_weight, float* grad_bias, void* workspace, size_t workspace_bytes,
+                                      int64_t rows, int64_t C, int dtype, void* stream) {
+    msda_status_t st = check_norm(rows, C, dtype);
+    if (st != MSDA_SUCCESS) return st;
+    const int es = dtype_size(dtype);
+    const bool sums = grad_weight || grad_bias;
+    if (!is_aligned(grad_weight, 4) || !is_aligned(grad_bias, 4))
+        return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: tensors need the alignment of their elements");
+    if (rows > 0) {
+        if (!x || !grad_out || !mean || !rstd || !grad_x)
+            return fail(MSDA_ERROR_INVALID_VALUE, "x, grad_out, mean, rstd and grad_x must be non-null");
+        if (!is_aligned(x, es) || !is_aligned(residual, es) || !is_aligned(grad_out, es) || !is_aligned(grad_sum, es) ||
+            !is_aligned(grad_x, es) || !is_aligned(weight, 4) || !is_aligned(mean, 4) || !is_aligned(rstd, 4))
+            return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: tensors need the alignment of their elements");
+        const size_t need = norm_workspace(rows, C, dtype);
+        if (sums && (!workspace || workspace_bytes < need))
+            return fail(MSDA_ERROR_INVALID_VALUE, "workspace of %zu bytes is smaller than the %zu needed",
+                        workspace ? workspace_bytes : (size_t)0, need);
+        if (sums && !is_aligned(workspace, 16))
+            return fail(MSDA_ERROR_INVALID_VALUE, "workspace must be 16-byte aligned");
+    }
+    msda::NormParams p = {};
+    p.x = x;
+    p.residual = residual;
+    p.weight = weight;
+    p.grad_out = grad_out;
+    p.grad_sum = grad_sum;
+    p.mean = const_cast<float*>(mean);
+    p.rstd = const_cast<float*>(rstd);
+    p.grad_x = grad_x;
+    p.partial = sums ? static_cast<float*>(workspace) : nullptr;
+    p.grad_weight = grad_weight;
+    p.grad_bias = grad_bias;
+    p.rows = rows;
+    p.C = (int)C;
+    p.blocks = msda::norm_backward_blocks(rows, C, dtype);
+    p.vec = norm_pieces(C, dtype, x, residual, grad_out, grad_sum, (const void*)grad_x);
+    hipError_t e = msda::launch_layernorm_backward(p, dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "layer norm backward launch: %s", hipGetErrorString(e));
+    return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- rotary positions
+
+namespace {
+
+msda_status_t rotary(const char* in_name, const void* x, const int64_t* x_stride, const float* pos, const float* freqs,
+                     const char* out_name, void* out, const int64_t* out_stride, int64_t N, int64_t T, int64_t M,
+                     int64_t D, int64_t A, int64_t R, int64_t pos_items, int interleaved, int dtype, float sign,
+                     void* stream) {
+    msda_status_t st = check_dtype(dtype);
+    if (st != MSDA_SUCCESS) return st;
+    if (N < 0 || T < 0 || M < 1 || D < 1)
+        return fail(MSDA_ERROR_INVALID_VALUE, "N=%lld and T=%lld must be >= 0, M=%lld and D=%lld >= 1", (long long)N,
+                    (long long)T, (long long)M, (long long)D);
+    if (A < 1 || A > 4) return fail(MSDA_ERROR_INVALID_VALUE, "A=%lld axes: 1 to 4 are taken", (long long)A);
+    if (R < 0 || R > D / 2)
+        return fail(MSDA_ERROR_INVALID_VALUE, "R=%lld pairs do not fit into D=%lld channels", (long long)R, (long long)D);
+    if (pos_items != 1 && pos_items != N)
+        return fail(MSDA_ERROR_INVALID_VALUE, "pos_items=%lld must be 1 or N=%lld", (long long)pos_items, (long long)N);
+    if (D > MSDA_ROTARY_MAX_D)
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "D=%lld channels per head exceeds MSDA_ROTARY_MAX_D=%d", (long long)D,
+                    MSDA_ROTARY_MAX_D);
+    if (M > 65536 / D)
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "M*D of M=%lld, D=%lld exceeds 65536", (long long)M, (long long)D);
+    if (N > kMaxInt || T > kMaxInt) return fail(MSDA_ERROR_NOT_SUPPORTED, "N or T exceeds 2^31-1");
+    if (N * T == 0) return ok();
+    if (!x || !out || (R > 0 && (!pos || !freqs)))
+        return fail(MSDA_ERROR_INVALID_VALUE, "%s, pos, freqs and %s must be non-null", in_name, out_name);
+    const int es = dtype_size(dtype);
+    if (!is_aligned(x, es) || !is_aligned(out, es) || !is_aligned(pos, 4) || !is_aligned(freqs, 4))
+        return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: tensors need the alignment of their elements");
+    msda::RotaryParams p = {};
+    const int64_t whole[3] = {T * M * D, M * D, D}, extent[3] = {N, T, M};
+    bool pieces = is_aligned(x, 16) && is_aligned(out, 16);
+    for (int i = 0; i < 3; ++i) {
+        p.xs[i] = x_stride ? x_stride[i] : whole[i];
+        p.os[i] = out_stride ? out_stride[i] : whole[i];
+        if (extent[i] > 1 && p.os[i] == 0)
+            return fail(MSDA_ERROR_INVALID_VALUE, "%s has a stride of 0 over %lld entries", out_name, (long long)extent[i]);
+        // a stride over a single entry is never used
+        if (extent[i] > 1) pieces = pieces && (p.xs[i] * es) % 16 == 0 && (p.os[i] * es) % 16 == 0;
+    }
+    const int64_t per = 16 / es;
+    p.x = x;
+    p.out = out;
+    p.pos = pos;
+    p.freqs = freqs;
+    p.T = T;
+    p.N = (int)N;
+    p.M = (int)M;
+    p.D = (int)D;
+    p.A = (int)A;
+    p.R = (int)R;
+    p.pos_item = pos_items == N && N > 1 ? T * A : 0;
+    p.interleaved = interleaved != 0;
+    p.vec = pieces && R % per == 0 && D % per == 0;
+    p.sign = sign;
+    hipError_t e = msda::launch_rotary(p, dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "rotary launch: %s", hipGetErrorString(e));
+    return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+msda_status_t msda_rotary_forward(const void* x, const int64_t* x_stride, const float* pos, const float* freqs,
+                                  void* out, const int64_t* out_stride, int64_t N, int64_t T, int64_t M, int64_t D,
+                                  int64_t A, int64_t R, int64_t pos_items, int interleaved, int dtype, void* stream) {
+    return rotary("x", x, x_stride, pos, freqs, "out", out, out_stride, N, T, M, D, A, R, pos_items, interleaved, dtype,
+                  1.f, stream);
+}
+
+msda_status_t msda_rotary_backward(const void* grad_out, const int64_t* grad_out_stride, const float* pos,
+                                   const float* freqs, void* grad_x, const int64_t* grad_x_stride, int64_t N, int64_t T,
+                                   int64_t M, int64_t D, int64_t A, int64_t R, int64_t pos_items, int interleaved,
+                                   int dtype, void* stream) {
+    return rotary("grad_out", grad_out, grad_out_stride, pos, freqs, "grad_x", grad_x, grad_x_stride, N, T, M, D, A, R,
+                  pos_items, interleaved, dtype, -1.f, stream);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- dense attention
+
+namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t round_up(size_t b) { return (b + 255) / 256 * 256; }
+
+msda_status_t check_attention(const msda_attention_t* a) {
+    if (!a) return fail(MSDA_ERROR_INVALID_VALUE, "the attention's description must be non-null");
+    msda_status_t st = check_dtype(a->dtype);
+    if (st != MSDA_SUCCESS) return st;
+    if (a->N < 0 || a->Lq < 0 || a->Lk < 0)
+        return fail(MSDA_ERROR_INVALID_VALUE, "N=%lld, Lq=%lld and Lk=%lld must be >= 0", (long long)a->N,
+                    (long long)a->Lq, (long long)a->Lk);
+    if (a->M < 1 || a->Mkv < 1 || a->D < 1 || a->M % a->Mkv != 0)
+        return fail(MSDA_ERROR_INVALID_VALUE, "M=%lld, Mkv=%lld and D=%lld must be >= 1 and M a multiple of Mkv",
+                    (long long)a->M, (long long)a->Mkv, (long long)a->D);
+    if (a->D > MSDA_ATTENTION_MAX_D)
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "D=%lld channels per head exceeds MSDA_ATTENTION_MAX_D=%d",
+                    (long long)a->D, MSDA_ATTENTION_MAX_D);
+    if (!(a->scale > 0.f) || isinf(a->scale))
+        return fail(MSDA_ERROR_INVALID_VALUE, "scale=%g must be finite and > 0", (double)a->scale);
+    if (!(a->softcap >= 0.f) || isinf(a->softcap))
+        return fail(MSDA_ERROR_INVALID_VALUE, "softcap=%g must be finite and >= 0", (double)a->softcap);
+    if (a->causal && a->Lk < a->Lq)
+        return fail(MSDA_ERROR_INVALID_VALUE, "causal needs Lk=%lld >= Lq=%lld", (long long)a->Lk, (long long)a->Lq);
+    if (a->N > kMaxInt || a->M > kMaxInt || a->Lk > kMaxInt - 1024 || a->Lq > (kMaxInt - 1024) / (a->M / a->Mkv))
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "N, M, Lk or Lq * M / Mkv exceeds 2^31");
+    // every launch is one grid: at most 2^30 slabs (batch item, key head) and 2^33 of their rows or keys, in at
+    // least 32 per workgroup of the attention kernels and 4 of the ones that add splits
+    const double slabs = (double)a->N * (double)a->Mkv, rows = (double)a->Lq * (double)(a->M / a->Mkv);
+    if (slabs > 1073741824.0 || slabs * rows > 8589934592.0 || slabs * (double)a->Lk > 8589934592.0)
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "N * Mkv heads of these lengths are too many for one launch");
+    // with empty extents any table may be null; the pointers are not looked at then
+    if (a->N > 0 && a->Lq > 0 && a->Lk > 0) {
+        if ((a->q_doc != nullptr) != (a->k_doc != nullptr))
+            return fail(MSDA_ERROR_INVALID_VALUE, "q_doc and k_doc must be given both or neither");
+        if (a->slopes && (!a->q_pos || !a->k_pos))
+            return fail(MSDA_ERROR_INVALID_VALUE, "slopes need q_pos and k_pos");
+        if (!is_aligned(a->slopes, 4) || !is_aligned(a->q_pos, 8) || !is_aligned(a->k_pos, 8) || !is_aligned(a->q_doc, 4) ||
+            !is_aligned(a->k_doc, 4) || !is_aligned(a->prefix, 4))
+            return fail(MSDA_ERROR_INVALID_VALUE, "misaligned table: positions need 8 bytes, the others 4");
+    }
+    return MSDA_SUCCESS;
+}
+
+// The kernels' view of a call. The workspace's pieces in order: documents of the key tiles and row tiles,
+// delta (backward), partial results of the splits.
+struct Attention {
+    msda::AttnParams p = {};
+    msda::AttnPlan rows = {1, 0, 1}, keys = {1, 0, 1};
+    size_t at_row_ranges = 0, at_delta = 0, at_part = 0, bytes = 0;
+};
+
+bool row_pieces(const void* base, const int64_t* stride, const int64_t* extent, int64_t D, int es) {
+    bool yes = is_aligned(base, 16) && (D * es) % 16 == 0;
+    for (int i = 0; i < 3; ++i) yes = yes && (extent[i] <= 1 || (stride[i] * es) % 16 == 0);
+    return yes;
+}
+
+Attention attention_of(const msda_attention_t& a, bool backward) {
+    Attention x;
+    msda::AttnParams& p = x.p;
+    const int64_t G = a.M / a.Mkv, tile = msda::attn_tile(a.dtype), DP = msda::attn_channels((int)a.D);
+    p.N = (int)a.N;
+    p.Lq = (int)a.Lq;
+    p.Lk = (int)a.Lk;
+    p.M = (int)a.M;
+    p.Mkv = (int)a.Mkv;
+    p.G = (int)G;
+    p.D = (int)a.D;
+    p.R = (int)(a.Lq * G);
+    p.k_tiles = (int)ceil_div(a.Lk, tile);
+    p.row_tiles = (int)ceil_div(p.R, tile);
+    p.causal = a.causal != 0;
+    p.scale = a.scale;
+    p.softcap = a.softcap;
+    for (int i = 0; i < 3; ++i) {
+        p.qs[i] = a.q_stride[i];
+        p.ks[i] = a.k_stride[i];
+        p.vs[i] = a.v_stride[i];
+    }
+    if (a.Lq > 0 && a.Lk > 0) {
+        p.slopes = a.slopes;
+        p.q_pos = a.q_pos;
+        p.k_pos = a.k_pos;
+        p.q_doc = a.q_doc;
+        p.k_doc = a.k_doc;
+        p.prefix = a.prefix;
+    }
+    const size_t slabs = (size_t)(a.N * a.Mkv);
+    if (a.Lq > 0) x.rows = msda::attn_plan(p, a.dtype, false);
+    if (backward && a.Lk > 0) x.keys = msda::attn_plan(p, a.dtype, true);
+    const bool docs = p.q_doc != nullptr;
+    x.at_row_ranges = docs ? round_up(sizeof(int4) * a.N * p.k_tiles) : 0;
+    x.at_delta = x.at_row_ranges + (docs && backward ? round_up(sizeof(int4) * a.N * p.row_tiles) : 0);
+    x.at_part = x.at_delta + (backward ? round_up(sizeof(float) * a.N * a.M * a.Lq) : 0);
+    size_t part = 0;
+    if (x.rows.splits > 1) part = slabs * p.R * x.rows.splits * (DP + (backward ? 0 : 2));
+    if (x.keys.splits > 1) {
+        const size_t b = slabs * p.Lk * x.keys.splits * 2 * DP;
+        if (b > part) part = b;
+    }
+    x.bytes = x.at_part + part * sizeof(float);
+    return x;
+}
+
+msda_status_t check_workspace(const Attention& x, const void* workspace, size_t bytes) {
+    if (x.bytes > 0 && (!workspace || bytes < x.bytes))
+        return fail(MSDA_ERROR_INVALID_VALUE, "workspace of %zu bytes is smaller than the %zu needed",
+                    workspace ? bytes : (size_t)0, x.bytes);
+    if (x.bytes > 0 && !is_aligned(workspace, 16))
+        return fail(MSDA_ERROR_INVALID_VALUE, "workspace must be 16-byte aligned");
+    return MSDA_SUCCESS;
+}
+
+void bind(Attention& x, const msda_attention_t& a, const void* q, const void* k, const void* v, void* workspace) {
+    msda::AttnParams& p = x.p;
+    const int es = dtype_size(a.dtype);
+    const int64_t qe[3] = {a.N, a.Lq, a.M}, ke[3] = {a.N, a.Lk, a.Mkv};
+    p.q = q;
+    p.k = k;
+    p.v = v;
+    p.q_vec = row_pieces(q, p.qs, qe, a.D, es);
+    p.k_vec = row_pieces(k, p.ks, ke, a.D, es);
+    p.v_vec = row_pieces(v, p.vs, ke, a.D, es);
+    p.out_vec = (a.D * es) % 16 == 0;
+    char* ws = static_cast<char*>(workspace);
+    p.k_ranges = reinterpret_cast<int4*>(ws);
+    p.row_ranges = reinterpret_cast<int4*>(ws + x.at_row_ranges);
+    p.delta = reinterpret_cast<float*>(ws + x.at_delta);
+    p.part = reinterpret_cast<float*>(ws + x.at_part);
+}
+
+void take_plan(msda::AttnParams& p, const msda::AttnPlan& plan) {
+    p.blocks = plan.blocks;
+    p.splits = plan.splits;
+}
+
+}  // namespace
+
+extern "C" {
+
+msda_status_t msda_attention_workspace_size(const msda_attention_t* a, int backward, size_t* bytes) {
+    if (!bytes) return fail(MSDA_ERROR_INVALID_VALUE, "bytes must be non-null");
+    *bytes = 0;
+    msda_status_t st = check_attention(a);
+    if (st != MSDA_SUCCESS) return st;
+    if (a->N > 0) *bytes = attention_of(*a, backward != 0).bytes;
+    return ok();
+}
+
+msda_status_t msda_attention_forward(const msda_attention_t* a, const void* q, const void* k, const void* v, void* out,
+                                     float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    msda_status_t st = check_attention(a);
+    if (st != MSDA_SUCCESS) return st;
+    if (a->N * a->Lq == 0) return ok();
+    const int es = dtype_size(a->dtype);
+    if (!q || !out || (a->Lk > 0 && (!k || !v)))
+        return fail(MSDA_ERROR_INVALID_VALUE, "q, k, v and out must be non-null");
+    if (!is_aligned(q, es) || !is_aligned(k, es) || !is_aligned(v, es) || !is_aligned(out, 16) || !is_aligned(lse, 4))
+        return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: out needs 16 bytes, lse 4, q, k and v their element's");
+    Attention x = attention_of(*a, false);
+    st = check_workspace(x, workspace, workspace_bytes);
+    if (st != MSDA_SUCCESS) return st;
+    bind(x, *a, q, k, v, workspace);
+    x.p.out = out;
+    x.p.lse = lse;
+    take_plan(x.p, x.rows);
+    hipError_t e = hipSuccess;
+    if (x.p.q_doc) e = msda::launch_attn_ranges(x.p, a->dtype, false, (hipStream_t)stream);
+    if (e == hipSuccess) e = msda::launch_attn_forward(x.p, a->dtype, x.rows.waves, (hipStream_t)stream);
+    if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "attention launch: %s", hipGetErrorString(e));
+    return ok();
+}
+
+msda_status_t msda_attention_backward(const msda_attention_t* a, const void* q, const void* k, const void* v,
+                                      const void* out, const float* lse, const void* grad_out, void* grad_q,
+                                      void* grad_k, void* grad_v, void* workspace, size_t workspace_bytes,
+                                      void* stream) {
+    msda_status_t st = check_attention(a);
+    if (st != MSDA_SUCCESS) return st;
+    if (a->N == 0 || (a->Lq == 0 && a->Lk == 0)) return ok();
+    const int es = dtype_size(a->dtype);
+    if ((a->Lq > 0 && (!q || !out || !lse || !grad_out || !grad_q)) || (a->Lk > 0 && (!k || !v || !grad_k || !grad_v)))
+        return fail(MSDA_ERROR_INVALID_VALUE,
+                    "q, k, v, out, lse, grad_out, grad_q, grad_k and grad_v must be non-null");
+    if (!is_aligned(q, es) || !is_aligned(k, es) || !is_aligned(v, es) || !is_aligned(lse, 4) || !is_aligned(out, 16) ||
+        !is_aligned(grad_out, 16) || !is_aligned(grad_q, 16) || !is_aligned(grad_k, 16) || !is_aligned(grad_v, 16))
+        return fail(MSDA_ERROR_INVALID_VALUE,
+                    "misaligned pointer: out and the gradients need 16 bytes, lse 4, q, k and v their element's");
+    Attention x = attention_of(*a, true);
+    st = check_workspace(x, workspace, workspace_bytes);
+    if (st != MSDA_SUCCESS) return st;
+    bind(x, *a, q, k, v, workspace);
+    x.p.o = out;
+    x.p.lse = const_cast<float*>(lse);
+    x.p.grad_out = grad_out;
+    x.p.grad_q = grad_q;
+    x.p.grad_k = grad_k;
+    x.p.grad_v = grad_v;
+    hipError_t e = hipSuccess;
+    if (x.p.q_doc) e = msda::launch_attn_ranges(x.p, a->dtype, true, (hipStream_t)stream);
+    if (e == hipSuccess && a->Lq > 0) {  // writes delta, which grad_k and grad_v need
+        take_plan(x.p, x.rows);
+        e = msda::launch_attn_grad_q(x.p, a->dtype, x.rows.waves, (hipStream_t)stream);
+    }
+    if (e == hipSuccess && a->Lk > 0) {
+        take_plan(x.p, x.keys);
+        e = msda::launch_attn_grad_kv(x.p, a->dtype, x.keys.waves, (hipStream_t)stream);
+    }
+    if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "attention backward launch: %s", hipGetErrorString(e));
+    return ok();
+}
+
+}  // extern "C"

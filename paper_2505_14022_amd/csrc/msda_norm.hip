@@ -1,0 +1,330 @@
+// Layer norm with a residual addition, forward and backward.
+//   s = x + residual;  xh = (s - mean) * rstd;  out = xh * weight + bias
+//   grad_x = rstd * (g - mean(g) - xh * mean(g * xh)) + grad_sum,  g = grad_out * weight
+//   grad_weight = sum over rows of grad_out * xh,  grad_bias = sum over rows of grad_out
+// Both directions are bound by memory: every tensor is read or written once. A row stays in the
+// registers of the G lanes that own it (G = 8 .. 64 lanes of a wave, or a whole workgroup for long
+// rows), so the mean and the sum of squared distances from it are two reductions over registers, not two
+// passes over memory, and the variance never comes from a difference of large sums. Lanes keep their
+// columns from row to row: weight and bias are loaded once, and in the backward each lane sums its columns'
+// grad_weight and grad_bias in registers over all its rows. A workgroup writes one row of partial sums,
+// and a second kernel adds the workgroups' rows in a fixed order.
+#include "msda_layer.h"
+#include "msda_layer.hpp"
+
+namespace msda {
+namespace {
+
+// Sums of NX values over the G lanes of a row; every lane of the row gets them. With G = NT the row is
+// the workgroup's: `red` holds the waves' sums, and all threads take part.
+template <int NT, int G, int NX>
+__device__ __forceinline__ void row_sums(float (&x)[NX], float* red) {
+#pragma unroll
+    for (int k = 0; k < NX; ++k) x[k] = group_sum<(G < 64 ? G : 64)>(x[k]);
+    if constexpr (G > 64) {
+        constexpr int W = NT / 64;
+        __syncthreads();  // the last sums have been read
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < NX; ++k) red[k * W + (threadIdx.x >> 6)] = x[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < NX; ++k) {
+            float t = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) t += red[k * W + w];
+            x[k] = t;
+        }
+    }
+}
+
+template <typename T, int VEC, int NT, int G, int NV>
+__global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
+    __shared__ float red[NT / 64];
+    const int g = threadIdx.x % G;
+    const int C = p.C;
+    const float inv_c = 1.f / (float)C;
+    float w[NV][VEC], b[NV][VEC];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * G + g) * VEC;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            w[j][i] = p.weight && c + i < C ? p.weight[c + i] : 1.f;
+            b[j][i] = p.bias && c + i < C ? p.bias[c + i] : 0.f;
+        }
+    }
+    const T* x = static_cast<const T*>(p.x);
+    const T* r = static_cast<const T*>(p.residual);
+    for (int64_t row = (int64_t)blockIdx.x * (NT / G) + threadIdx.x / G; row < p.rows;
+         row += (int64_t)gridDim.x * (NT / G)) {
+        const int64_t at = row * C;
+        float s[NV][VEC];
+        float sum[1] = {0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * G + g) * VEC;
+            if (c < C) {
+                load_piece(s[j], x + at + c);
+                if (r) {
+                    float y[VEC];
+                    load_piece(y, r + at + c);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) s[j][i] += y[i];
+                }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum[0] += s[j][i];
+            }
+        }
+        row_sums<NT, G>(sum, red);
+        const float mean = sum[0] * inv_c;
+        float sq[1] = {0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * G + g) * VEC;
+            if (c < C) {
+                if (p.sum) store_piece(static_cast<T*>(p.sum) + at + c, s[j]);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    s[j][i] -= mean;
+                    sq[0] += s[j][i] * s[j][i];
+                }
+            }
+        }
+        row_sums<NT, G>(sq, red);
+        const float rstd = 1.f / sqrtf(sq[0] * inv_c + p.eps);
+        if (g == 0) {
+            if (p.mean) p.mean[row] = mean;
+            if (p.rstd) p.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * G + g) * VEC;
+            if (c < C) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) s[j][i] = s[j][i] * rstd * w[j][i] + b[j][i];
+                store_piece(static_cast<T*>(p.out) + at + c, s[j]);
+            }
+        }
+    }
+}
+
+template <typename T, int VEC, int NT, int G, int NV>
+__global__ __launch_bounds__(NT) void norm_bwd_kernel(NormParams p) {
+    constexpr int kRows = NT / G;
+    __shared__ float red[2 * NT / 64];
+    __shared__ float cols[kRows > 1 ? NT * NV * VEC : 1];
+    const int g = threadIdx.x % G;
+    const int C = p.C;
+    const float inv_c = 1.f / (float)C;
+    float w[NV][VEC], gw[NV][VEC], gb[NV][VEC];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * G + g) * VEC;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            w[j][i] = p.weight && c + i < C ? p.weight[c + i] : 1.f;
+            gw[j][i] = gb[j][i] = 0.f;
+        }
+    }
+    const T* x = static_cast<const T*>(p.x);
+    const T* r = static_cast<const T*>(p.residual);
+    const T* go = static_cast<const T*>(p.grad_out);
+    const T* gs = static_cast<const T*>(p.grad_sum);
+    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G; row < p.rows;
+         row += (int64_t)gridDim.x * kRows) {
+        const int64_t at = row * C;
+        const float mean = p.mean[row], rstd = p.rstd[row];
+        float xh[NV][VEC], gv[NV][VEC];
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * G + g) * VEC;
+            if (c < C) {
+                load_piece(xh[j], x + at + c);
+                load_piece(gv[j], go + at + c);
+                if (r) {
+                    float y[VEC];
+                    load_piece(y, r + at + c);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) xh[j][i] += y[i];
+                }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    xh[j][i] = (xh[j][i] - mean) * rstd;
+                    gw[j][i] += gv[j][i] * xh[j][i];
+                    gb[j][i] += gv[j][i];
+                    gv[j][i] *= w[j][i];
+                    s[0] += gv[j][i];
+                    s[1] += gv[j][i] * xh[j][i];
+                }
+            }
+        }
+        row_sums<NT, G>(s, red);
+        const float m0 = s[0] * inv_c, m1 = s[1] * inv_c;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * G + g) * VEC;
+            if (c < C) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) gv[j][i] = rstd * (gv[j][i] - m0 - xh[j][i] * m1);
+                if (gs) {
+                    float y[VEC];
+                    load_piece(y, gs + at + c);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) gv[j][i] += y[i];
+                }
+                store_piece(static_cast<T*>(p.grad_x) + at + c, gv[j]);
+            }
+        }
+    }
+    if (!p.partial) return;
+    float* part = p.partial + (int64_t)blockIdx.x * C;
+    for (int which = 0; which < 2; ++which, part += (int64_t)gridDim.x * C) {
+        if constexpr (kRows > 1) {
+            // the workgroup's rows: one after the other's columns in LDS, then added up column by column
+            if (which) __syncthreads();
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    cols[(threadIdx.x / G) * (G * NV * VEC) + (j * G + g) * VEC + i] = which ? gb[j][i] : gw[j][i];
+            __syncthreads();
+            for (int c = threadIdx.x; c < C; c += NT) {
+                float t = 0.f;
+#pragma unroll
+                for (int k = 0; k < kRows; ++k) t += cols[k * (G * NV * VEC) + c];
+                part[c] = t;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int c = (j * G + g) * VEC;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (c + i < C) part[c + i] = which ? gb[j][i] : gw[j][i];
+            }
+        }
+    }
+}
+
+// The workgroups' partial sums added up: 32 columns by 32 runs of workgroups per workgroup.
+__global__ __launch_bounds__(1024) void norm_sum_kernel(const float* partial, float* grad_weight, float* grad_bias,
+                                                        int C, int blocks) {
+    __shared__ float s[32][33];
+    float* out = blockIdx.y ? grad_bias : grad_weight;
+    if (!out) return;
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
+    const float* col = partial + (int64_t)blockIdx.y * blocks * C + c;
+    float t = 0.f;
+    if (c < C)
+        for (int b = k; b < blocks; b += 32) t += col[(int64_t)b * C];
+    s[k][threadIdx.x & 31] = t;
+    __syncthreads();
+    if (k == 0 && c < C) {
+        t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t += s[i][threadIdx.x];
+        out[c] = t;
+    }
+}
+
+__global__ __launch_bounds__(256) void norm_zero_kernel(float* grad_weight, float* grad_bias, int C) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= C) return;
+    if (grad_weight) grad_weight[c] = 0.f;
+    if (grad_bias) grad_bias[c] = 0.f;
+}
+
+// Lanes per row and the row's pieces per lane: a lane keeps at most 16 elements, since the backward holds
+// five values of each. Called with a functor taking (threads, lanes, pieces) as integral constants.
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+template <int VEC, typename F>
+hipError_t by_row(int C, F f) {
+    const int n = (C + VEC - 1) / VEC;
+    if (n <= 8) return f(Int<256>(), Int<8>(), Int<1>());
+    if (n <= 16) return f(Int<256>(), Int<16>(), Int<1>());
+    if (n <= 32) return f(Int<256>(), Int<32>(), Int<1>());
+    if (n <= 64) return f(Int<256>(), Int<64>(), Int<1>());
+    if (n <= 128) return f(Int<256>(), Int<64>(), Int<2>());
+    if (n <= 256) return f(Int<256>(), Int<256>(), Int<1>());
+    if (n <= 512) return f(Int<256>(), Int<256>(), Int<2>());
+    if (n <= 1024) return f(Int<1024>(), Int<1024>(), Int<1>());
+    if constexpr (VEC < 16) {
+        if (n <= 2048) return f(Int<1024>(), Int<1024>(), Int<2>());
+    }
+    if constexpr (VEC <= 4) {
+        if (n <= 4096) return f(Int<1024>(), Int<1024>(), Int<4>());
+    }
+    if constexpr (VEC == 1) return f(Int<1024>(), Int<1024>(), Int<16>());
+    return hipErrorInvalidValue;
+}
+
+// Rows of a workgroup of the backward (as by_row, for the host).
+int rows_per_block(int64_t C, int vec) {
+    const int64_t n = (C + vec - 1) / vec;
+    return n <= 8 ? 32 : n <= 16 ? 16 : n <= 32 ? 8 : n <= 128 ? 4 : 1;
+}
+
+template <typename T, int VEC, bool BWD>
+hipError_t launch_rows_of(const NormParams& p, hipStream_t stream) {
+    return by_row<VEC>(p.C, [&](auto nt, auto g, auto nv) {
+        constexpr int NT = decltype(nt)::value, G = decltype(g)::value, NV = decltype(nv)::value;
+        const int64_t need = (p.rows + NT / G - 1) / (NT / G);
+        if constexpr (BWD) {
+            hipLaunchKernelGGL((norm_bwd_kernel<T, VEC, NT, G, NV>), dim3(p.blocks), dim3(NT), 0, stream, p);
+        } else {
+            const int64_t most = 2048 * 256 / NT;  // every CU full: lanes keep weight and bias over several rows
+            hipLaunchKernelGGL((norm_fwd_kernel<T, VEC, NT, G, NV>), dim3((unsigned)(need < most ? need : most)),
+                               dim3(NT), 0, stream, p);
+        }
+        return hipGetLastError();
+    });
+}
+
+template <typename T, bool BWD>
+hipError_t launch_typed(const NormParams& p, hipStream_t stream) {
+    return p.vec ? launch_rows_of<T, 16 / sizeof(T), BWD>(p, stream) : launch_rows_of<T, 1, BWD>(p, stream);
+}
+
+template <bool BWD>
+hipError_t launch_norm(const NormParams& p, int dtype, hipStream_t stream) {
+    if (dtype == MSDA_F32) return launch_typed<float, BWD>(p, stream);
+    if (dtype == MSDA_F16) return launch_typed<_Float16, BWD>(p, stream);
+    return launch_typed<bf16_t, BWD>(p, stream);
+}
+
+}  // namespace
+
+int norm_backward_blocks(int64_t rows, int64_t C, int dtype) {
+    // the count must not depend on the pointers' alignment: rows that fill a workgroup in 16-byte pieces
+    const int vec = (C * dtype_size(dtype)) % 16 == 0 ? 16 / dtype_size(dtype) : 1;
+    const int64_t need = (rows + rows_per_block(C, vec) - 1) / rows_per_block(C, vec);
+    const int64_t most = 1024;
+    if (need <= most) return (int)(need < 1 ? 1 : need);
+    const int64_t turns = (need + most - 1) / most;  // rows per workgroup, as even as can be
+    return (int)((need + turns - 1) / turns);
+}
+
+hipError_t launch_layernorm_forward(const NormParams& p, int dtype, hipStream_t stream) {
+    return launch_norm<false>(p, dtype, stream);
+}
+
+hipError_t launch_layernorm_backward(const NormParams& p, int dtype, hipStream_t stream) {
+    if (p.rows == 0) {
+        if (!p.grad_weight && !p.grad_bias) return hipSuccess;
+        hipLaunchKernelGGL(norm_zero_kernel, dim3((p.C + 255) / 256), dim3(256), 0, stream, p.grad_weight, p.grad_bias,
+                           p.C);
+        return hipGetLastError();
+    }
+    hipError_t e = launch_norm<true>(p, dtype, stream);
+    if (e != hipSuccess || !p.partial) return e;
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((p.C + 31) / 32, 2), dim3(1024), 0, stream, p.partial, p.grad_weight,
+                       p.grad_bias, p.C, p.blocks);
+    return hipGetLastError();
+}
+
+}  // namespace msda

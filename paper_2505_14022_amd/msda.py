@@ -23,7 +23,11 @@ MSDA_ERROR_NOT_SUPPORTED = 2
 MSDA_ERROR_LAUNCH_FAILED = 3
 MSDA_F32 = 0
 MSDA_F16 = 1
+MSDA_BF16 = 2
 MSDA_MAX_LEVELS = 16
+MSDA_LAYERNORM_MAX_C = 16384
+MSDA_ROTARY_MAX_D = 1024
+MSDA_ATTENTION_MAX_D = 128
 MSDA_WORKSPACE_PREFERRED = 0
 MSDA_WORKSPACE_OWNER = 1
 MSDA_WORKSPACE_DETERMINISTIC = 2
@@ -31,7 +35,10 @@ MSDA_WORKSPACE_DETERMINISTIC = 2
 EXPORTED = ["msda_check_args", "msda_forward", "msda_backward", "msda_backward_atomic",
             "msda_backward_deterministic", "msda_backward_workspace_size",
             "msda_forward_fused", "msda_backward_fused_workspace_size", "msda_backward_fused",
-            "msda_status_string", "msda_last_error", "msda_version", "msda_release", "msda_backward_noalloc"]
+            "msda_status_string", "msda_last_error", "msda_version", "msda_release", "msda_backward_noalloc",
+            "msda_layernorm_forward", "msda_layernorm_backward", "msda_layernorm_backward_workspace_size",
+            "msda_rotary_forward", "msda_rotary_backward",
+            "msda_attention_forward", "msda_attention_backward", "msda_attention_workspace_size"]
 MSDA_NOALLOC_SCRATCH_BYTES = 128 << 20
 
 
@@ -39,6 +46,14 @@ class MsdaError(RuntimeError):
     def __init__(self, status: int, where: str, detail: str):
         self.status = status
         super().__init__(f"{where}: {status_string(status)}: {detail}")
+
+
+class AttentionDescription(ctypes.Structure):
+    """msda_attention_t."""
+    _fields_ = [(name, ctypes.c_int64) for name in ("N", "Lq", "Lk", "M", "Mkv", "D")] + \
+        [("dtype", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + \
+        [(name, ctypes.c_int64 * 3) for name in ("q_stride", "k_stride", "v_stride")] + \
+        [(name, ctypes.c_void_p) for name in ("slopes", "q_pos", "k_pos", "q_doc", "k_doc", "prefix")]
 
 
 _lib = None
@@ -83,6 +98,24 @@ def lib():
         L.msda_version.restype = ctypes.c_int
         L.msda_release.argtypes = []
         L.msda_release.restype = ctypes.c_int
+        f32, size, sizep = ctypes.c_float, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+        L.msda_layernorm_forward.argtypes = [vp] * 8 + [i64, i64, f32, ctypes.c_int, vp]
+        L.msda_layernorm_forward.restype = ctypes.c_int
+        L.msda_layernorm_backward_workspace_size.argtypes = [i64, i64, ctypes.c_int, sizep]
+        L.msda_layernorm_backward_workspace_size.restype = ctypes.c_int
+        L.msda_layernorm_backward.argtypes = [vp] * 11 + [size, i64, i64, ctypes.c_int, vp]
+        L.msda_layernorm_backward.restype = ctypes.c_int
+        L.msda_rotary_forward.argtypes = [vp, ip, vp, vp, vp, ip] + [i64] * 7 + [ctypes.c_int, ctypes.c_int, vp]
+        L.msda_rotary_forward.restype = ctypes.c_int
+        L.msda_rotary_backward.argtypes = L.msda_rotary_forward.argtypes
+        L.msda_rotary_backward.restype = ctypes.c_int
+        desc = ctypes.POINTER(AttentionDescription)
+        L.msda_attention_workspace_size.argtypes = [desc, ctypes.c_int, sizep]
+        L.msda_attention_workspace_size.restype = ctypes.c_int
+        L.msda_attention_forward.argtypes = [desc] + [vp] * 6 + [size, vp]
+        L.msda_attention_forward.restype = ctypes.c_int
+        L.msda_attention_backward.argtypes = [desc] + [vp] * 10 + [size, vp]
+        L.msda_attention_backward.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -411,3 +444,275 @@ def backward_fused_raw(value_ptr: int, shapes: np.ndarray, starts: np.ndarray, r
     return lib().msda_backward_fused(value_ptr, _iptr(shapes), _iptr(starts), ref_ptr, off_ptr, logit_ptr,
                                      gout_ptr, gv_ptr, gref_ptr, goff_ptr, glog_ptr, ws_ptr, ws_bytes, *dims,
                                      dtype, stream)
+
+
+# ---------------------------------------------------------------- layer operators
+
+
+def _layer_dtype(t) -> int:
+    import torch
+
+    if t.dtype == torch.bfloat16:
+        return MSDA_BF16
+    if t.dtype in (torch.float32, torch.float16):
+        return _dtype_code(t)
+    raise ValueError(f"dtype must be float32, float16 or bfloat16, got {t.dtype}")
+
+
+def _expect(name, t, shape, dtype, like, strided=False):
+    """Checks one tensor argument: its shape and dtype, the device of `like`, and contiguity (with
+    `strided`, of the channels alone). None passes."""
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    if not t.is_cuda:
+        raise ValueError("tensor arguments must be device tensors")
+    if strided:
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"the channels of {name} must be contiguous")
+    elif not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+@contextlib.contextmanager
+def _launching(t, stream):
+    """Makes the device of `t` current and yields the stream handle of a call on it: `stream`, or torch's
+    current stream of that device. Memory that torch allocates meanwhile is for use on that stream."""
+    import torch
+
+    if isinstance(stream, torch.cuda.Stream) and stream.device != t.device:
+        raise ValueError(f"the stream is of {stream.device}, the tensors are on {t.device}")
+    here = t.device.index == torch.cuda.current_device()
+    with _NO_CONTEXT if here else torch.cuda.device(t.device), _on(stream):
+        yield _stream(stream)
+
+
+def _address(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _strides(t):
+    return (ctypes.c_int64 * 3)(*t.stride()[:3])
+
+
+def _workspace(workspace, nbytes, like):
+    """The workspace tensor of a call: one of `nbytes` for "auto", or the caller's."""
+    import torch
+
+    if isinstance(workspace, str):
+        if workspace != "auto":
+            raise ValueError(f"workspace must be 'auto' or a tensor, not {workspace!r}")
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+    if workspace is not None and (workspace.device != like.device or not workspace.is_contiguous()):
+        raise ValueError(f"the workspace must be contiguous and on {like.device}")
+    return workspace
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def layernorm_workspace_size(rows, C, dtype) -> int:
+    """msda_layernorm_backward_workspace_size: bytes of device workspace for the sums over rows."""
+    out = ctypes.c_size_t(0)
+    _raise(lib().msda_layernorm_backward_workspace_size(rows, C, int(dtype), ctypes.byref(out)),
+           "msda_layernorm_backward_workspace_size")
+    return int(out.value)
+
+
+def _rows(x):
+    if x.dim() < 1:
+        raise ValueError("x must have a channel dimension")
+    C = x.shape[-1]
+    rows = 1
+    for n in x.shape[:-1]:
+        rows *= n
+    return rows, C
+
+
+def layernorm_forward(x, weight=None, bias=None, residual=None, eps=1e-5, want_sum: bool = False, out=None, mean=None,
+                      rstd=None, sum=None, stream=None):
+    """(out, mean, rstd) from msda_layernorm_forward: layer norm of x + residual over the last dimension; with
+    want_sum (or a `sum` tensor) also x + residual itself, as a fourth result. weight and bias are fp32."""
+    import torch
+
+    rows, C = _rows(x)
+    code = _layer_dtype(x)
+    _expect("x", x, x.shape, x.dtype, x)
+    for name, t in (("residual", residual), ("out", out), ("sum", sum)):
+        _expect(name, t, x.shape, x.dtype, x)
+    for name, t in (("weight", weight), ("bias", bias)):
+        _expect(name, t, (C,), torch.float32, x)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _expect(name, t, x.shape[:-1], torch.float32, x)
+    with _launching(x, stream) as s:
+        out = torch.empty_like(x) if out is None else out
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
+        sum = torch.empty_like(x) if sum is None and want_sum else sum
+        r = lib().msda_layernorm_forward(_address(x), _address(residual), _address(weight), _address(bias), _address(out),
+                                         _address(sum), _address(mean), _address(rstd), rows, C, float(eps), code, s)
+    _raise(r, "msda_layernorm_forward")
+    return (out, mean, rstd) if sum is None else (out, mean, rstd, sum)
+
+
+def layernorm_backward(x, grad_out, mean, rstd, weight=None, residual=None, grad_sum=None,
+                       want_weight_grads: bool = True, grad_x=None, grad_weight=None, grad_bias=None, workspace="auto",
+                       stream=None):
+    """(grad_x, grad_weight, grad_bias) from msda_layernorm_backward; grad_x is the gradient of x and of residual.
+    Without want_weight_grads the last two are None (or the tensors given). grad_sum: the gradient of the
+    forward's `sum`."""
+    import torch
+
+    rows, C = _rows(x)
+    code = _layer_dtype(x)
+    _expect("x", x, x.shape, x.dtype, x)
+    for name, t in (("residual", residual), ("grad_out", grad_out), ("grad_sum", grad_sum), ("grad_x", grad_x)):
+        _expect(name, t, x.shape, x.dtype, x)
+    for name, t in (("weight", weight), ("grad_weight", grad_weight), ("grad_bias", grad_bias)):
+        _expect(name, t, (C,), torch.float32, x)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _expect(name, t, x.shape[:-1], torch.float32, x)
+    with _launching(x, stream) as s:
+        grad_x = torch.empty_like(x) if grad_x is None else grad_x
+        if want_weight_grads:
+            grad_weight = torch.empty(C, dtype=torch.float32, device=x.device) if grad_weight is None else grad_weight
+            grad_bias = torch.empty(C, dtype=torch.float32, device=x.device) if grad_bias is None else grad_bias
+        wanted = grad_weight is not None or grad_bias is not None
+        ws = _workspace(workspace, layernorm_workspace_size(rows, C, code) if wanted else 0, x)
+        r = lib().msda_layernorm_backward(_address(x), _address(residual), _address(weight), _address(grad_out),
+                                          _address(grad_sum), _address(mean), _address(rstd), _address(grad_x),
+                                          _address(grad_weight), _address(grad_bias), _address(ws), _bytes(ws), rows, C,
+                                          code, s)
+    _raise(r, "msda_layernorm_backward")
+    return grad_x, grad_weight, grad_bias
+
+
+def _rotate(entry, in_name, x, pos, freqs, interleaved, out_name, out, stream):
+    import torch
+
+    if x.dim() != 4 or freqs.dim() != 2:
+        raise ValueError(f"{in_name} must be [N, T, M, D] and freqs [A, R], not {tuple(x.shape)} and {tuple(freqs.shape)}")
+    N, T, M, D = x.shape
+    A, R = freqs.shape
+    code = _layer_dtype(x)
+    shared = pos.dim() == 2
+    _expect(in_name, x, x.shape, x.dtype, x, strided=True)
+    _expect(out_name, out, x.shape, x.dtype, x, strided=True)
+    _expect("pos", pos, (T, A) if shared else (N, T, A), torch.float32, x)
+    _expect("freqs", freqs, (A, R), torch.float32, x)
+    with _launching(x, stream) as s:
+        out = torch.empty((N, T, M, D), dtype=x.dtype, device=x.device) if out is None else out
+        r = getattr(lib(), entry)(_address(x), _strides(x), _address(pos), _address(freqs), _address(out), _strides(out),
+                                  N, T, M, D, A, R, 1 if shared else N, int(bool(interleaved)), code, s)
+    _raise(r, entry)
+    return out
+
+
+def rotary_forward(x, pos, freqs, interleaved: bool = False, out=None, stream=None):
+    """x [N, T, M, D] with its channel pairs turned by the angles pos . freqs, from msda_rotary_forward. pos is
+    [N, T, A], or [T, A] for the same positions in every batch item; freqs is [A, R]. x may be a view whose channels
+    are contiguous (the queries and keys of a packed projection); out=x rotates in place."""
+    return _rotate("msda_rotary_forward", "x", x, pos, freqs, interleaved, "out", out, stream)
+
+
+def rotary_backward(grad_out, pos, freqs, interleaved: bool = False, grad_x=None, stream=None):
+    """The gradient of rotary_forward's x from msda_rotary_backward: grad_out turned back. grad_x=grad_out turns in
+    place."""
+    return _rotate("msda_rotary_backward", "grad_out", grad_out, pos, freqs, interleaved, "grad_x", grad_x, stream)
+
+
+def _attention(q, k, v, scale, softcap, slopes, q_pos, k_pos, q_doc, k_doc, prefix, causal):
+    """The call's msda_attention_t, after the checks of its tensors."""
+    import torch
+
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError(f"q must be [N, Lq, M, D] and k [N, Lk, Mkv, D], not {tuple(q.shape)} and {tuple(k.shape)}")
+    N, Lq, M, D = q.shape
+    _, Lk, Mkv, _ = k.shape
+    code = _layer_dtype(q)
+    _expect("q", q, q.shape, q.dtype, q, strided=True)
+    for name, t in (("k", k), ("v", v)):
+        _expect(name, t, (N, Lk, Mkv, D), q.dtype, q, strided=True)
+    _expect("slopes", slopes, (M,), torch.float32, q)
+    _expect("q_pos", q_pos, (N, Lq, 2), torch.float32, q)
+    _expect("k_pos", k_pos, (N, Lk, 2), torch.float32, q)
+    _expect("q_doc", q_doc, (N, Lq), torch.int32, q)
+    _expect("k_doc", k_doc, (N, Lk), torch.int32, q)
+    _expect("prefix", prefix, (N,), torch.int32, q)
+    if (q_doc is None) != (k_doc is None):
+        raise ValueError("q_doc and k_doc must be given both or neither")
+    if slopes is not None and (q_pos is None or k_pos is None):
+        raise ValueError("slopes need q_pos and k_pos")
+    return AttentionDescription(N, Lq, Lk, M, Mkv, D, code, int(bool(causal)),
+                                D ** -0.5 if scale is None else float(scale), float(softcap), _strides(q), _strides(k),
+                                _strides(v), *(_address(t) for t in (slopes, q_pos, k_pos, q_doc, k_doc, prefix)))
+
+
+def _attention_workspace(a, backward: bool) -> int:
+    out = ctypes.c_size_t(0)
+    _raise(lib().msda_attention_workspace_size(ctypes.byref(a), int(backward), ctypes.byref(out)),
+           "msda_attention_workspace_size")
+    return int(out.value)
+
+
+def attention_workspace_size(q, k, v, backward: bool = False, scale=None, softcap: float = 0.0, slopes=None, q_pos=None,
+                             k_pos=None, q_doc=None, k_doc=None, prefix=None, causal: bool = False) -> int:
+    """msda_attention_workspace_size of the call with these arguments."""
+    return _attention_workspace(_attention(q, k, v, scale, softcap, slopes, q_pos, k_pos, q_doc, k_doc, prefix, causal),
+                                backward)
+
+
+def attention_forward(q, k, v, scale=None, softcap: float = 0.0, slopes=None, q_pos=None, k_pos=None, q_doc=None,
+                      k_doc=None, prefix=None, causal: bool = False, want_lse: bool = True, out=None, lse=None,
+                      workspace="auto", stream=None):
+    """(out [N, Lq, M, D], lse [N, M, Lq] or None) from msda_attention_forward.
+
+    q [N, Lq, M, D], k and v [N, Lk, Mkv, D], M a multiple of Mkv; views whose channels are contiguous are
+    taken. scale: D ** -0.5 when None. softcap: cap of the scores (0: none). slopes [M], q_pos [N, Lq, 2] and
+    k_pos [N, Lk, 2] (fp32): a bias of -slope times the distance. q_doc [N, Lq] and k_doc [N, Lk] (int32): queries see
+    the keys of their own document, -1 is padding. prefix [N] (int32): the first keys, common to all documents
+    and exempt from the order. causal: the last query sees every key, each one before it one fewer.
+    workspace: "auto" allocates it, or a caller-owned uint8 tensor of attention_workspace_size bytes.
+    """
+    import torch
+
+    a = _attention(q, k, v, scale, softcap, slopes, q_pos, k_pos, q_doc, k_doc, prefix, causal)
+    _expect("out", out, q.shape, q.dtype, q)
+    _expect("lse", lse, (a.N, a.M, a.Lq), torch.float32, q)
+    with _launching(q, stream) as s:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        if lse is None and want_lse:
+            lse = torch.empty((a.N, a.M, a.Lq), dtype=torch.float32, device=q.device)
+        ws = _workspace(workspace, _attention_workspace(a, False), q)
+        r = lib().msda_attention_forward(ctypes.byref(a), _address(q), _address(k), _address(v), _address(out),
+                                         _address(lse), _address(ws), _bytes(ws), s)
+    _raise(r, "msda_attention_forward")
+    return out, lse
+
+
+def attention_backward(q, k, v, out, lse, grad_out, scale=None, softcap: float = 0.0, slopes=None, q_pos=None, k_pos=None,
+                       q_doc=None, k_doc=None, prefix=None, causal: bool = False, grad_q=None, grad_k=None, grad_v=None,
+                       workspace="auto", stream=None):
+    """(grad_q, grad_k, grad_v) from msda_attention_backward, with the forward's arguments and its out and lse."""
+    import torch
+
+    a = _attention(q, k, v, scale, softcap, slopes, q_pos, k_pos, q_doc, k_doc, prefix, causal)
+    for name, t in (("out", out), ("grad_out", grad_out), ("grad_q", grad_q)):
+        _expect(name, t, q.shape, q.dtype, q)
+    _expect("lse", lse, (a.N, a.M, a.Lq), torch.float32, q)
+    for name, t in (("grad_k", grad_k), ("grad_v", grad_v)):
+        _expect(name, t, k.shape, q.dtype, q)
+    with _launching(q, stream) as s:
+        grad_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if grad_q is None else grad_q
+        grad_k = torch.empty(k.shape, dtype=q.dtype, device=q.device) if grad_k is None else grad_k
+        grad_v = torch.empty(k.shape, dtype=q.dtype, device=q.device) if grad_v is None else grad_v
+        ws = _workspace(workspace, _attention_workspace(a, True), q)
+        r = lib().msda_attention_backward(ctypes.byref(a), _address(q), _address(k), _address(v), _address(out),
+                                          _address(lse), _address(grad_out), _address(grad_q), _address(grad_k),
+                                          _address(grad_v), _address(ws), _bytes(ws), s)
+    _raise(r, "msda_attention_backward")
+    return grad_q, grad_k, grad_v
