@@ -370,6 +370,7 @@ typedef struct {
     int64_t N, Lq, Lk, M, Mkv, D; /* M a multiple of Mkv; 1 <= D <= MSDA_ATTENTION_MAX_D              */
     int dtype;                    /* of q, k, v, out and the gradients                                */
     int causal;                   /* nonzero: the order rule above; needs Lk >= Lq                    */
+    int unaligned;                /* nonzero: q, k and v may start off 16-byte boundaries; see below  */
     float scale;                  /* finite, > 0                                                      */
     float softcap;                /* finite, >= 0; 0: scores are not capped                           */
     int64_t q_stride[3];          /* strides of q [N, Lq, M, D] in elements: batch item, token, head; */
@@ -393,9 +394,10 @@ msda_status_t msda_attention_workspace_size(const msda_attention_t* a, int backw
  * backward pass needs it). Few queries over many keys are split over the keys and joined, so a single
  * token against a long cache fills the GPU. workspace: DEVICE scratch of at least
  * msda_attention_workspace_size bytes, 16-byte aligned (may be NULL if that is 0), used by nothing
- * else until the enqueued work completes; a smaller one is MSDA_ERROR_INVALID_VALUE. Pointers need the
- * alignment of their elements; tensors whose base, strides and rows are multiples of 16 bytes are
- * read in 16-byte pieces. Out is 16-byte aligned. N * Lq == 0 is a no-op; Lk == 0 writes out = 0, lse = -inf.
+ * else until the enqueued work completes; a smaller one is MSDA_ERROR_INVALID_VALUE. Out is 16-byte
+ * aligned. q, k and v are read in 16-byte pieces: each needs 16-byte alignment, unless its strides or
+ * D channels are not multiples of 16 bytes or `unaligned` is set; it is copied into the workspace then.
+ * N * Lq == 0 is a no-op; Lk == 0 writes out = 0, lse = -inf.
  */
 msda_status_t msda_attention_forward(const msda_attention_t* a, const void* q, const void* k, const void* v,
                                      void* out, float* lse, void* workspace, size_t workspace_bytes,

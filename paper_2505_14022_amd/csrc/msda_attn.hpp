@@ -129,22 +129,6 @@ __device__ __forceinline__ typename Op<T>::Frag row_frag(const T* row, int c, in
     return *reinterpret_cast<const typename Op<T>::Frag*>(row + c * Op<T>::K + (lane >> 5) * (Op<T>::K / 2));
 }
 
-// 16 bytes of a row in global memory from channel d on; channels from D on are zero.
-template <typename T>
-__device__ __forceinline__ uint4 load_chunk(const T* row, int d, int D, bool vec) {
-    constexpr int n = 16 / sizeof(T);
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (vec) {
-        if (d < D) x = *reinterpret_cast<const uint4*>(row + d);
-    } else {
-        Piece<T, n> y;
-#pragma unroll
-        for (int i = 0; i < n; ++i) y.v[i] = d + i < D ? row[d + i] : (T)0.f;
-        x = __builtin_bit_cast(uint4, y);
-    }
-    return x;
-}
-
 // Whether 16 bytes hold an infinity or NaN.
 template <typename T>
 __device__ __forceinline__ bool not_finite(uint4 x) {
@@ -159,41 +143,97 @@ __device__ __forceinline__ bool not_finite(uint4 x) {
     return bad;
 }
 
-// Geometry of a tile in LDS: rows padded by 16 bytes, which spreads a column of 16-byte reads over the banks.
-template <typename T, int DP>
+// Geometry of the tiles that a workgroup of NW waves stages in LDS. Rows are padded by 16 bytes, which spreads
+// a column of 16-byte reads over the banks. A lone wave (few owners) takes half tiles: what it has in flight
+// stays in its registers.
+template <typename T, int DP, int NW>
 struct TileOf {
-    static constexpr int kRows = Op<T>::kTile;
+    static constexpr int kRows = NW == 1 ? 32 : Op<T>::kTile;
+    static constexpr int kBlocks = kRows / 32;
     static constexpr int kPer = 16 / sizeof(T);          // elements of a 16-byte chunk
     static constexpr int kChunks = DP / kPer;            // chunks of a row
     static constexpr int kStride = DP + kPer;
     static constexpr int kElems = kRows * kStride;
+    static constexpr int kLoads = kRows * kChunks / (64 * NW);  // chunks per thread
+    // row and first channel of the thread's a-th chunk
+    static __device__ __forceinline__ int row(int a) { return ((int)threadIdx.x + a * 64 * NW) / kChunks; }
+    static __device__ __forceinline__ int channel(int a) { return ((int)threadIdx.x + a * 64 * NW) % kChunks * kPer; }
+    static __device__ __forceinline__ void put(T* tile, int a, uint4 x) {
+        *reinterpret_cast<uint4*>(tile + row(a) * kStride + channel(a)) = x;
+    }
 };
 
-// acc (channels x owners) += sum over the 32 rows of a tile of weight * row, where a weight of zero takes
-// nothing from the row, whatever it holds: for tiles with infinities or NaN of which some pairs are masked.
-// `w` holds the owner's weights in the register order above.
-template <typename T, int DP>
-__device__ __forceinline__ void add_rows(acc_t (&acc)[DP / 32], const acc_t& w, const T* tile, int stride, int lane) {
-    const int h = lane >> 5;
+// Channels d .. of a row in global memory, zero from D on. Rows are whole 16-byte chunks.
+template <typename T>
+__device__ __forceinline__ uint4 load_chunk(const T* row, int d, int D) {
+    return d < D ? *reinterpret_cast<const uint4*>(row + d) : make_uint4(0, 0, 0, 0);
+}
+
+// What a masked pair holds must reach nothing, but in a matrix product zero times an infinity or a NaN is a NaN. In
+// calls with masks the tiles that are summed over are therefore staged with zeros in place of such values, and
+// what they make of an owner's channel that does see them is noted in LDS, two bits per channel: 1 infinity, 2 minus
+// infinity, both NaN; it is added to the result as it is written. (A rare path that holds no sums, so it costs
+// the others no registers.)
+template <int DP>
+struct Odd {
+    static constexpr int kWords = DP / 16;  // per owner
+    uint32_t* mine;                         // the lane's owner's
+    bool any = false;
+
+    __device__ __forceinline__ void start(uint32_t* words, int owner, int lane, bool masks) {
+        mine = words + owner * kWords;
+        if (masks)
+            for (int i = lane >> 5; i < kWords; i += 2) mine[i] = 0;
+    }
+    // `w`: the owner's weights of 32 rows in the register order above; row_at(r): row r's D channels in memory (asked
+    // for rows of nonzero weight only). Half wave h notes every other word.
+    template <typename T, typename F>
+    __device__ __forceinline__ void note(const acc_t& w, int D, int lane, F row_at) {
+        any = true;
 #pragma unroll 1
-    for (int r = 0; r < 16; ++r) {
-        float x = 0.f;
+        for (int r = 0; r < 16; ++r) {
+            float x = 0.f, half[2];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x = i == r ? w[i] : x;
-        float half[2];
-        both_halves(x, half[0], half[1]);
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-            const T* row = tile + (8 * (r >> 2) + 4 * hh + (r & 3)) * stride + 4 * h;
-#pragma unroll
-            for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float y = (float)row[t * 32 + 8 * (i >> 2) + (i & 3)];
-                    acc[t][i] += half[hh] == 0.f ? 0.f : half[hh] * y;
+            for (int i = 0; i < 16; ++i) x = i == r ? w[i] : x;
+            both_halves(x, half[0], half[1]);
+#pragma unroll 1
+            for (int hh = 0; hh < 2; ++hh) {
+                const float y = hh ? half[1] : half[0];
+                if (y == 0.f) continue;
+                const T* row = row_at(8 * (r >> 2) + 4 * hh + (r & 3));
+#pragma unroll 1
+                for (int k = lane >> 5; k < kWords; k += 2) {
+                    uint32_t bits = mine[k];
+#pragma unroll 1
+                    for (int c = 0; c < 16 && k * 16 + c < D; ++c) {
+                        const float v = (float)row[k * 16 + c];
+                        const uint32_t code = fabsf(v) < kInf ? 0u : v != v ? 3u : (v > 0.f) == (y > 0.f) ? 1u : 2u;
+                        bits |= code << (2 * c);
+                    }
+                    mine[k] = bits;
                 }
+            }
         }
     }
+    // Adds what was noted to channels d .. d + 3 of the owner's result.
+    __device__ __forceinline__ void apply(float (&x)[4], int d) const {
+        if (!any) return;
+        const uint32_t codes = mine[d >> 4] >> (2 * (d & 15));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t code = codes >> (2 * e) & 3u;
+            x[e] += code == 0u ? 0.f : code == 1u ? kInf : code == 2u ? -kInf : __builtin_nanf("");
+        }
+    }
+};
+
+// A chunk without its infinities and NaN.
+template <typename T>
+__device__ __forceinline__ uint4 finite_only(uint4 x) {
+    auto y = __builtin_bit_cast(Piece<T, 16 / sizeof(T)>, x);
+#pragma unroll
+    for (int i = 0; i < (int)(16 / sizeof(T)); ++i) y.v[i] = fabsf((float)y.v[i]) < kInf ? y.v[i] : (T)0.f;
+    return __builtin_bit_cast(uint4, y);
 }
 
 // acc += tile^T (32 rows from tile on) times the owner's weights.
@@ -211,10 +251,10 @@ __device__ __forceinline__ void add_product(acc_t (&acc)[DP / 32], const acc_t& 
     }
 }
 
-// 32 rows of a tile times the owner's fragments.
+// s + 32 rows of a tile times the owner's fragments.
 template <typename T, int DP>
-__device__ __forceinline__ acc_t row_product(const T* tile, int stride, const typename Op<T>::Frag* own, int lane) {
-    acc_t s = {};
+__device__ __forceinline__ acc_t row_product(const T* tile, int stride, const typename Op<T>::Frag* own, int lane,
+                                             acc_t s) {
 #pragma unroll
     for (int c = 0; c < DP / Op<T>::K; ++c) s = Op<T>::mma(row_frag(tile + (lane & 31) * stride, c, lane), own[c], s);
     return s;
@@ -277,6 +317,199 @@ struct TileWalk {
 // a slab read its keys through one L2.
 __device__ __forceinline__ int xcd_item(int b, int grid) { return (b & 7) * (grid >> 3) + (b >> 3); }
 int xcd_grid(int64_t items) { return (int)((items + 7) / 8 * 8); }
+
+// What a workgroup works on.
+struct Work {
+    int slab, block, split, n, kv, common, off;
+    bool any;
+    // last_first: blocks from the last to the first, so that causal rows with the most keys go first
+    __device__ __forceinline__ Work(const AttnParams& p, bool last_first) {
+        const int item = xcd_item(blockIdx.x, gridDim.x), per_slab = p.blocks * p.splits;
+        any = item < p.N * p.Mkv * per_slab;
+        slab = item / per_slab;
+        const int rest = item - slab * per_slab;
+        block = rest / p.splits;
+        split = rest - block * p.splits;
+        if (last_first) block = p.blocks - 1 - block;
+        n = slab / p.Mkv;
+        kv = slab - n * p.Mkv;
+        off = p.Lk - p.Lq;
+        common = any && p.prefix ? min(max(p.prefix[n], 0), p.Lk) : 0;
+    }
+};
+
+// The row that a lane owns, and what it sees: keys up to `last` of document `doc`, or below `common`.
+struct Row32 {
+    int row, i, head, doc, last;
+    int64_t at;    // its place in [N, Lq, M]
+    int64_t stat;  // its place in [N, M, Lq]
+    float slope;
+    float2 pos;
+    // over the workgroup's rows: the last query and the documents; over the wave's: the first one's last key
+    int i_last, last0, doc0;
+    Range docs;
+    bool one_doc, no_pad;
+
+    template <int NW>
+    static __device__ __forceinline__ Row32 of(const AttnParams& p, const Work& w, int wave, int lane, bool biased) {
+        Row32 x;
+        const int first = w.block * 32 * NW;
+        x.row = first + wave * 32 + (lane & 31);
+        const int row = min(x.row, p.R - 1);
+        x.i = row / p.G;
+        x.head = w.kv * p.G + row - x.i * p.G;
+        x.at = ((int64_t)w.n * p.Lq + x.i) * p.M + x.head;
+        x.stat = ((int64_t)w.n * p.M + x.head) * p.Lq + x.i;
+        x.doc = p.q_doc ? p.q_doc[(int64_t)w.n * p.Lq + x.i] : 0;
+        x.last = x.doc < 0 ? -1 : p.causal ? max(x.i + w.off, w.common - 1) : p.Lk - 1;
+        x.slope = 0.f;
+        x.pos = make_float2(0.f, 0.f);
+        if (biased && p.slopes) {
+            x.slope = p.slopes[x.head] * kLog2e;
+            x.pos = reinterpret_cast<const float2*>(p.q_pos)[(int64_t)w.n * p.Lq + x.i];
+        }
+        x.i_last = (min(first + 32 * NW, p.R) - 1) / p.G;
+        x.docs = {0, 0, 1};
+        if (p.q_doc) x.docs = wave_range(p.q_doc + (int64_t)w.n * p.Lq, first / p.G, x.i_last, lane);
+        x.doc0 = __builtin_amdgcn_readfirstlane(x.doc);
+        x.one_doc = __all((x.doc == x.doc0) & (x.doc >= 0));
+        x.no_pad = __all(x.doc >= 0);
+        x.last0 = p.causal ? __builtin_amdgcn_readfirstlane(x.last) : p.Lk - 1;  // rows go up with their lanes
+        return x;
+    }
+};
+
+// Keys and values staged tile by tile, for kernels that own rows: two buffers in LDS, and the next tile in
+// registers while the waves work on the current one.
+// SUM_VALUES: the kernel sums over the values (forward), else over the keys (grad_q).
+template <typename T, int DP, int NW, bool BIASED, bool SUM_VALUES>
+struct KeyTiles {
+    using Tile = TileOf<T, DP, NW>;
+    struct Shared {
+        T k[2][Tile::kElems], v[2][Tile::kElems];
+        int doc[2][Tile::kRows];
+        float2 pos[2][BIASED ? Tile::kRows : 1];
+        int odd[2][NW];  // per wave: some of what it staged was not finite
+    };
+    Shared& sh;
+    const AttnParams& p;
+    const Work& w;
+    const Row32& own;
+    const int4* ranges;
+    const T *k, *v;
+    TileWalk walk;
+    int t, lane;
+    bool masks;
+    Range kr;
+    uint4 kx[Tile::kLoads], vx[Tile::kLoads];
+    int doc_x;
+    float2 pos_x;
+
+    __device__ __forceinline__ KeyTiles(Shared& s, const AttnParams& q, const Work& work, const Row32& row, int l)
+        : sh(s), p(q), w(work), own(row), lane(l) {
+        ranges = p.k_ranges + (int64_t)w.n * p.k_tiles;
+        k = static_cast<const T*>(p.k) + w.n * p.ks[0] + w.kv * p.ks[2];
+        v = static_cast<const T*>(p.v) + w.n * p.vs[0] + w.kv * p.vs[2];
+        walk.at = (int)((int64_t)p.k_tiles * w.split / p.splits);
+        walk.end = (int)((int64_t)p.k_tiles * (w.split + 1) / p.splits);
+        masks = p.q_doc || p.causal;
+        kr = {0, 0, 1};
+        doc_x = 0;
+        pos_x = make_float2(0.f, 0.f);
+    }
+    // Finds the next tile that the workgroup's rows see, and loads it.
+    __device__ __forceinline__ void fetch() {
+        t = walk.next(lane, [&](int u) {
+            const bool first = u * Tile::kRows < w.common;
+            if (p.causal && u * Tile::kRows > own.i_last + w.off && !first) return false;
+            return !p.q_doc || meet(own.docs, range_of(ranges[u]), first);
+        });
+        if (t < 0) return;
+        const int j0 = t * Tile::kRows;
+        const T* kt = k + j0 * p.ks[1];
+        const T* vt = v + j0 * p.vs[1];
+        if (p.q_doc) kr = range_of(ranges[t]);
+        const int* docs = p.k_doc + (int64_t)w.n * p.Lk + j0;
+#pragma unroll
+        for (int a = 0; a < Tile::kLoads; ++a) {
+            const int r = Tile::row(a), d = Tile::channel(a);
+            kx[a] = vx[a] = make_uint4(0, 0, 0, 0);
+            // padding is not read: what it holds must reach nothing
+            if (j0 + r < p.Lk && (kr.whole || docs[r] >= 0)) {
+                kx[a] = load_chunk(kt + r * p.ks[1], d, p.D);
+                vx[a] = load_chunk(vt + r * p.vs[1], d, p.D);
+            }
+        }
+        if ((int)threadIdx.x < Tile::kRows) {
+            const int r = threadIdx.x;
+            doc_x = j0 + r >= p.Lk ? -1 : p.k_doc ? docs[r] : 0;
+            if (BIASED && p.slopes && j0 + r < p.Lk)
+                pos_x = reinterpret_cast<const float2*>(p.k_pos)[(int64_t)w.n * p.Lk + j0 + r];
+        }
+    }
+    __device__ __forceinline__ void stage(int b) {
+        if (masks) {
+            bool odd = false;
+#pragma unroll
+            for (int a = 0; a < Tile::kLoads; ++a) odd |= not_finite<T>(SUM_VALUES ? vx[a] : kx[a]);
+            const bool some = __any(odd);
+            if (some) {
+#pragma unroll
+                for (int a = 0; a < Tile::kLoads; ++a) {
+                    uint4& x = SUM_VALUES ? vx[a] : kx[a];
+                    x = finite_only<T>(x);
+                }
+            }
+            if (lane == 0) sh.odd[b][threadIdx.x >> 6] = some;
+        }
+#pragma unroll
+        for (int a = 0; a < Tile::kLoads; ++a) {
+            Tile::put(sh.k[b], a, kx[a]);
+            Tile::put(sh.v[b], a, vx[a]);
+        }
+        if ((int)threadIdx.x < Tile::kRows) {
+            sh.doc[b][threadIdx.x] = doc_x;
+            if (BIASED) sh.pos[b][threadIdx.x] = pos_x;
+        }
+    }
+    // Notes what the weights of the block of 32 keys from key j0 on meet that was not finite in buffer b.
+    __device__ __forceinline__ void note_odd(Odd<DP>& odd, const acc_t& weight, int b, int j0) const {
+        if (!masks) return;
+        int some = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) some |= sh.odd[b][i];
+        if (some)
+            odd.template note<T>(weight, p.D, lane, [&](int r) {
+                return SUM_VALUES ? v + (j0 + r) * p.vs[1] : k + (j0 + r) * p.ks[1];
+            });
+    }
+    // Whether all rows of the wave see all keys of the tile just loaded.
+    __device__ __forceinline__ bool whole() const {
+        const int j1 = t * Tile::kRows + Tile::kRows - 1;
+        bool x = j1 <= own.last0 && j1 < p.Lk;
+        if (p.q_doc)
+            x = x && kr.whole && ((own.one_doc && kr.lo == own.doc0 && kr.hi == own.doc0) || (own.no_pad && j1 < w.common));
+        return x;
+    }
+};
+
+// The row of the register r of a 32 x 32 block.
+__device__ __forceinline__ int block_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+// Raw scores of a block turned into scores in units of log 2 once multiplied by the result. With a cap,
+// slack[r] gets the cap's derivative 1 - tanh^2 if `slack` is given.
+template <typename T>
+__device__ __forceinline__ float cap_scores(const AttnParams& p, acc_t& s, acc_t* slack) {
+    if (!(p.softcap > 0.f)) return p.scale * kLog2e;
+    const float a = p.scale / p.softcap, cap = p.softcap * kLog2e;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const float t = tanh_of<std::is_same_v<T, float>>(s[r] * a);
+        if (slack) (*slack)[r] *= 1.f - t * t;
+        s[r] = cap * t;
+    }
+    return 1.f;
+}
 
 // Stores four consecutive channels of a result row.
 template <typename T>

@@ -68,23 +68,34 @@ struct AttnParams {
     int64_t qs[3], ks[3], vs[3];  // strides in elements: batch item, token, head
     int N, Lq, Lk, M, Mkv, G, D;
     int R;                        // rows of a slab: Lq * G
+    int row_width;                // elements from one row of o and grad_out to the next (D, or more where they were packed)
     int k_tiles, row_tiles, blocks, splits;
     int causal;
     float scale, softcap;
-    bool q_vec, k_vec, v_vec, out_vec;  // read (or written) in 16-byte pieces
 };
 
-// How a call is cut up: waves per workgroup, workgroups per slab, splits of the other axis. Workgroups own
-// rows (forward, grad_q) or keys (grad_k and grad_v).
-struct AttnPlan {
-    int waves, blocks, splits;
+// A copy of a strided tensor in rows of `width` elements, whole 16-byte pieces.
+struct AttnPack {
+    const void* from;
+    void* to;
+    int64_t stride[3];
+    int64_t L;
+    int N, H, D, width;
 };
-AttnPlan attn_plan(const AttnParams& p, int dtype, bool own_keys);
-int attn_tile(int dtype);                            // keys or rows per tile in LDS
-int attn_channels(int D);                            // channels that the kernels hold: 32, 64 or 128
-hipError_t launch_attn_ranges(const AttnParams& p, int dtype, bool rows, hipStream_t stream);
+
+// How a call is cut up: waves per workgroup, rows or keys per tile of the other axis, workgroups per slab and
+// splits of the other axis. Workgroups own rows (forward, grad_q) or keys (grad_k and grad_v).
+struct AttnPlan {
+    int waves, tile, blocks, splits;
+};
+// lone_waves: few owners may go to workgroups of one wave (the forward).
+AttnPlan attn_plan(int64_t slabs, int64_t own, int64_t across, int dtype, bool lone_waves);
+int attn_channels(int D);  // channels that the kernels hold: 32, 64 or 128
+hipError_t launch_attn_pack(const AttnPack& c, int dtype, hipStream_t stream);
+// The documents of tiles of k_tile keys, and of row_tile rows unless that is 0.
+hipError_t launch_attn_ranges(const AttnParams& p, int k_tile, int row_tile, hipStream_t stream);
 hipError_t launch_attn_forward(const AttnParams& p, int dtype, int waves, hipStream_t stream);
-hipError_t launch_attn_grad_q(const AttnParams& p, int dtype, int waves, hipStream_t stream);
-hipError_t launch_attn_grad_kv(const AttnParams& p, int dtype, int waves, hipStream_t stream);
+hipError_t launch_attn_grad_q(const AttnParams& p, int dtype, hipStream_t stream);
+hipError_t launch_attn_grad_kv(const AttnParams& p, int dtype, hipStream_t stream);
 
 }  // namespace msda

@@ -264,16 +264,20 @@ msda_status_t check_attention(const msda_attention_t* a) {
     return MSDA_SUCCESS;
 }
 
-// The kernels' view of a call. The workspace's pieces in order: documents of the key tiles and row tiles,
-// delta (backward), partial results of the splits.
+// The kernels' view of a call, and how it is cut up. The workspace's pieces in order: documents of the key tiles
+// and row tiles, delta (backward), packed copies of q, k, v, out and grad_out, partial results of the splits.
 struct Attention {
     msda::AttnParams p = {};
-    msda::AttnPlan rows = {1, 0, 1}, keys = {1, 0, 1};
-    size_t at_row_ranges = 0, at_delta = 0, at_part = 0, bytes = 0;
+    msda::AttnPlan rows = {1, 32, 0, 1}, keys = {1, 32, 0, 1};
+    size_t at_row_ranges = 0, at_delta = 0, at_pack[5] = {0, 0, 0, 0, 0}, at_part = 0, bytes = 0;
+    bool pack[5] = {false, false, false, false, false};
+    int width = 0;  // of a packed row
 };
 
-bool row_pieces(const void* base, const int64_t* stride, const int64_t* extent, int64_t D, int es) {
-    bool yes = is_aligned(base, 16) && (D * es) % 16 == 0;
+// Whether rows of D channels with these strides are whole 16-byte pieces on 16-byte boundaries of their base.
+bool row_pieces(const int64_t* stride, int64_t N, int64_t L, int64_t H, int64_t D, int es) {
+    const int64_t extent[3] = {N, L, H};
+    bool yes = (D * es) % 16 == 0;
     for (int i = 0; i < 3; ++i) yes = yes && (extent[i] <= 1 || (stride[i] * es) % 16 == 0);
     return yes;
 }
@@ -281,7 +285,8 @@ bool row_pieces(const void* base, const int64_t* stride, const int64_t* extent, 
 Attention attention_of(const msda_attention_t& a, bool backward) {
     Attention x;
     msda::AttnParams& p = x.p;
-    const int64_t G = a.M / a.Mkv, tile = msda::attn_tile(a.dtype), DP = msda::attn_channels((int)a.D);
+    const int es = dtype_size(a.dtype);
+    const int64_t G = a.M / a.Mkv, DP = msda::attn_channels((int)a.D), slabs = a.N * a.Mkv;
     p.N = (int)a.N;
     p.Lq = (int)a.Lq;
     p.Lk = (int)a.Lk;
@@ -290,8 +295,6 @@ Attention attention_of(const msda_attention_t& a, bool backward) {
     p.G = (int)G;
     p.D = (int)a.D;
     p.R = (int)(a.Lq * G);
-    p.k_tiles = (int)ceil_div(a.Lk, tile);
-    p.row_tiles = (int)ceil_div(p.R, tile);
     p.causal = a.causal != 0;
     p.scale = a.scale;
     p.softcap = a.softcap;
@@ -308,20 +311,33 @@ Attention attention_of(const msda_attention_t& a, bool backward) {
         p.k_doc = a.k_doc;
         p.prefix = a.prefix;
     }
-    const size_t slabs = (size_t)(a.N * a.Mkv);
-    if (a.Lq > 0) x.rows = msda::attn_plan(p, a.dtype, false);
-    if (backward && a.Lk > 0) x.keys = msda::attn_plan(p, a.dtype, true);
+    if (a.Lq > 0) x.rows = msda::attn_plan(slabs, p.R, p.Lk, a.dtype, !backward);
+    if (backward && a.Lk > 0) x.keys = msda::attn_plan(slabs, p.Lk, p.R, a.dtype, false);
+    p.k_tiles = (int)ceil_div(a.Lk, x.rows.tile);
+    p.row_tiles = (int)ceil_div(p.R, x.keys.tile);
     const bool docs = p.q_doc != nullptr;
-    x.at_row_ranges = docs ? round_up(sizeof(int4) * a.N * p.k_tiles) : 0;
-    x.at_delta = x.at_row_ranges + (docs && backward ? round_up(sizeof(int4) * a.N * p.row_tiles) : 0);
-    x.at_part = x.at_delta + (backward ? round_up(sizeof(float) * a.N * a.M * a.Lq) : 0);
+    size_t at = docs ? round_up(sizeof(int4) * a.N * p.k_tiles) : 0;
+    x.at_row_ranges = at;
+    if (docs && backward) at += round_up(sizeof(int4) * a.N * p.row_tiles);
+    x.at_delta = at;
+    if (backward) at += round_up(sizeof(float) * a.N * a.M * a.Lq);
+    x.width = (int)ceil_div(a.D * es, 16) * 16 / es;
+    x.pack[0] = a.unaligned || !row_pieces(a.q_stride, a.N, a.Lq, a.M, a.D, es);
+    x.pack[1] = a.unaligned || !row_pieces(a.k_stride, a.N, a.Lk, a.Mkv, a.D, es);
+    x.pack[2] = a.unaligned || !row_pieces(a.v_stride, a.N, a.Lk, a.Mkv, a.D, es);
+    x.pack[3] = x.pack[4] = backward && (a.D * es) % 16 != 0;
+    for (int i = 0; i < 5; ++i) {
+        x.at_pack[i] = at;
+        if (x.pack[i]) at += round_up((size_t)es * a.N * (i == 1 || i == 2 ? a.Lk * a.Mkv : a.Lq * a.M) * x.width);
+    }
+    x.at_part = at;
     size_t part = 0;
-    if (x.rows.splits > 1) part = slabs * p.R * x.rows.splits * (DP + (backward ? 0 : 2));
+    if (x.rows.splits > 1) part = (size_t)slabs * p.R * x.rows.splits * (DP + (backward ? 0 : 2));
     if (x.keys.splits > 1) {
-        const size_t b = slabs * p.Lk * x.keys.splits * 2 * DP;
+        const size_t b = (size_t)slabs * p.Lk * x.keys.splits * 2 * DP;
         if (b > part) part = b;
     }
-    x.bytes = x.at_part + part * sizeof(float);
+    x.bytes = at + part * sizeof(float);
     return x;
 }
 
@@ -334,22 +350,56 @@ msda_status_t check_workspace(const Attention& x, const void* workspace, size_t 
     return MSDA_SUCCESS;
 }
 
-void bind(Attention& x, const msda_attention_t& a, const void* q, const void* k, const void* v, void* workspace) {
-    msda::AttnParams& p = x.p;
+msda_status_t check_bases(const msda_attention_t& a, const Attention& x, const void* q, const void* k, const void* v) {
     const int es = dtype_size(a.dtype);
-    const int64_t qe[3] = {a.N, a.Lq, a.M}, ke[3] = {a.N, a.Lk, a.Mkv};
-    p.q = q;
-    p.k = k;
-    p.v = v;
-    p.q_vec = row_pieces(q, p.qs, qe, a.D, es);
-    p.k_vec = row_pieces(k, p.ks, ke, a.D, es);
-    p.v_vec = row_pieces(v, p.vs, ke, a.D, es);
-    p.out_vec = (a.D * es) % 16 == 0;
+    if (!is_aligned(q, x.pack[0] ? es : 16) || !is_aligned(k, x.pack[1] ? es : 16) || !is_aligned(v, x.pack[2] ? es : 16))
+        return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: q, k and v need 16 bytes (their element's where "
+                    "they are packed: see msda_attention_t's unaligned)");
+    return MSDA_SUCCESS;
+}
+
+// Points the kernels at their tensors, and enqueues the copies of those that have to be packed. out and grad_out
+// are null in the forward.
+hipError_t bind(Attention& x, const msda_attention_t& a, const void* q, const void* k, const void* v, const void* out,
+                const void* grad_out, void* workspace, hipStream_t stream) {
+    msda::AttnParams& p = x.p;
     char* ws = static_cast<char*>(workspace);
     p.k_ranges = reinterpret_cast<int4*>(ws);
     p.row_ranges = reinterpret_cast<int4*>(ws + x.at_row_ranges);
     p.delta = reinterpret_cast<float*>(ws + x.at_delta);
     p.part = reinterpret_cast<float*>(ws + x.at_part);
+    p.row_width = x.pack[3] ? x.width : p.D;
+    int64_t rows[3] = {a.Lq * a.M * a.D, a.M * a.D, a.D};  // of out and grad_out
+    const void* from[5] = {q, k, v, out, grad_out};
+    int64_t* stride[5] = {p.qs, p.ks, p.vs, rows, rows};
+    for (int i = 0; i < 5; ++i) {
+        if (!x.pack[i]) continue;
+        const bool of_keys = i == 1 || i == 2;
+        msda::AttnPack c = {};
+        c.L = of_keys ? a.Lk : a.Lq;
+        c.H = (int)(of_keys ? a.Mkv : a.M);
+        if (c.L == 0) continue;
+        c.from = from[i];
+        c.to = ws + x.at_pack[i];
+        c.N = p.N;
+        c.D = p.D;
+        c.width = x.width;
+        for (int e = 0; e < 3; ++e) c.stride[e] = stride[i][e];
+        hipError_t e = msda::launch_attn_pack(c, a.dtype, stream);
+        if (e != hipSuccess) return e;
+        from[i] = c.to;
+        if (i < 3) {
+            stride[i][0] = c.L * c.H * c.width;
+            stride[i][1] = (int64_t)c.H * c.width;
+            stride[i][2] = c.width;
+        }
+    }
+    p.q = from[0];
+    p.k = from[1];
+    p.v = from[2];
+    p.o = from[3];
+    p.grad_out = from[4];
+    return hipSuccess;
 }
 
 void take_plan(msda::AttnParams& p, const msda::AttnPlan& plan) {
@@ -375,20 +425,18 @@ msda_status_t msda_attention_forward(const msda_attention_t* a, const void* q, c
     msda_status_t st = check_attention(a);
     if (st != MSDA_SUCCESS) return st;
     if (a->N * a->Lq == 0) return ok();
-    const int es = dtype_size(a->dtype);
     if (!q || !out || (a->Lk > 0 && (!k || !v)))
         return fail(MSDA_ERROR_INVALID_VALUE, "q, k, v and out must be non-null");
-    if (!is_aligned(q, es) || !is_aligned(k, es) || !is_aligned(v, es) || !is_aligned(out, 16) || !is_aligned(lse, 4))
-        return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: out needs 16 bytes, lse 4, q, k and v their element's");
+    if (!is_aligned(out, 16) || !is_aligned(lse, 4))
+        return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: out needs 16 bytes, lse 4");
     Attention x = attention_of(*a, false);
-    st = check_workspace(x, workspace, workspace_bytes);
-    if (st != MSDA_SUCCESS) return st;
-    bind(x, *a, q, k, v, workspace);
+    if ((st = check_bases(*a, x, q, k, v)) != MSDA_SUCCESS) return st;
+    if ((st = check_workspace(x, workspace, workspace_bytes)) != MSDA_SUCCESS) return st;
+    hipError_t e = bind(x, *a, q, k, v, nullptr, nullptr, workspace, (hipStream_t)stream);
     x.p.out = out;
     x.p.lse = lse;
     take_plan(x.p, x.rows);
-    hipError_t e = hipSuccess;
-    if (x.p.q_doc) e = msda::launch_attn_ranges(x.p, a->dtype, false, (hipStream_t)stream);
+    if (e == hipSuccess && x.p.q_doc) e = msda::launch_attn_ranges(x.p, x.rows.tile, 0, (hipStream_t)stream);
     if (e == hipSuccess) e = msda::launch_attn_forward(x.p, a->dtype, x.rows.waves, (hipStream_t)stream);
     if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "attention launch: %s", hipGetErrorString(e));
     return ok();
@@ -401,33 +449,29 @@ msda_status_t msda_attention_backward(const msda_attention_t* a, const void* q, 
     msda_status_t st = check_attention(a);
     if (st != MSDA_SUCCESS) return st;
     if (a->N == 0 || (a->Lq == 0 && a->Lk == 0)) return ok();
-    const int es = dtype_size(a->dtype);
     if ((a->Lq > 0 && (!q || !out || !lse || !grad_out || !grad_q)) || (a->Lk > 0 && (!k || !v || !grad_k || !grad_v)))
         return fail(MSDA_ERROR_INVALID_VALUE,
                     "q, k, v, out, lse, grad_out, grad_q, grad_k and grad_v must be non-null");
-    if (!is_aligned(q, es) || !is_aligned(k, es) || !is_aligned(v, es) || !is_aligned(lse, 4) || !is_aligned(out, 16) ||
-        !is_aligned(grad_out, 16) || !is_aligned(grad_q, 16) || !is_aligned(grad_k, 16) || !is_aligned(grad_v, 16))
-        return fail(MSDA_ERROR_INVALID_VALUE,
-                    "misaligned pointer: out and the gradients need 16 bytes, lse 4, q, k and v their element's");
+    if (!is_aligned(lse, 4) || !is_aligned(out, 16) || !is_aligned(grad_out, 16) || !is_aligned(grad_q, 16) ||
+        !is_aligned(grad_k, 16) || !is_aligned(grad_v, 16))
+        return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: out and the gradients need 16 bytes, lse 4");
     Attention x = attention_of(*a, true);
-    st = check_workspace(x, workspace, workspace_bytes);
-    if (st != MSDA_SUCCESS) return st;
-    bind(x, *a, q, k, v, workspace);
-    x.p.o = out;
+    if ((st = check_bases(*a, x, q, k, v)) != MSDA_SUCCESS) return st;
+    if ((st = check_workspace(x, workspace, workspace_bytes)) != MSDA_SUCCESS) return st;
+    hipError_t e = bind(x, *a, q, k, v, out, grad_out, workspace, (hipStream_t)stream);
     x.p.lse = const_cast<float*>(lse);
-    x.p.grad_out = grad_out;
     x.p.grad_q = grad_q;
     x.p.grad_k = grad_k;
     x.p.grad_v = grad_v;
-    hipError_t e = hipSuccess;
-    if (x.p.q_doc) e = msda::launch_attn_ranges(x.p, a->dtype, true, (hipStream_t)stream);
+    if (e == hipSuccess && x.p.q_doc)
+        e = msda::launch_attn_ranges(x.p, x.rows.tile, x.keys.tile, (hipStream_t)stream);
     if (e == hipSuccess && a->Lq > 0) {  // writes delta, which grad_k and grad_v need
         take_plan(x.p, x.rows);
-        e = msda::launch_attn_grad_q(x.p, a->dtype, x.rows.waves, (hipStream_t)stream);
+        e = msda::launch_attn_grad_q(x.p, a->dtype, (hipStream_t)stream);
     }
     if (e == hipSuccess && a->Lk > 0) {
         take_plan(x.p, x.keys);
-        e = msda::launch_attn_grad_kv(x.p, a->dtype, x.keys.waves, (hipStream_t)stream);
+        e = msda::launch_attn_grad_kv(x.p, a->dtype, (hipStream_t)stream);
     }
     if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "attention backward launch: %s", hipGetErrorString(e));
     return ok();

@@ -51,7 +51,7 @@ class MsdaError(RuntimeError):
 class AttentionDescription(ctypes.Structure):
     """msda_attention_t."""
     _fields_ = [(name, ctypes.c_int64) for name in ("N", "Lq", "Lk", "M", "Mkv", "D")] + \
-        [("dtype", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + \
+        [("dtype", ctypes.c_int), ("causal", ctypes.c_int), ("unaligned", ctypes.c_int), ("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + \
         [(name, ctypes.c_int64 * 3) for name in ("q_stride", "k_stride", "v_stride")] + \
         [(name, ctypes.c_void_p) for name in ("slopes", "q_pos", "k_pos", "q_doc", "k_doc", "prefix")]
 
@@ -647,7 +647,8 @@ def _attention(q, k, v, scale, softcap, slopes, q_pos, k_pos, q_doc, k_doc, pref
         raise ValueError("q_doc and k_doc must be given both or neither")
     if slopes is not None and (q_pos is None or k_pos is None):
         raise ValueError("slopes need q_pos and k_pos")
-    return AttentionDescription(N, Lq, Lk, M, Mkv, D, code, int(bool(causal)),
+    unaligned = int(any(t.data_ptr() % 16 for t in (q, k, v)))
+    return AttentionDescription(N, Lq, Lk, M, Mkv, D, code, int(bool(causal)), unaligned,
                                 D ** -0.5 if scale is None else float(scale), float(softcap), _strides(q), _strides(k),
                                 _strides(v), *(_address(t) for t in (slopes, q_pos, k_pos, q_doc, k_doc, prefix)))
 

@@ -95,11 +95,11 @@ def test_rotary_empty_is_a_no_op(L):
 
 
 def description(**kw):
-    d = dict(N=2, Lq=70, Lk=90, M=4, Mkv=2, D=32, dtype=2, causal=0, scale=0.1, softcap=0.0)
+    d = dict(N=2, Lq=70, Lk=90, M=4, Mkv=2, D=32, dtype=2, causal=0, unaligned=0, scale=0.1, softcap=0.0)
     tables = {k: kw.pop(k, None) for k in ("slopes", "q_pos", "k_pos", "q_doc", "k_doc", "prefix")}
     d.update(kw)
     arr = ctypes.c_int64 * 3
-    return msda.AttentionDescription(*(d[k] for k in ("N", "Lq", "Lk", "M", "Mkv", "D", "dtype", "causal", "scale", "softcap")),
+    return msda.AttentionDescription(*(d[k] for k in ("N", "Lq", "Lk", "M", "Mkv", "D", "dtype", "causal", "unaligned", "scale", "softcap")),
                                      arr(d["Lq"] * d["M"] * d["D"], d["M"] * d["D"], d["D"]),
                                      *(arr(d["Lk"] * d["Mkv"] * d["D"], d["Mkv"] * d["D"], d["D"]) for _ in range(2)),
                                      *tables.values())
@@ -141,9 +141,12 @@ def test_attention_refuses_bad_pointers_and_workspaces(L, no_gpu):
         assert L.msda_attention_workspace_size(ctypes.byref(a), b, ctypes.byref(size)) == OK
         need.append(size.value)
     assert 0 < need[0] < need[1]
-    for kw in (dict(q=None), dict(k=None), dict(out=None), dict(q=0x1001), dict(out=0x4008), dict(lse=0x5002),
+    for kw in (dict(q=None), dict(k=None), dict(out=None), dict(q=0x1008), dict(v=0x3002), dict(out=0x4008), dict(lse=0x5002),
                dict(ws=None, nbytes=0), dict(nbytes=need[0] - 1), dict(ws=0x10008)):
         assert forward(L, a, **kw) == INVALID, kw
+    loose = description(unaligned=1)  # may start anywhere but off its elements
+    assert forward(L, loose, q=0x1001) == INVALID and "misaligned" in msda.last_error()
+    assert forward(L, loose, q=0x1002, nbytes=0) == INVALID and "workspace" in msda.last_error()
     for kw in (dict(lse=None), dict(go=None), dict(gq=None), dict(gk=None), dict(gv=None), dict(go=0x6008), dict(gv=0x9002),
                dict(ws=None, nbytes=0), dict(nbytes=need[1] - 1)):
         assert backward(L, a, **kw) == INVALID, kw
