@@ -129,18 +129,14 @@ __device__ __forceinline__ typename Op<T>::Frag row_frag(const T* row, int c, in
     return *reinterpret_cast<const typename Op<T>::Frag*>(row + c * Op<T>::K + (lane >> 5) * (Op<T>::K / 2));
 }
 
-// Whether 16 bytes hold an infinity or NaN.
+// Whether 16 bytes hold an infinity or NaN: an exponent of all ones carries into the sign's place when one is
+// added to it, and no other does.
 template <typename T>
 __device__ __forceinline__ bool not_finite(uint4 x) {
-    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
-    constexpr uint32_t e = std::is_same_v<T, float> ? 0x7f800000u : std::is_same_v<T, bf16_t> ? 0x7f80u : 0x7c00u;
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        bad |= (u[i] & e) == e;
-        if constexpr (sizeof(T) == 2) bad |= (u[i] & (e << 16)) == (e << 16);
-    }
-    return bad;
+    constexpr uint32_t e = std::is_same_v<T, float> ? 0x7f800000u : std::is_same_v<T, bf16_t> ? 0x7f807f80u : 0x7c007c00u;
+    constexpr uint32_t one = std::is_same_v<T, float> ? 0x00800000u : std::is_same_v<T, bf16_t> ? 0x00800080u : 0x04000400u;
+    constexpr uint32_t sign = std::is_same_v<T, float> ? 0x80000000u : 0x80008000u;
+    return (((x.x & e) + one) | ((x.y & e) + one) | ((x.z & e) + one) | ((x.w & e) + one)) & sign;
 }
 
 // Geometry of the tiles that a workgroup of NW waves stages in LDS. Rows are padded by 16 bytes, which spreads
@@ -155,13 +151,19 @@ struct TileOf {
     static constexpr int kStride = DP + kPer;
     static constexpr int kElems = kRows * kStride;
     static constexpr int kLoads = kRows * kChunks / (64 * NW);  // chunks per thread
-    // row and first channel of the thread's a-th chunk
-    static __device__ __forceinline__ int row(int a) { return ((int)threadIdx.x + a * 64 * NW) / kChunks; }
-    static __device__ __forceinline__ int channel(int a) { return ((int)threadIdx.x + a * 64 * NW) % kChunks * kPer; }
+    static constexpr int kStep = 64 * NW / kChunks;             // rows between two chunks of a thread
+    // row of the thread's a-th chunk, and the first channel of all of them
+    static __device__ __forceinline__ int row(int a) { return (int)threadIdx.x / kChunks + a * kStep; }
+    static __device__ __forceinline__ int channel() { return (int)threadIdx.x % kChunks * kPer; }
     static __device__ __forceinline__ void put(T* tile, int a, uint4 x) {
-        *reinterpret_cast<uint4*>(tile + row(a) * kStride + channel(a)) = x;
+        *reinterpret_cast<uint4*>(tile + row(a) * kStride + channel()) = x;
     }
 };
+
+// 16 bytes at a byte offset below 2^31 from a base that is the same in all lanes.
+__device__ __forceinline__ uint4 load_at(const void* base, int offset) {
+    return *reinterpret_cast<const uint4*>(static_cast<const char*>(base) + (uint32_t)offset);
+}
 
 // Channels d .. of a row in global memory, zero from D on. Rows are whole 16-byte chunks.
 template <typename T>
@@ -267,9 +269,8 @@ __device__ __forceinline__ acc_t row_product(const T* tile, int stride, const ty
 struct Range {
     int lo, hi, whole;
 };
-__device__ __forceinline__ Range range_of(const int4 x) { return {x.x, x.y, x.z}; }
 __device__ __forceinline__ bool meet(Range a, Range b, bool common) {
-    return a.hi >= 0 && b.hi >= 0 && (common || (a.lo <= b.hi && b.lo <= a.hi));
+    return (a.hi >= 0) & (b.hi >= 0) & (common | ((a.lo <= b.hi) & (b.lo <= a.hi)));
 }
 
 // Range of the documents of tokens first .. last, by one wave.
@@ -294,21 +295,31 @@ __device__ __forceinline__ Range wave_range(const int* doc, int first, int last,
             __builtin_amdgcn_readfirstlane(whole)};
 }
 
-// Walks over the tiles of [at, end) that `test` accepts, 64 at a time: one lane tests one tile. The result
-// is the same in every wave of a workgroup, whose test does not depend on the wave.
+// Walks over the tiles of [at, end) that `test` accepts, 64 at a time: one lane tests one tile and keeps its
+// documents, so that going on to the next tile reads no memory. The result is the same in every wave of a
+// workgroup, whose test does not depend on the wave.
 struct TileWalk {
     int at, end;
     uint64_t left = 0;
+    Range held = {0, 0, 1};
+    // The next tile or -1; its documents into `of` (with `ranges`).
     template <typename F>
-    __device__ __forceinline__ int next(int lane, F test) {
+    __device__ __forceinline__ int next(int lane, const int4* ranges, Range& of, F test) {
         while (left == 0) {
             if (at >= end) return -1;
             const int t = at + lane;
-            left = __ballot(t < end && test(t));
+            if (ranges && t < end) {
+                const int4 x = ranges[t];
+                held = {x.x, x.y, x.z};
+            }
+            left = __ballot(t < end && test(t, held));
             at += 64;
         }
         const int b = __builtin_ctzll(left);
         left &= left - 1;
+        if (ranges)
+            of = {__builtin_amdgcn_readlane(held.lo, b), __builtin_amdgcn_readlane(held.hi, b),
+                  __builtin_amdgcn_readlane(held.whole, b)};
         return __builtin_amdgcn_readfirstlane(at - 64 + b);
     }
 };
@@ -380,7 +391,8 @@ struct Row32 {
 };
 
 // Keys and values staged tile by tile, for kernels that own rows: two buffers in LDS, and the next tile in
-// registers while the waves work on the current one.
+// registers while the waves work on the current one. All loads of a tile are issued together; what must not
+// count (keys past the last, padding) is dropped when the tile is put into LDS.
 // SUM_VALUES: the kernel sums over the values (forward), else over the keys (grad_q).
 template <typename T, int DP, int NW, bool BIASED, bool SUM_VALUES>
 struct KeyTiles {
@@ -395,59 +407,88 @@ struct KeyTiles {
     const AttnParams& p;
     const Work& w;
     const Row32& own;
-    const int4* ranges;
     const T *k, *v;
+    const int* docs;
     TileWalk walk;
-    int t, lane;
-    bool masks;
+    int t, lane, k_off, v_off;  // byte offsets of the thread's first chunk from a tile's first key
+    bool masks, clean;          // clean: all of the tile's keys count
     Range kr;
     uint4 kx[Tile::kLoads], vx[Tile::kLoads];
-    int doc_x;
-    float2 pos_x;
+    int doc_x[Tile::kLoads];
+    float2 pos_x[Tile::kLoads];
 
     __device__ __forceinline__ KeyTiles(Shared& s, const AttnParams& q, const Work& work, const Row32& row, int l)
         : sh(s), p(q), w(work), own(row), lane(l) {
-        ranges = p.k_ranges + (int64_t)w.n * p.k_tiles;
         k = static_cast<const T*>(p.k) + w.n * p.ks[0] + w.kv * p.ks[2];
         v = static_cast<const T*>(p.v) + w.n * p.vs[0] + w.kv * p.vs[2];
+        docs = p.k_doc ? p.k_doc + (int64_t)w.n * p.Lk : nullptr;
         walk.at = (int)((int64_t)p.k_tiles * w.split / p.splits);
         walk.end = (int)((int64_t)p.k_tiles * (w.split + 1) / p.splits);
         masks = p.q_doc || p.causal;
         kr = {0, 0, 1};
-        doc_x = 0;
-        pos_x = make_float2(0.f, 0.f);
+        k_off = (Tile::row(0) * (int)p.ks[1] + Tile::channel()) * (int)sizeof(T);
+        v_off = (Tile::row(0) * (int)p.vs[1] + Tile::channel()) * (int)sizeof(T);
+#pragma unroll
+        for (int a = 0; a < Tile::kLoads; ++a) {
+            kx[a] = vx[a] = make_uint4(0, 0, 0, 0);  // what lanes of channels from D on put into LDS
+            doc_x[a] = 0;
+            pos_x[a] = make_float2(0.f, 0.f);
+        }
     }
     // Finds the next tile that the workgroup's rows see, and loads it.
     __device__ __forceinline__ void fetch() {
-        t = walk.next(lane, [&](int u) {
+        const int4* ranges = p.q_doc ? p.k_ranges + (int64_t)w.n * p.k_tiles : nullptr;
+        t = walk.next(lane, ranges, kr, [&](int u, Range of) {
             const bool first = u * Tile::kRows < w.common;
-            if (p.causal && u * Tile::kRows > own.i_last + w.off && !first) return false;
-            return !p.q_doc || meet(own.docs, range_of(ranges[u]), first);
+            const bool in_order = !p.causal | (u * Tile::kRows <= own.i_last + w.off) | first;
+            return in_order & (!p.q_doc | meet(own.docs, of, first));
         });
         if (t < 0) return;
         const int j0 = t * Tile::kRows;
+        const bool full = j0 + Tile::kRows <= p.Lk;
+        clean = full && kr.whole;
         const T* kt = k + j0 * p.ks[1];
         const T* vt = v + j0 * p.vs[1];
-        if (p.q_doc) kr = range_of(ranges[t]);
-        const int* docs = p.k_doc + (int64_t)w.n * p.Lk + j0;
+        if (full) {
+            if (Tile::channel() < p.D) {
 #pragma unroll
-        for (int a = 0; a < Tile::kLoads; ++a) {
-            const int r = Tile::row(a), d = Tile::channel(a);
-            kx[a] = vx[a] = make_uint4(0, 0, 0, 0);
-            // padding is not read: what it holds must reach nothing
-            if (j0 + r < p.Lk && (kr.whole || docs[r] >= 0)) {
-                kx[a] = load_chunk(kt + r * p.ks[1], d, p.D);
-                vx[a] = load_chunk(vt + r * p.vs[1], d, p.D);
+                for (int a = 0; a < Tile::kLoads; ++a) {
+                    kx[a] = load_at(kt + a * Tile::kStep * p.ks[1], k_off);
+                    vx[a] = load_at(vt + a * Tile::kStep * p.vs[1], v_off);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int a = 0; a < Tile::kLoads; ++a)
+                if (j0 + Tile::row(a) < p.Lk && Tile::channel() < p.D) {
+                    kx[a] = load_at(kt + a * Tile::kStep * p.ks[1], k_off);
+                    vx[a] = load_at(vt + a * Tile::kStep * p.vs[1], v_off);
+                }
+        }
+        if (!clean || masks) {
+#pragma unroll
+            for (int a = 0; a < Tile::kLoads; ++a) {
+                const int j = j0 + Tile::row(a);
+                doc_x[a] = 0;
+                if (docs) doc_x[a] = docs[min(j, p.Lk - 1)];
             }
         }
-        if ((int)threadIdx.x < Tile::kRows) {
-            const int r = threadIdx.x;
-            doc_x = j0 + r >= p.Lk ? -1 : p.k_doc ? docs[r] : 0;
-            if (BIASED && p.slopes && j0 + r < p.Lk)
-                pos_x = reinterpret_cast<const float2*>(p.k_pos)[(int64_t)w.n * p.Lk + j0 + r];
+        if (BIASED && p.slopes) {
+#pragma unroll
+            for (int a = 0; a < Tile::kLoads; ++a)
+                if (Tile::channel() == 0)
+                    pos_x[a] = reinterpret_cast<const float2*>(p.k_pos)[(int64_t)w.n * p.Lk + min(j0 + Tile::row(a), p.Lk - 1)];
         }
     }
+    // Puts the tile into buffer b.
     __device__ __forceinline__ void stage(int b) {
+        if (!clean) {
+#pragma unroll
+            for (int a = 0; a < Tile::kLoads; ++a) {
+                if (t * Tile::kRows + Tile::row(a) >= p.Lk) doc_x[a] = -1;
+                if (doc_x[a] < 0) kx[a] = vx[a] = make_uint4(0, 0, 0, 0);
+            }
+        }
         if (masks) {
             bool odd = false;
 #pragma unroll
@@ -467,9 +508,12 @@ struct KeyTiles {
             Tile::put(sh.k[b], a, kx[a]);
             Tile::put(sh.v[b], a, vx[a]);
         }
-        if ((int)threadIdx.x < Tile::kRows) {
-            sh.doc[b][threadIdx.x] = doc_x;
-            if (BIASED) sh.pos[b][threadIdx.x] = pos_x;
+        if (Tile::channel() == 0) {
+#pragma unroll
+            for (int a = 0; a < Tile::kLoads; ++a) {
+                if (!clean || masks) sh.doc[b][Tile::row(a)] = doc_x[a];
+                if (BIASED) sh.pos[b][Tile::row(a)] = pos_x[a];
+            }
         }
     }
     // Notes what the weights of the block of 32 keys from key j0 on meet that was not finite in buffer b.

@@ -18,11 +18,11 @@ template <typename T>
 constexpr int kProbShift = std::is_same_v<T, _Float16> ? 8 : 0;
 
 // Waves per SIMD that the kernels' registers have to leave room for.
-constexpr int grad_q_waves(int DP) { return DP == 32 ? 3 : 2; }
+constexpr int grad_q_waves(int DP, size_t element) { return DP == 32 ? 3 : DP == 128 && element == 4 ? 1 : 2; }
 constexpr int grad_kv_waves(int DP) { return DP == 32 ? 3 : DP == 64 ? 2 : 1; }
 
 template <typename T, int DP, int NW, bool EXTRAS>
-__global__ __launch_bounds__(64 * NW, grad_q_waves(DP)) void attn_grad_q_kernel(AttnParams p) {
+__global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_grad_q_kernel(AttnParams p) {
     using O = Op<T>;
     using Keys = KeyTiles<T, DP, NW, EXTRAS, false>;
     using Tile = typename Keys::Tile;
@@ -156,57 +156,63 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     const int doc0 = __builtin_amdgcn_readfirstlane(doc);
     const bool one_doc = __all((doc == doc0) & (doc >= 0)), no_pad = __all(!pad);
     const int wave_last = j_first + wave * 32 + 31;
-    const int4* row_ranges = p.row_ranges + (int64_t)w.n * p.row_tiles;
     const bool masks = p.q_doc || p.causal;
 
     TileWalk walk;
     walk.at = (int)((int64_t)p.row_tiles * w.split / p.splits);
     walk.end = (int)((int64_t)p.row_tiles * (w.split + 1) / p.splits);
-    int t;
+    int t = -1;
+    bool clean = true;  // all of the tile's rows count
     Range rr = {0, 0, 1};
     uint4 qx[Tile::kLoads], gx[Tile::kLoads];
+    bool pad_x[Tile::kLoads];
     float lse_x = 0.f, delta_x = 0.f, slope_x = 0.f;
     int doc_x = -1, last_x = -1;
     float2 pos_x = make_float2(0.f, 0.f);
-    auto query_row = [&](int r) {
-        const int i = r / p.G, head = w.kv * p.G + r - i * p.G;
-        return static_cast<const T*>(p.q) + w.n * p.qs[0] + i * p.qs[1] + head * p.qs[2];
-    };
-    auto grad_row = [&](int r) {
-        const int i = r / p.G, head = w.kv * p.G + r - i * p.G;
-        return static_cast<const T*>(p.grad_out) + (((int64_t)w.n * p.Lq + i) * p.M + head) * p.row_width;
-    };
+#pragma unroll
+    for (int a = 0; a < Tile::kLoads; ++a) {
+        qx[a] = gx[a] = make_uint4(0, 0, 0, 0);  // what lanes of channels from D on put into LDS
+        pad_x[a] = false;
+    }
+    const float inv_g = 1.f / (float)p.G;
+    const T* q_base = static_cast<const T*>(p.q) + w.n * p.qs[0] + w.kv * p.G * p.qs[2];
+    const T* g_base = static_cast<const T*>(p.grad_out) + ((int64_t)w.n * p.Lq * p.M + w.kv * p.G) * p.row_width;
+    auto query_row = [&](int r) { return q_base + r / p.G * p.qs[1] + r % p.G * p.qs[2]; };
+    auto grad_row = [&](int r) { return g_base + ((int64_t)(r / p.G) * p.M + r % p.G) * p.row_width; };
     auto fetch = [&]() {
-        t = walk.next(lane, [&](int u) {
+        const int4* ranges = p.q_doc ? p.row_ranges + (int64_t)w.n * p.row_tiles : nullptr;
+        t = walk.next(lane, ranges, rr, [&](int u, Range of) {
             const int i_last = (min((u + 1) * Tile::kRows, p.R) - 1) / p.G;
-            if (p.causal && j_first > i_last + w.off && j_first >= w.common) return false;
-            return !p.q_doc || meet(docs, range_of(row_ranges[u]), j_first < w.common);
+            const bool first = j_first < w.common, in_order = !p.causal | (j_first <= i_last + w.off) | first;
+            return in_order & (!p.q_doc | meet(docs, of, first));
         });
         if (t < 0) return;
-        const int r0 = t * Tile::kRows;
-        if (p.q_doc) rr = range_of(row_ranges[t]);
+        // row r of the tile is query i0 + (g0 + r) / G of head (g0 + r) % G of the group
+        const int r0 = t * Tile::kRows, i0 = r0 / p.G, g0 = r0 - i0 * p.G;
+        clean = r0 + Tile::kRows <= p.R && rr.whole;
+        const T* qt = q_base + i0 * p.qs[1];
+        const T* gt = g_base + (int64_t)i0 * p.M * p.row_width;
 #pragma unroll
         for (int a = 0; a < Tile::kLoads; ++a) {
-            const int r = r0 + Tile::row(a), d = Tile::channel(a);
-            qx[a] = gx[a] = make_uint4(0, 0, 0, 0);
-            if (r < p.R && (rr.whole || p.q_doc[(int64_t)w.n * p.Lq + r / p.G] >= 0)) {
-                qx[a] = load_chunk(query_row(r), d, p.D);
-                gx[a] = load_chunk(grad_row(r), d, p.D);
+            const int x = g0 + Tile::row(a), i = small_div(x, inv_g), g = x - i * p.G;
+            const bool in = r0 + Tile::row(a) < p.R;
+            if (in && Tile::channel() < p.D) {
+                qx[a] = load_at(qt, (i * (int)p.qs[1] + g * (int)p.qs[2] + Tile::channel()) * (int)sizeof(T));
+                gx[a] = load_at(gt, ((i * p.M + g) * p.row_width + Tile::channel()) * (int)sizeof(T));
             }
+            if (!clean) pad_x[a] = !in || (p.q_doc && p.q_doc[(int64_t)w.n * p.Lq + i0 + i] < 0);
         }
         if ((int)threadIdx.x < Tile::kRows) {
-            const int r = r0 + threadIdx.x;
+            const int x = g0 + (int)threadIdx.x, i = i0 + small_div(x, inv_g), head = w.kv * p.G + x - (i - i0) * p.G;
             lse_x = kInf;  // rows past the last: p = 0
             delta_x = 0.f;
             last_x = doc_x = -1;
-            if (r < p.R) {
-                const int i = r / p.G, head = w.kv * p.G + r - i * p.G;
+            if (r0 + (int)threadIdx.x < p.R) {
                 const int64_t at = ((int64_t)w.n * p.M + head) * p.Lq + i;
-                const float x = p.lse[at];
-                if (x != -kInf) lse_x = x * kLog2e;
+                lse_x = p.lse[at];
                 delta_x = p.delta[at];
                 doc_x = p.q_doc ? p.q_doc[(int64_t)w.n * p.Lq + i] : 0;
-                last_x = doc_x < 0 ? -1 : p.causal ? max(i + w.off, w.common - 1) : p.Lk - 1;
+                last_x = p.causal ? max(i + w.off, w.common - 1) : p.Lk - 1;
                 if (EXTRAS && p.slopes) {
                     slope_x = p.slopes[head] * kLog2e;
                     pos_x = reinterpret_cast<const float2*>(p.q_pos)[(int64_t)w.n * p.Lq + i];
@@ -215,6 +221,11 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
         }
     };
     auto stage = [&](int b) {
+        if (!clean) {
+#pragma unroll
+            for (int a = 0; a < Tile::kLoads; ++a)
+                if (pad_x[a]) qx[a] = gx[a] = make_uint4(0, 0, 0, 0);
+        }
         if (masks) {  // sums are over queries and over grad_out
             bool odd = false;
 #pragma unroll
@@ -238,10 +249,10 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             Tile::put(s_g[b], a, gx[a]);
         }
         if ((int)threadIdx.x < Tile::kRows) {
-            s_lse[b][threadIdx.x] = kProbShift<T> - lse_x;
+            s_lse[b][threadIdx.x] = lse_x == -kInf ? -kInf : kProbShift<T> - lse_x * kLog2e;
             s_delta[b][threadIdx.x] = -delta_x;
             s_doc[b][threadIdx.x] = doc_x;
-            s_last[b][threadIdx.x] = last_x;
+            s_last[b][threadIdx.x] = doc_x < 0 ? -1 : last_x;
             if (EXTRAS) {
                 s_slope[b][threadIdx.x] = slope_x;
                 s_pos[b][threadIdx.x] = pos_x;

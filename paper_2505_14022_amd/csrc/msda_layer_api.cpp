@@ -244,13 +244,18 @@ msda_status_t check_attention(const msda_attention_t* a) {
         return fail(MSDA_ERROR_INVALID_VALUE, "softcap=%g must be finite and >= 0", (double)a->softcap);
     if (a->causal && a->Lk < a->Lq)
         return fail(MSDA_ERROR_INVALID_VALUE, "causal needs Lk=%lld >= Lq=%lld", (long long)a->Lk, (long long)a->Lq);
-    if (a->N > kMaxInt || a->M > kMaxInt || a->Lk > kMaxInt - 1024 || a->Lq > (kMaxInt - 1024) / (a->M / a->Mkv))
-        return fail(MSDA_ERROR_NOT_SUPPORTED, "N, M, Lk or Lq * M / Mkv exceeds 2^31");
+    if (a->M > 32768)  // the rows of a tile lie within 2^31 bytes
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "M=%lld heads exceeds 32768", (long long)a->M);
+    if (a->N > kMaxInt || a->Lk > kMaxInt - 1024 || a->Lq > (kMaxInt - 1024) / (a->M / a->Mkv))
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "N, Lk or Lq * M / Mkv exceeds 2^31");
     // every launch is one grid: at most 2^30 slabs (batch item, key head) and 2^33 of their rows or keys, in at
     // least 32 per workgroup of the attention kernels and 4 of the ones that add splits
     const double slabs = (double)a->N * (double)a->Mkv, rows = (double)a->Lq * (double)(a->M / a->Mkv);
     if (slabs > 1073741824.0 || slabs * rows > 8589934592.0 || slabs * (double)a->Lk > 8589934592.0)
         return fail(MSDA_ERROR_NOT_SUPPORTED, "N * Mkv heads of these lengths are too many for one launch");
+    for (int i = 0; i < 3; ++i)
+        if (a->q_stride[i] < 0 || a->k_stride[i] < 0 || a->v_stride[i] < 0)
+            return fail(MSDA_ERROR_INVALID_VALUE, "strides must be >= 0");
     // with empty extents any table may be null; the pointers are not looked at then
     if (a->N > 0 && a->Lq > 0 && a->Lk > 0) {
         if ((a->q_doc != nullptr) != (a->k_doc != nullptr))
@@ -274,12 +279,14 @@ struct Attention {
     int width = 0;  // of a packed row
 };
 
-// Whether rows of D channels with these strides are whole 16-byte pieces on 16-byte boundaries of their base.
-bool row_pieces(const int64_t* stride, int64_t N, int64_t L, int64_t H, int64_t D, int es) {
+// Whether rows of D channels with these strides are whole 16-byte pieces on 16-byte boundaries of their base, and
+// the rows of a tile (at most 65 tokens of `heads` heads) lie within the 31 bits of the kernels' offsets.
+bool row_pieces(const int64_t* stride, int64_t N, int64_t L, int64_t H, int64_t heads, int64_t D, int es) {
     const int64_t extent[3] = {N, L, H};
     bool yes = (D * es) % 16 == 0;
     for (int i = 0; i < 3; ++i) yes = yes && (extent[i] <= 1 || (stride[i] * es) % 16 == 0);
-    return yes;
+    const double reach = (L > 1 ? 65.0 * fabs((double)stride[1]) : 0.0) + (double)(heads - 1) * fabs((double)stride[2]) + D;
+    return yes && reach * es < 2147483648.0;
 }
 
 Attention attention_of(const msda_attention_t& a, bool backward) {
@@ -322,9 +329,9 @@ Attention attention_of(const msda_attention_t& a, bool backward) {
     x.at_delta = at;
     if (backward) at += round_up(sizeof(float) * a.N * a.M * a.Lq);
     x.width = (int)ceil_div(a.D * es, 16) * 16 / es;
-    x.pack[0] = a.unaligned || !row_pieces(a.q_stride, a.N, a.Lq, a.M, a.D, es);
-    x.pack[1] = a.unaligned || !row_pieces(a.k_stride, a.N, a.Lk, a.Mkv, a.D, es);
-    x.pack[2] = a.unaligned || !row_pieces(a.v_stride, a.N, a.Lk, a.Mkv, a.D, es);
+    x.pack[0] = a.unaligned || !row_pieces(a.q_stride, a.N, a.Lq, a.M, G, a.D, es);
+    x.pack[1] = a.unaligned || !row_pieces(a.k_stride, a.N, a.Lk, a.Mkv, 1, a.D, es);
+    x.pack[2] = a.unaligned || !row_pieces(a.v_stride, a.N, a.Lk, a.Mkv, 1, a.D, es);
     x.pack[3] = x.pack[4] = backward && (a.D * es) % 16 != 0;
     for (int i = 0; i < 5; ++i) {
         x.at_pack[i] = at;
