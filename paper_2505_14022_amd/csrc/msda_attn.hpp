@@ -28,15 +28,16 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 
 // tanh(x) = 1 - 2 / (e^2x + 1), off by an fp32 rounding of 1; with fp32 operands, where that shows in
 // the result, |x| < 1/4 goes through the series x - x^3/3 + 2x^5/15 - 17x^7/315 (next term: 8e-8 of x).
+// Of s * a, with a2 = 2 log2(e) a.
 template <bool SERIES>
-__device__ __forceinline__ float tanh_of(float x) {
-    const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(exp2_of(2.f * kLog2e * x) + 1.f);
+__device__ __forceinline__ float tanh_of(float s, float a, float a2) {
+    const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(exp2_of(s * a2) + 1.f), 1.f);
     if constexpr (!SERIES) return t;
-    const float x2 = x * x;
-    float s = __builtin_fmaf(x2, -17.f / 315.f, 2.f / 15.f);
-    s = __builtin_fmaf(s, x2, -1.f / 3.f);
-    s = __builtin_fmaf(s * x2, x, x);
-    return fabsf(x) < 0.25f ? s : t;
+    const float x = s * a, x2 = x * x;
+    float y = __builtin_fmaf(x2, -17.f / 315.f, 2.f / 15.f);
+    y = __builtin_fmaf(y, x2, -1.f / 3.f);
+    y = __builtin_fmaf(y * x2, x, x);
+    return fabsf(x) < 0.25f ? y : t;
 }
 
 // The value of both half waves' lanes l and l ^ 32: x of the lower half in lo, of the upper in hi.
@@ -273,40 +274,18 @@ __device__ __forceinline__ bool meet(Range a, Range b, bool common) {
     return (a.hi >= 0) & (b.hi >= 0) & (common | ((a.lo <= b.hi) & (b.lo <= a.hi)));
 }
 
-// Range of the documents of tokens first .. last, by one wave.
-__device__ __forceinline__ Range wave_range(const int* doc, int first, int last, int lane) {
-    int lo = 0x7fffffff, hi = -1, whole = 1;
-    for (int i = first + lane; i <= last; i += 64) {
-        const int d = doc[i];
-        if (d >= 0) {
-            lo = min(lo, d);
-            hi = max(hi, d);
-        } else {
-            whole = 0;
-        }
-    }
-#pragma unroll
-    for (int m = 32; m; m >>= 1) {
-        lo = min(lo, __shfl_xor(lo, m, 64));
-        hi = max(hi, __shfl_xor(hi, m, 64));
-        whole &= __shfl_xor(whole, m, 64);
-    }
-    return {__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi),
-            __builtin_amdgcn_readfirstlane(whole)};
-}
-
 // Walks over the tiles of [at, end) that `test` accepts, 64 at a time: one lane tests one tile and keeps its
 // documents, so that going on to the next tile reads no memory. The result is the same in every wave of a
 // workgroup, whose test does not depend on the wave.
 struct TileWalk {
-    int at, end;
+    int at = 0, end = 0;
     uint64_t left = 0;
     Range held = {0, 0, 1};
-    // The next tile or -1; its documents into `of` (with `ranges`).
+    // Whether there is a tile left to visit.
     template <typename F>
-    __device__ __forceinline__ int next(int lane, const int4* ranges, Range& of, F test) {
+    __device__ __forceinline__ bool more(int lane, const int4* ranges, F test) {
         while (left == 0) {
-            if (at >= end) return -1;
+            if (at >= end) return false;
             const int t = at + lane;
             if (ranges && t < end) {
                 const int4 x = ranges[t];
@@ -315,6 +294,12 @@ struct TileWalk {
             left = __ballot(t < end && test(t, held));
             at += 64;
         }
+        return true;
+    }
+    // The next tile or -1; its documents into `of` (with `ranges`).
+    template <typename F>
+    __device__ __forceinline__ int next(int lane, const int4* ranges, Range& of, F test) {
+        if (!more(lane, ranges, test)) return -1;
         const int b = __builtin_ctzll(left);
         left &= left - 1;
         if (ranges)
@@ -329,10 +314,12 @@ struct TileWalk {
 __device__ __forceinline__ int xcd_item(int b, int grid) { return (b & 7) * (grid >> 3) + (b >> 3); }
 int xcd_grid(int64_t items) { return (int)((items + 7) / 8 * 8); }
 
-// What a workgroup works on.
+// What a workgroup works on: a block of owners and a run of the other axis' tiles.
 struct Work {
     int slab, block, split, n, kv, common, off;
     bool any;
+    Range docs;  // of the block's owners
+    TileWalk walk;
     // last_first: blocks from the last to the first, so that causal rows with the most keys go first
     __device__ __forceinline__ Work(const AttnParams& p, bool last_first) {
         const int item = xcd_item(blockIdx.x, gridDim.x), per_slab = p.blocks * p.splits;
@@ -346,8 +333,31 @@ struct Work {
         kv = slab - n * p.Mkv;
         off = p.Lk - p.Lq;
         common = any && p.prefix ? min(max(p.prefix[n], 0), p.Lk) : 0;
+        docs = {0, 0, 1};
+        if (any && p.own_ranges) {
+            const int4 x = p.own_ranges[(int64_t)n * p.blocks + block];
+            docs = {x.x, x.y, x.z};
+        }
+        walk.at = split * p.chunk;
+        walk.end = min(walk.at + p.chunk, p.tiles);
+    }
+    __device__ __forceinline__ const int4* tile_ranges(const AttnParams& p) const {
+        return p.tile_ranges ? p.tile_ranges + (int64_t)n * p.tiles : nullptr;
+    }
+    // With splits, notes whether this one has any tile to visit: the rest of it is not written otherwise.
+    __device__ __forceinline__ bool note_split(const AttnParams& p, bool visits_any) const {
+        if (p.splits == 1) return true;
+        if (threadIdx.x == 0) p.filled[((int64_t)slab * p.blocks + block) * p.splits + split] = visits_any;
+        return visits_any;
     }
 };
+
+// Whether any of a block of rows, up to query i_last and of documents `rows`, sees any of the keys from j_first on, of
+// documents `keys`.
+__device__ __forceinline__ bool sees(const AttnParams& p, const Work& w, int i_last, Range rows, int j_first, Range keys) {
+    const bool first = j_first < w.common, in_order = !p.causal | (j_first <= i_last + w.off) | first;
+    return in_order & (!p.q_doc | meet(rows, keys, first));
+}
 
 // The row that a lane owns, and what it sees: keys up to `last` of document `doc`, or below `common`.
 struct Row32 {
@@ -356,9 +366,7 @@ struct Row32 {
     int64_t stat;  // its place in [N, M, Lq]
     float slope;
     float2 pos;
-    // over the workgroup's rows: the last query and the documents; over the wave's: the first one's last key
-    int i_last, last0, doc0;
-    Range docs;
+    int last0, doc0;  // of the wave's first row
     bool one_doc, no_pad;
 
     template <int NW>
@@ -379,9 +387,6 @@ struct Row32 {
             x.slope = p.slopes[x.head] * kLog2e;
             x.pos = reinterpret_cast<const float2*>(p.q_pos)[(int64_t)w.n * p.Lq + x.i];
         }
-        x.i_last = (min(first + 32 * NW, p.R) - 1) / p.G;
-        x.docs = {0, 0, 1};
-        if (p.q_doc) x.docs = wave_range(p.q_doc + (int64_t)w.n * p.Lq, first / p.G, x.i_last, lane);
         x.doc0 = __builtin_amdgcn_readfirstlane(x.doc);
         x.one_doc = __all((x.doc == x.doc0) & (x.doc >= 0));
         x.no_pad = __all(x.doc >= 0);
@@ -389,6 +394,10 @@ struct Row32 {
         return x;
     }
 };
+
+// The keys of a staged tile as the rows' masks need them: the document, kCommon for one that all documents
+// see, or -1 for one that nobody sees.
+constexpr int kCommon = -2;
 
 // Keys and values staged tile by tile, for kernels that own rows: two buffers in LDS, and the next tile in
 // registers while the waves work on the current one. All loads of a tile are issued together; what must not
@@ -405,25 +414,21 @@ struct KeyTiles {
     };
     Shared& sh;
     const AttnParams& p;
-    const Work& w;
-    const Row32& own;
+    Work& w;
     const T *k, *v;
     const int* docs;
-    TileWalk walk;
-    int t, lane, k_off, v_off;  // byte offsets of the thread's first chunk from a tile's first key
+    int t, lane, i_last, k_off, v_off;  // byte offsets of the thread's first chunk from a tile's first key
     bool masks, clean;          // clean: all of the tile's keys count
     Range kr;
     uint4 kx[Tile::kLoads], vx[Tile::kLoads];
     int doc_x[Tile::kLoads];
     float2 pos_x[Tile::kLoads];
 
-    __device__ __forceinline__ KeyTiles(Shared& s, const AttnParams& q, const Work& work, const Row32& row, int l)
-        : sh(s), p(q), w(work), own(row), lane(l) {
+    __device__ __forceinline__ KeyTiles(Shared& s, const AttnParams& q, Work& work, int l) : sh(s), p(q), w(work), lane(l) {
         k = static_cast<const T*>(p.k) + w.n * p.ks[0] + w.kv * p.ks[2];
         v = static_cast<const T*>(p.v) + w.n * p.vs[0] + w.kv * p.vs[2];
         docs = p.k_doc ? p.k_doc + (int64_t)w.n * p.Lk : nullptr;
-        walk.at = (int)((int64_t)p.k_tiles * w.split / p.splits);
-        walk.end = (int)((int64_t)p.k_tiles * (w.split + 1) / p.splits);
+        i_last = (min((w.block + 1) * 32 * NW, p.R) - 1) / p.G;
         masks = p.q_doc || p.causal;
         kr = {0, 0, 1};
         k_off = (Tile::row(0) * (int)p.ks[1] + Tile::channel()) * (int)sizeof(T);
@@ -435,14 +440,14 @@ struct KeyTiles {
             pos_x[a] = make_float2(0.f, 0.f);
         }
     }
+    // Whether the workgroup's rows see any of its run of tiles.
+    __device__ __forceinline__ bool any() {
+        return w.walk.more(lane, w.tile_ranges(p), [&](int u, Range of) { return sees(p, w, i_last, w.docs, u * Tile::kRows, of); });
+    }
     // Finds the next tile that the workgroup's rows see, and loads it.
     __device__ __forceinline__ void fetch() {
-        const int4* ranges = p.q_doc ? p.k_ranges + (int64_t)w.n * p.k_tiles : nullptr;
-        t = walk.next(lane, ranges, kr, [&](int u, Range of) {
-            const bool first = u * Tile::kRows < w.common;
-            const bool in_order = !p.causal | (u * Tile::kRows <= own.i_last + w.off) | first;
-            return in_order & (!p.q_doc | meet(own.docs, of, first));
-        });
+        t = w.walk.next(lane, w.tile_ranges(p), kr,
+                        [&](int u, Range of) { return sees(p, w, i_last, w.docs, u * Tile::kRows, of); });
         if (t < 0) return;
         const int j0 = t * Tile::kRows;
         const bool full = j0 + Tile::kRows <= p.Lk;
@@ -511,7 +516,8 @@ struct KeyTiles {
         if (Tile::channel() == 0) {
 #pragma unroll
             for (int a = 0; a < Tile::kLoads; ++a) {
-                if (!clean || masks) sh.doc[b][Tile::row(a)] = doc_x[a];
+                const int j = t * Tile::kRows + Tile::row(a);
+                if (!clean || masks) sh.doc[b][Tile::row(a)] = doc_x[a] >= 0 && j < w.common ? kCommon : doc_x[a];
                 if (BIASED) sh.pos[b][Tile::row(a)] = pos_x[a];
             }
         }
@@ -528,7 +534,7 @@ struct KeyTiles {
             });
     }
     // Whether all rows of the wave see all keys of the tile just loaded.
-    __device__ __forceinline__ bool whole() const {
+    __device__ __forceinline__ bool whole(const Row32& own) const {
         const int j1 = t * Tile::kRows + Tile::kRows - 1;
         bool x = j1 <= own.last0 && j1 < p.Lk;
         if (p.q_doc)
@@ -540,19 +546,38 @@ struct KeyTiles {
 // The row of the register r of a 32 x 32 block.
 __device__ __forceinline__ int block_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
-// Raw scores of a block turned into scores in units of log 2 once multiplied by the result. With a cap,
-// slack[r] gets the cap's derivative 1 - tanh^2 if `slack` is given.
+// Raw scores of a block made scores in units of log 2, but for a factor, which is returned and left to the
+// exponent: the scale, or the cap, of which `s` holds the tanh then. `ds` (if given) is multiplied by the cap's
+// derivative 1 - tanh^2.
 template <typename T>
-__device__ __forceinline__ float cap_scores(const AttnParams& p, acc_t& s, acc_t* slack) {
+__device__ __forceinline__ float cap_scores(const AttnParams& p, acc_t& s, acc_t* ds) {
     if (!(p.softcap > 0.f)) return p.scale * kLog2e;
-    const float a = p.scale / p.softcap, cap = p.softcap * kLog2e;
+    const float a = p.scale / p.softcap, a2 = 2.f * kLog2e * a;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        const float t = tanh_of<std::is_same_v<T, float>>(s[r] * a);
-        if (slack) (*slack)[r] *= 1.f - t * t;
-        s[r] = cap * t;
+        s[r] = tanh_of<std::is_same_v<T, float>>(s[r], a, a2);
+        if (ds) (*ds)[r] *= __builtin_fmaf(-s[r], s[r], 1.f);
     }
-    return 1.f;
+    return p.softcap * kLog2e;
+}
+
+// Replaces the values of pairs that are not seen in a block of one lane's row and the 32 keys from jt on in the tile. `last`: the
+// row's last key, counted from the tile's first; `codes`: the tile's keys. Four at a time, or the compiler holds the
+// comparisons of all in scalar registers and spills them.
+template <int N>
+__device__ __forceinline__ void hide(acc_t (&x)[N], float with, int jt, int h, int last, int doc, const int* codes) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int4 c4 = *reinterpret_cast<const int4*>(codes + jt + 8 * g + 4 * h);
+        const int code[4] = {c4.x, c4.y, c4.z, c4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool seen = ((code[e] == doc) | (code[e] == kCommon)) & (jt + 8 * g + 4 * h + e <= last);
+#pragma unroll
+            for (int n = 0; n < N; ++n) x[n][4 * g + e] = seen ? x[n][4 * g + e] : with;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 // Stores four consecutive channels of a result row.

@@ -28,9 +28,12 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
     __shared__ uint32_t odd_words[32 * NW * Odd<DP>::kWords];
-    const Work w(p, true);
+    Work w(p, true);
     if (!w.any) return;
     const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
+    Keys keys(sh, p, w, lane);
+    const bool any = w.note_split(p, keys.any());
+    if (!any && w.split > 0) return;  // the first split writes delta
     const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS);
     typename O::Frag q[DP / O::K], go[DP / O::K];
     float delta = 0.f;
@@ -49,6 +52,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
         }
         delta = halves_sum(delta);
         if (w.split == 0 && h == 0 && own.row < p.R) p.delta[own.stat] = delta;
+        if (!any) return;
     }
     const float lse = p.lse[own.stat] == -kInf ? kInf : p.lse[own.stat] * kLog2e;  // a row that saw nothing: p = 0
     acc_t minus_delta, gq[DP / 32];
@@ -58,11 +62,10 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
     for (int u = 0; u < DP / 32; ++u) gq[u] = acc_t{};
     Odd<DP> odd;
     odd.start(odd_words, wave * 32 + (lane & 31), lane, p.q_doc || p.causal);
-    Keys keys(sh, p, w, own, lane);
     keys.fetch();
     for (int b = 0; keys.t >= 0; b ^= 1) {
         keys.stage(b);
-        const bool whole = keys.whole();
+        const bool whole = keys.whole(own);
         const int j0 = keys.t * Tile::kRows;
         __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
         keys.fetch();
@@ -87,12 +90,9 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
 #pragma unroll
             for (int r = 0; r < 16; ++r) ds[r] *= exp2_of(__builtin_fmaf(s[r], unit, -lse));
             if (!whole) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int jt = kb * 32 + block_row(r, h), kd = sh.doc[b][jt];
-                    const bool seen = (j0 + jt <= own.last) & (kd >= 0) & ((kd == own.doc) | (j0 + jt < w.common));
-                    ds[r] = seen ? ds[r] : 0.f;
-                }
+                acc_t x[1] = {ds};
+                hide(x, 0.f, kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
+                ds = x[0];
             }
             add_product<T, DP>(gq, ds, kt, Tile::kStride, lane);
             keys.note_odd(odd, ds, b, j0 + kb * 32);
@@ -126,12 +126,17 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     __shared__ __attribute__((aligned(16))) float2 s_pos[2][EXTRAS ? Tile::kRows : 1];
     __shared__ int s_odd[2][NW];
     __shared__ uint32_t odd_words[2][32 * NW * Odd<DP>::kWords];
-    const Work w(p, false);  // the first keys have the most rows
+    Work w(p, false);  // the first keys have the most rows
     if (!w.any) return;
     const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
+    const int j_first = w.block * 32 * NW;
+    auto visits = [&](int u, Range of) {
+        return sees(p, w, (min((u + 1) * Tile::kRows, p.R) - 1) / p.G, of, j_first, w.docs);
+    };
+    if (!w.note_split(p, w.walk.more(lane, w.tile_ranges(p), visits))) return;
 
     // the lane's key, in registers with its value
-    const int j_first = w.block * 32 * NW, key = j_first + wave * 32 + (lane & 31);
+    const int key = j_first + wave * 32 + (lane & 31);
     const int j = min(key, p.Lk - 1);
     const int doc = p.k_doc ? p.k_doc[(int64_t)w.n * p.Lk + j] : 0;
     const bool pad = key >= p.Lk || doc < 0;  // what padding holds must reach nothing
@@ -149,18 +154,14 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     float2 pos = make_float2(0.f, 0.f);
     if (EXTRAS && p.slopes) pos = reinterpret_cast<const float2*>(p.k_pos)[(int64_t)w.n * p.Lk + j];
     const bool is_common = key < w.common;
+    const int key_code = pad ? 0x7fffffff : key;  // past the last key that any row sees
 
-    // what the workgroup's keys are seen by at most, and the wave's at least
-    Range docs = {0, 0, 1};
-    if (p.k_doc) docs = wave_range(p.k_doc + (int64_t)w.n * p.Lk, j_first, min(j_first + 32 * NW, p.Lk) - 1, lane);
+    // what all of the wave's keys are seen by
     const int doc0 = __builtin_amdgcn_readfirstlane(doc);
     const bool one_doc = __all((doc == doc0) & (doc >= 0)), no_pad = __all(!pad);
     const int wave_last = j_first + wave * 32 + 31;
     const bool masks = p.q_doc || p.causal;
 
-    TileWalk walk;
-    walk.at = (int)((int64_t)p.row_tiles * w.split / p.splits);
-    walk.end = (int)((int64_t)p.row_tiles * (w.split + 1) / p.splits);
     int t = -1;
     bool clean = true;  // all of the tile's rows count
     Range rr = {0, 0, 1};
@@ -180,12 +181,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     auto query_row = [&](int r) { return q_base + r / p.G * p.qs[1] + r % p.G * p.qs[2]; };
     auto grad_row = [&](int r) { return g_base + ((int64_t)(r / p.G) * p.M + r % p.G) * p.row_width; };
     auto fetch = [&]() {
-        const int4* ranges = p.q_doc ? p.row_ranges + (int64_t)w.n * p.row_tiles : nullptr;
-        t = walk.next(lane, ranges, rr, [&](int u, Range of) {
-            const int i_last = (min((u + 1) * Tile::kRows, p.R) - 1) / p.G;
-            const bool first = j_first < w.common, in_order = !p.causal | (j_first <= i_last + w.off) | first;
-            return in_order & (!p.q_doc | meet(docs, of, first));
-        });
+        t = w.walk.next(lane, w.tile_ranges(p), rr, visits);
         if (t < 0) return;
         // row r of the tile is query i0 + (g0 + r) / G of head (g0 + r) % G of the group
         const int r0 = t * Tile::kRows, i0 = r0 / p.G, g0 = r0 - i0 * p.G;
@@ -307,11 +303,17 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             }
             if (!whole) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int at = rb * 32 + block_row(r, h), qd = s_doc[b][at];
-                    const bool seen = (key <= s_last[b][at]) & !pad & ((qd == doc) | is_common);
-                    s[r] = seen ? s[r] : 0.f;
-                    ds[r] = seen ? ds[r] : 0.f;
+                for (int g = 0; g < 4; ++g) {  // four at a time, as in hide()
+                    const int at = rb * 32 + 8 * g + 4 * h;
+                    const int4 l4 = *reinterpret_cast<const int4*>(&s_last[b][at]), d4 = *reinterpret_cast<const int4*>(&s_doc[b][at]);
+                    const int last[4] = {l4.x, l4.y, l4.z, l4.w}, row_doc[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool seen = (key_code <= last[e]) & ((row_doc[e] == doc) | is_common);
+                        s[4 * g + e] = seen ? s[4 * g + e] : 0.f;
+                        ds[4 * g + e] = seen ? ds[4 * g + e] : 0.f;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
             add_product<T, DP>(gv, s, gt, Tile::kStride, lane);
@@ -361,19 +363,21 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(AttnParams p) {
     const int64_t per_slab = KV ? p.Lk : p.R;
     const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
     if (at >= (int64_t)p.N * p.Mkv * per_slab) return;
+    const int64_t slab = at / per_slab, n = slab / p.Mkv;
+    const int own = (int)(at - slab * per_slab), kv = (int)(slab - n * p.Mkv);
+    const int* filled = p.filled + (slab * p.blocks + own / p.own_rows) * p.splits;
     const int e0 = (threadIdx.x % kLanes) * 4;
     const float* part = p.part + at * p.splits * (kLanes * 4) + e0;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int s = 0; s < p.splits; ++s) {
+        if (!filled[s]) continue;
         const float4 y = *reinterpret_cast<const float4*>(part + (int64_t)s * (kLanes * 4));
         x[0] += y.x;
         x[1] += y.y;
         x[2] += y.z;
         x[3] += y.w;
     }
-    const int64_t slab = at / per_slab, n = slab / p.Mkv;
-    const int own = (int)(at - slab * per_slab), kv = (int)(slab - n * p.Mkv);
     const bool values = KV && e0 >= DP;
     T* out;
     if constexpr (KV) {

@@ -21,9 +21,11 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
     __shared__ uint32_t odd_words[32 * NW * Odd<DP>::kWords];
-    const Work w(p, true);
+    Work w(p, true);
     if (!w.any) return;
     const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
+    Keys keys(sh, p, w, lane);
+    if (!w.note_split(p, keys.any())) return;
     const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS);
     typename O::Frag q[DP / O::K];
     const T* qr = static_cast<const T*>(p.q) + w.n * p.qs[0] + own.i * p.qs[1] + own.head * p.qs[2];
@@ -37,11 +39,10 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
     float m = -kInf, l = 0.f;
     Odd<DP> odd;
     odd.start(odd_words, wave * 32 + (lane & 31), lane, p.q_doc || p.causal);
-    Keys keys(sh, p, w, own, lane);
     keys.fetch();
     for (int b = 0; keys.t >= 0; b ^= 1) {
         keys.stage(b);
-        const bool whole = keys.whole();
+        const bool whole = keys.whole(own);
         const int j0 = keys.t * Tile::kRows;
         __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
         keys.fetch();
@@ -64,12 +65,9 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
                 }
             }
             if (!whole) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int jt = kb * 32 + block_row(r, h), kd = sh.doc[b][jt];
-                    const bool seen = (j0 + jt <= own.last) & (kd >= 0) & ((kd == own.doc) | (j0 + jt < w.common));
-                    s[kb][r] = seen ? s[kb][r] : -kInf;
-                }
+                acc_t x[1] = {s[kb]};
+                hide(x, -kInf, kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
+                s[kb] = x[0];
             }
         }
         float top = s[0][0];
@@ -142,15 +140,20 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
     const int64_t rows = (int64_t)p.N * p.Mkv * p.R;
     const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
     if (at >= rows) return;
+    const int64_t slab = at / p.R;
+    const int row = (int)(at - slab * p.R), i = row / p.G;
+    const int* filled = p.filled + (slab * p.blocks + row / p.own_rows) * p.splits;
     const int d = (threadIdx.x % kLanes) * 4;
     const float2* stats = reinterpret_cast<const float2*>(p.part + rows * p.splits * DP) + at * p.splits;
     const float* part = p.part + at * p.splits * DP + d;
-    float top = -kInf;
-    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, stats[s].x);
+    float top = -kInf, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s)
+        if (filled[s]) top = fmaxf(top, stats[s].x);
     const float base = top == -kInf ? 0.f : top;
-    float x[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
 #pragma unroll 4
     for (int s = 0; s < p.splits; ++s) {
+        if (!filled[s]) continue;
         const float2 ml = stats[s];
         const float w = exp2_of(ml.x - base);
         const float4 y = *reinterpret_cast<const float4*>(part + (int64_t)s * DP);
@@ -160,8 +163,6 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
         x[2] += w * y.z;
         x[3] += w * y.w;
     }
-    const int64_t slab = at / p.R;
-    const int row = (int)(at - slab * p.R), i = row / p.G;
     const int64_t n = slab / p.Mkv;
     const int head = (int)(slab - n * p.Mkv) * p.G + row - i * p.G;
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -172,21 +173,35 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
         p.lse[(n * p.M + head) * p.Lq + i] = l == 0.f ? -kInf : (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Documents of each tile of keys, or of each tile of rows (the queries that its rows belong to).
-__global__ __launch_bounds__(256) void attn_ranges_kernel(AttnParams p, int k_tile, int row_tile) {
+// Documents of the tiles and blocks of each table of a call, one wave for each.
+__global__ __launch_bounds__(256) void attn_ranges_kernel(AttnRanges c) {
     const int lane = threadIdx.x & 63;
-    const int per = p.k_tiles + (row_tile ? p.row_tiles : 0);
-    const int64_t item = (int64_t)blockIdx.x * 4 + wave_index();
-    if (item >= (int64_t)p.N * per) return;
-    const int64_t n = item / per;
-    int t = (int)(item - n * per);
-    const bool keys = t < p.k_tiles;
-    if (!keys) t -= p.k_tiles;
-    const int first = keys ? t * k_tile : t * row_tile / p.G;
-    const int last = keys ? min((t + 1) * k_tile, p.Lk) - 1 : (min((t + 1) * row_tile, p.R) - 1) / p.G;
-    const Range r = wave_range(keys ? p.k_doc + n * p.Lk : p.q_doc + n * p.Lq, first, last, lane);
-    int4* into = keys ? p.k_ranges + n * p.k_tiles : p.row_ranges + n * p.row_tiles;
-    if (lane == 0) into[t] = make_int4(r.lo, r.hi, r.whole, 0);
+    int64_t item = (int64_t)blockIdx.x * 4 + wave_index();
+    if (item >= (int64_t)c.N * c.per_item) return;
+    const int64_t n = item / c.per_item;
+    int t = (int)(item - n * c.per_item), k = 0;
+    while (t >= c.table[k].count) t -= c.table[k++].count;
+    const AttnRanges::Table& x = c.table[k];
+    // owners t * size .. of which `group` consecutive ones are of one token
+    const int first = (int)((int64_t)t * x.size / x.group), last = (int)(min((int64_t)(t + 1) * x.size, (int64_t)x.tokens * x.group) - 1) / x.group;
+    const int* doc = x.doc + n * x.tokens;
+    int lo = 0x7fffffff, hi = -1, whole = 1;
+    for (int i = first + lane; i <= last; i += 64) {
+        const int d = doc[i];
+        if (d >= 0) {
+            lo = min(lo, d);
+            hi = max(hi, d);
+        } else {
+            whole = 0;
+        }
+    }
+#pragma unroll
+    for (int m = 32; m; m >>= 1) {
+        lo = min(lo, __shfl_xor(lo, m, 64));
+        hi = max(hi, __shfl_xor(hi, m, 64));
+        whole &= __shfl_xor(whole, m, 64);
+    }
+    if (lane == 0) x.into[n * x.count + t] = make_int4(lo, hi, whole, 0);
 }
 
 // Rows that are not whole 16-byte chunks on 16-byte boundaries, copied so that they are: [N, L, H, width] from
@@ -234,16 +249,32 @@ hipError_t launch_typed(const AttnParams& p, int waves, hipStream_t stream) {
 int attn_tile(int dtype, int waves) { return dtype == MSDA_F32 || waves == 1 ? 32 : Op<_Float16>::kTile; }
 int attn_channels(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
-AttnPlan attn_plan(int64_t slabs, int64_t own, int64_t across, int dtype, bool lone_waves) {
+AttnPlan attn_plan(const AttnParams& p, int dtype, AttnKernel kernel) {
+    const int DP = attn_channels(p.D);
+    const int64_t slabs = (int64_t)p.N * p.Mkv, own = kernel == kGradKV ? p.Lk : p.R, across = kernel == kGradKV ? p.R : p.Lk;
     AttnPlan a;
-    a.waves = lone_waves && own <= 32 ? 1 : 4;
+    a.waves = kernel == kForward && own <= 32 ? 1 : 4;
     a.tile = attn_tile(dtype, a.waves);
     a.blocks = (int)((own + 32 * a.waves - 1) / (32 * a.waves));
-    // enough waves for two on each of the 1024 SIMDs, of at least four tiles each
-    const int64_t waves = slabs * a.blocks * a.waves, tiles = (across + a.tile - 1) / a.tile;
-    int64_t splits = waves > 0 ? (2048 + waves - 1) / waves : 1;
-    if (splits > tiles / 4) splits = tiles / 4;
-    a.splits = (int)(splits < 1 ? 1 : splits > 256 ? 256 : splits);
+    const int64_t tiles = (across + a.tile - 1) / a.tile, waves = slabs * a.blocks * a.waves;
+    // Waves that the card holds at once, by the kernels' registers (a lone wave's by its LDS); twice as many keep it
+    // full while workgroups of different lengths end. With one split each, DETR-encoder self-attention over 4947
+    // pixels (2496 waves) took 203, 202 and 248 us in the three kernels, with three 123, 143 and 206.
+    const int per_simd = a.waves == 1 ? 1 : DP == 32 ? (kernel == kForward ? 4 : 3) : DP == 64 ? (kernel == kForward ? 3 : 2)
+                                                                                   : kernel == kGradKV ? 1 : 2;
+    int64_t splits = waves > 0 ? (2048 * per_simd + waves - 1) / waves : 1;
+    const bool full = waves >= 1024 * per_simd;
+    // runs shorter than this do not pay for the workgroup's start and its partial results
+    const int64_t least = full ? 16 : 4;
+    // and the partial results of all splits have to fit into half a GB
+    const int64_t split_bytes = slabs * own * DP * 4 * (kernel == kGradKV ? 2 : 1), most = ((int64_t)512 << 20) / (split_bytes + 1);
+    int64_t chunk = (tiles + splits - 1) / splits;
+    if (chunk < least) chunk = least;
+    if ((tiles + chunk - 1) / chunk > most) chunk = most > 1 ? (tiles + most - 1) / most : tiles;
+    a.chunk = (int)(chunk < 1 ? 1 : chunk);
+    a.splits = (int)((tiles + a.chunk - 1) / a.chunk);
+    if (a.splits < 1) a.splits = 1;
+    a.tiles = (int)tiles;
     return a;
 }
 
@@ -255,9 +286,9 @@ hipError_t launch_attn_pack(const AttnPack& c, int dtype, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t launch_attn_ranges(const AttnParams& p, int k_tile, int row_tile, hipStream_t stream) {
-    const int64_t items = (int64_t)p.N * (p.k_tiles + (row_tile ? p.row_tiles : 0));
-    hipLaunchKernelGGL(attn_ranges_kernel, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, stream, p, k_tile, row_tile);
+hipError_t launch_attn_ranges(const AttnRanges& c, hipStream_t stream) {
+    const int64_t items = (int64_t)c.N * c.per_item;
+    hipLaunchKernelGGL(attn_ranges_kernel, dim3((unsigned)((items + 3) / 4)), dim3(256), 0, stream, c);
     return hipGetLastError();
 }
 

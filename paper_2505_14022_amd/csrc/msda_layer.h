@@ -63,13 +63,15 @@ struct AttnParams {
     float* delta;                // [N, M, Lq]: sum over channels of grad_out * o (backward)
     const float *slopes, *q_pos, *k_pos;
     const int *q_doc, *k_doc, *prefix;
-    int4 *k_ranges, *row_ranges;  // documents of each key tile [N, k_tiles] and row tile [N, row_tiles]
-    float* part;                  // partial results of the splits, or null with one split
+    const int4 *own_ranges, *tile_ranges;  // documents of the kernel's blocks [N, blocks] and tiles [N, tiles], or null
+    float* part;                  // partial results of the splits
+    int* filled;                  // [slabs, blocks, splits]: whether a split has a partial result
     int64_t qs[3], ks[3], vs[3];  // strides in elements: batch item, token, head
     int N, Lq, Lk, M, Mkv, G, D;
     int R;                        // rows of a slab: Lq * G
     int row_width;                // elements from one row of o and grad_out to the next (D, or more where they were packed)
-    int k_tiles, row_tiles, blocks, splits;
+    int blocks, own_rows;         // workgroups of a slab's owners, and the owners of each
+    int tiles, chunk, splits;     // tiles of the other axis, in runs of `chunk` for each of `splits` workgroups
     int causal;
     float scale, softcap;
 };
@@ -83,17 +85,26 @@ struct AttnPack {
     int N, H, D, width;
 };
 
-// How a call is cut up: waves per workgroup, rows or keys per tile of the other axis, workgroups per slab and
-// splits of the other axis. Workgroups own rows (forward, grad_q) or keys (grad_k and grad_v).
+// How a kernel is cut up: waves per workgroup, rows or keys per tile of the other axis, workgroups per slab, and the
+// runs of tiles that the workgroups of a block share. Workgroups own rows (forward, grad_q) or keys (grad_k and grad_v).
+enum AttnKernel { kForward, kGradQ, kGradKV };
 struct AttnPlan {
-    int waves, tile, blocks, splits;
+    int waves = 1, tile = 32, blocks = 0, tiles = 0, splits = 1, chunk = 1;
 };
-// lone_waves: few owners may go to workgroups of one wave (the forward).
-AttnPlan attn_plan(int64_t slabs, int64_t own, int64_t across, int dtype, bool lone_waves);
+AttnPlan attn_plan(const AttnParams& p, int dtype, AttnKernel kernel);
 int attn_channels(int D);  // channels that the kernels hold: 32, 64 or 128
 hipError_t launch_attn_pack(const AttnPack& c, int dtype, hipStream_t stream);
-// The documents of tiles of k_tile keys, and of row_tile rows unless that is 0.
-hipError_t launch_attn_ranges(const AttnParams& p, int k_tile, int row_tile, hipStream_t stream);
+// The documents of runs of `size` owners (keys, or rows of `group` heads to a token) of each batch item: the smallest
+// and largest that are not padding, and whether none is.
+struct AttnRanges {
+    struct Table {
+        const int* doc;  // [N, tokens]
+        int4* into;      // [N, count]
+        int tokens, group, size, count;
+    } table[4];
+    int N, per_item;     // per_item: the counts' sum
+};
+hipError_t launch_attn_ranges(const AttnRanges& c, hipStream_t stream);
 hipError_t launch_attn_forward(const AttnParams& p, int dtype, int waves, hipStream_t stream);
 hipError_t launch_attn_grad_q(const AttnParams& p, int dtype, hipStream_t stream);
 hipError_t launch_attn_grad_kv(const AttnParams& p, int dtype, hipStream_t stream);

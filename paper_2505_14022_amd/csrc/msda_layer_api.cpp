@@ -270,11 +270,11 @@ msda_status_t check_attention(const msda_attention_t* a) {
 }
 
 // The kernels' view of a call, and how it is cut up. The workspace's pieces in order: documents of the key tiles
-// and row tiles, delta (backward), packed copies of q, k, v, out and grad_out, partial results of the splits.
+// and row tiles, delta (backward), runs per block, packed copies of q, k, v, out and grad_out, partial results of the splits.
 struct Attention {
     msda::AttnParams p = {};
-    msda::AttnPlan rows = {1, 32, 0, 1}, keys = {1, 32, 0, 1};
-    size_t at_row_ranges = 0, at_delta = 0, at_pack[5] = {0, 0, 0, 0, 0}, at_part = 0, bytes = 0;
+    msda::AttnPlan rows, keys;
+    size_t at_ranges[4] = {0, 0, 0, 0}, at_delta = 0, at_filled = 0, at_pack[5] = {0, 0, 0, 0, 0}, at_part = 0, bytes = 0;
     bool pack[5] = {false, false, false, false, false};
     int width = 0;  // of a packed row
 };
@@ -318,16 +318,23 @@ Attention attention_of(const msda_attention_t& a, bool backward) {
         p.k_doc = a.k_doc;
         p.prefix = a.prefix;
     }
-    if (a.Lq > 0) x.rows = msda::attn_plan(slabs, p.R, p.Lk, a.dtype, !backward);
-    if (backward && a.Lk > 0) x.keys = msda::attn_plan(slabs, p.Lk, p.R, a.dtype, false);
-    p.k_tiles = (int)ceil_div(a.Lk, x.rows.tile);
-    p.row_tiles = (int)ceil_div(p.R, x.keys.tile);
-    const bool docs = p.q_doc != nullptr;
-    size_t at = docs ? round_up(sizeof(int4) * a.N * p.k_tiles) : 0;
-    x.at_row_ranges = at;
-    if (docs && backward) at += round_up(sizeof(int4) * a.N * p.row_tiles);
+    if (a.Lq > 0) x.rows = msda::attn_plan(p, a.dtype, backward ? msda::kGradQ : msda::kForward);
+    if (backward && a.Lk > 0) x.keys = msda::attn_plan(p, a.dtype, msda::kGradKV);
+    // tables of documents: key tiles and row blocks of one side's kernels, row tiles and key blocks of the other's
+    const int counts[4] = {x.rows.tiles, x.rows.blocks, x.keys.tiles, x.keys.blocks};
+    size_t at = 0;
+    for (int i = 0; i < 4; ++i) {
+        x.at_ranges[i] = at;
+        if (p.q_doc) at += round_up(sizeof(int4) * a.N * counts[i]);
+    }
     x.at_delta = at;
     if (backward) at += round_up(sizeof(float) * a.N * a.M * a.Lq);
+    x.at_filled = at;
+    size_t filled = 0;
+    for (const msda::AttnPlan* plan : {&x.rows, &x.keys})
+        if (plan->splits > 1 && (size_t)slabs * plan->blocks * plan->splits > filled)
+            filled = (size_t)slabs * plan->blocks * plan->splits;
+    at += round_up(sizeof(int) * filled);
     x.width = (int)ceil_div(a.D * es, 16) * 16 / es;
     x.pack[0] = a.unaligned || !row_pieces(a.q_stride, a.N, a.Lq, a.M, G, a.D, es);
     x.pack[1] = a.unaligned || !row_pieces(a.k_stride, a.N, a.Lk, a.Mkv, 1, a.D, es);
@@ -371,9 +378,8 @@ hipError_t bind(Attention& x, const msda_attention_t& a, const void* q, const vo
                 const void* grad_out, void* workspace, hipStream_t stream) {
     msda::AttnParams& p = x.p;
     char* ws = static_cast<char*>(workspace);
-    p.k_ranges = reinterpret_cast<int4*>(ws);
-    p.row_ranges = reinterpret_cast<int4*>(ws + x.at_row_ranges);
     p.delta = reinterpret_cast<float*>(ws + x.at_delta);
+    p.filled = reinterpret_cast<int*>(ws + x.at_filled);
     p.part = reinterpret_cast<float*>(ws + x.at_part);
     p.row_width = x.pack[3] ? x.width : p.D;
     int64_t rows[3] = {a.Lq * a.M * a.D, a.M * a.D, a.D};  // of out and grad_out
@@ -409,9 +415,37 @@ hipError_t bind(Attention& x, const msda_attention_t& a, const void* q, const vo
     return hipSuccess;
 }
 
-void take_plan(msda::AttnParams& p, const msda::AttnPlan& plan) {
+// Enqueues the tables of documents.
+hipError_t find_ranges(const Attention& x, void* workspace, hipStream_t stream) {
+    const msda::AttnParams& p = x.p;
+    if (!p.q_doc) return hipSuccess;
+    const msda::AttnPlan &r = x.rows, &k = x.keys;
+    msda::AttnRanges c = {{{p.k_doc, nullptr, p.Lk, 1, r.tile, r.tiles},
+                           {p.q_doc, nullptr, p.Lq, p.G, 32 * r.waves, r.blocks},
+                           {p.q_doc, nullptr, p.Lq, p.G, k.tile, k.tiles},
+                           {p.k_doc, nullptr, p.Lk, 1, 32 * k.waves, k.blocks}}, p.N, 0};
+    for (int i = 0; i < 4; ++i) {
+        c.table[i].into = reinterpret_cast<int4*>(static_cast<char*>(workspace) + x.at_ranges[i]);
+        c.per_item += c.table[i].count;
+    }
+    return msda::launch_attn_ranges(c, stream);
+}
+
+// The parameters of the kernels that own rows, or keys.
+msda::AttnParams kernel_params(const Attention& x, bool keys, void* workspace) {
+    msda::AttnParams p = x.p;
+    const msda::AttnPlan& plan = keys ? x.keys : x.rows;
     p.blocks = plan.blocks;
+    p.own_rows = 32 * plan.waves;
+    p.tiles = plan.tiles;
     p.splits = plan.splits;
+    p.chunk = plan.chunk;
+    if (p.q_doc) {
+        const char* ws = static_cast<const char*>(workspace);
+        p.tile_ranges = reinterpret_cast<const int4*>(ws + x.at_ranges[keys ? 2 : 0]);
+        p.own_ranges = reinterpret_cast<const int4*>(ws + x.at_ranges[keys ? 3 : 1]);
+    }
+    return p;
 }
 
 }  // namespace
@@ -442,9 +476,9 @@ msda_status_t msda_attention_forward(const msda_attention_t* a, const void* q, c
     hipError_t e = bind(x, *a, q, k, v, nullptr, nullptr, workspace, (hipStream_t)stream);
     x.p.out = out;
     x.p.lse = lse;
-    take_plan(x.p, x.rows);
-    if (e == hipSuccess && x.p.q_doc) e = msda::launch_attn_ranges(x.p, x.rows.tile, 0, (hipStream_t)stream);
-    if (e == hipSuccess) e = msda::launch_attn_forward(x.p, a->dtype, x.rows.waves, (hipStream_t)stream);
+    if (e == hipSuccess) e = find_ranges(x, workspace, (hipStream_t)stream);
+    if (e == hipSuccess)
+        e = msda::launch_attn_forward(kernel_params(x, false, workspace), a->dtype, x.rows.waves, (hipStream_t)stream);
     if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "attention launch: %s", hipGetErrorString(e));
     return ok();
 }
@@ -470,16 +504,11 @@ msda_status_t msda_attention_backward(const msda_attention_t* a, const void* q, 
     x.p.grad_q = grad_q;
     x.p.grad_k = grad_k;
     x.p.grad_v = grad_v;
-    if (e == hipSuccess && x.p.q_doc)
-        e = msda::launch_attn_ranges(x.p, x.rows.tile, x.keys.tile, (hipStream_t)stream);
-    if (e == hipSuccess && a->Lq > 0) {  // writes delta, which grad_k and grad_v need
-        take_plan(x.p, x.rows);
-        e = msda::launch_attn_grad_q(x.p, a->dtype, (hipStream_t)stream);
-    }
-    if (e == hipSuccess && a->Lk > 0) {
-        take_plan(x.p, x.keys);
-        e = msda::launch_attn_grad_kv(x.p, a->dtype, (hipStream_t)stream);
-    }
+    if (e == hipSuccess) e = find_ranges(x, workspace, (hipStream_t)stream);
+    if (e == hipSuccess && a->Lq > 0)  // writes delta, which grad_k and grad_v need
+        e = msda::launch_attn_grad_q(kernel_params(x, false, workspace), a->dtype, (hipStream_t)stream);
+    if (e == hipSuccess && a->Lk > 0)
+        e = msda::launch_attn_grad_kv(kernel_params(x, true, workspace), a->dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "attention backward launch: %s", hipGetErrorString(e));
     return ok();
 }
