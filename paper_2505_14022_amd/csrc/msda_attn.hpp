@@ -254,12 +254,15 @@ __device__ __forceinline__ void add_product(acc_t (&acc)[DP / 32], const acc_t& 
     }
 }
 
-// s + 32 rows of a tile times the owner's fragments.
+// s + 32 rows of a tile times the owner's fragments, of D channels.
 template <typename T, int DP>
-__device__ __forceinline__ acc_t row_product(const T* tile, int stride, const typename Op<T>::Frag* own, int lane,
+__device__ __forceinline__ acc_t row_product(const T* tile, int stride, const typename Op<T>::Frag* own, int lane, int D,
                                              acc_t s) {
 #pragma unroll
-    for (int c = 0; c < DP / Op<T>::K; ++c) s = Op<T>::mma(row_frag(tile + (lane & 31) * stride, c, lane), own[c], s);
+    for (int c = 0; c < DP / Op<T>::K; ++c) {
+        if (sizeof(T) == 2 || c * Op<T>::K < D)  // in fp32 a chunk beyond D is 256 cycles of products of zeros
+            s = Op<T>::mma(row_frag(tile + (lane & 31) * stride, c, lane), own[c], s);
+    }
     return s;
 }
 

@@ -72,8 +72,8 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
 #pragma unroll
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
             const T* kt = sh.k[b] + kb * 32 * Tile::kStride;
-            acc_t s = row_product<T, DP>(kt, Tile::kStride, q, lane, acc_t{});
-            acc_t ds = row_product<T, DP>(sh.v[b] + kb * 32 * Tile::kStride, Tile::kStride, go, lane, minus_delta);
+            acc_t s = row_product<T, DP>(kt, Tile::kStride, q, lane, p.D, acc_t{});
+            acc_t ds = row_product<T, DP>(sh.v[b] + kb * 32 * Tile::kStride, Tile::kStride, go, lane, p.D, minus_delta);
             float unit = p.scale * kLog2e;
             if constexpr (EXTRAS) {
                 unit = cap_scores<T>(p, s, &ds);
@@ -263,7 +263,8 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     odd_k.start(odd_words[0], wave * 32 + (lane & 31), lane, masks);
     odd_v.start(odd_words[1], wave * 32 + (lane & 31), lane, masks);
     fetch();
-    for (int b = 0; t >= 0; b ^= 1) {
+    for (int b = 0; ; b ^= 1) {
+        if (t < 0) break;
         stage(b);
         // rows past the last have p = 0, keys past the last are not written
         const int r0 = t * Tile::kRows;
@@ -279,8 +280,8 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             acc_t ds;  // the sums of dP begin at -delta
 #pragma unroll
             for (int r = 0; r < 16; ++r) ds[r] = s_delta[b][rb * 32 + block_row(r, h)];
-            acc_t s = row_product<T, DP>(qt, Tile::kStride, k, lane, acc_t{});
-            ds = row_product<T, DP>(gt, Tile::kStride, v, lane, ds);
+            acc_t s = row_product<T, DP>(qt, Tile::kStride, k, lane, p.D, acc_t{});
+            ds = row_product<T, DP>(gt, Tile::kStride, v, lane, p.D, ds);
             float unit = p.scale * kLog2e;
             if constexpr (EXTRAS) {
                 unit = cap_scores<T>(p, s, &ds);
@@ -370,13 +371,13 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(AttnParams p) {
     const float* part = p.part + at * p.splits * (kLanes * 4) + e0;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = 0; s < p.splits; ++s) {
-        if (!filled[s]) continue;
+    for (int s = 0; s < p.splits; ++s) {  // loads do not wait for one another: what is not filled is dropped
+        const bool full = filled[s];
         const float4 y = *reinterpret_cast<const float4*>(part + (int64_t)s * (kLanes * 4));
-        x[0] += y.x;
-        x[1] += y.y;
-        x[2] += y.z;
-        x[3] += y.w;
+        x[0] += full ? y.x : 0.f;
+        x[1] += full ? y.y : 0.f;
+        x[2] += full ? y.z : 0.f;
+        x[3] += full ? y.w : 0.f;
     }
     const bool values = KV && e0 >= DP;
     T* out;

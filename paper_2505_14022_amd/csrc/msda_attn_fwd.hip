@@ -12,7 +12,7 @@ namespace msda {
 namespace {
 
 // Waves per SIMD that the registers of a kernel that owns rows have to leave room for.
-constexpr int row_waves(int DP, int NW) { return NW == 1 ? (DP == 128 ? 1 : 2) : DP == 32 ? 4 : DP == 64 ? 3 : 2; }
+constexpr int row_waves(int DP, int NW) { return NW == 1 ? (DP > 32 ? 1 : 2) : DP == 32 ? 4 : DP == 64 ? 3 : 2; }
 
 template <typename T, int DP, int NW, bool EXTRAS>
 __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(AttnParams p) {
@@ -51,7 +51,7 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
         float unit = p.scale * kLog2e;  // of the raw scores, left to the exponent where nothing comes between
 #pragma unroll
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
-            s[kb] = row_product<T, DP>(sh.k[b] + kb * 32 * Tile::kStride, Tile::kStride, q, lane, acc_t{});
+            s[kb] = row_product<T, DP>(sh.k[b] + kb * 32 * Tile::kStride, Tile::kStride, q, lane, p.D, acc_t{});
             if constexpr (EXTRAS) {
                 unit = cap_scores<T>(p, s[kb], nullptr);
                 if (p.slopes) {
@@ -133,44 +133,53 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
     if (p.lse && h == 0) p.lse[own.stat] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Joins the splits of a row: DP / 4 lanes per row, four channels each.
+// Joins the splits of a row: DP / 4 lanes of four channels each, times `groups` (a power of two, a wave holds whole
+// rows) to which the splits are dealt. Loads do not wait for one another: what a split that is not filled holds
+// is dropped.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p) {
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p, int groups) {
     constexpr int kLanes = DP / 4;
     const int64_t rows = (int64_t)p.N * p.Mkv * p.R;
-    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / (kLanes * groups);
     if (at >= rows) return;
     const int64_t slab = at / p.R;
-    const int row = (int)(at - slab * p.R), i = row / p.G;
+    const int lane = threadIdx.x % (kLanes * groups), row = (int)(at - slab * p.R), i = row / p.G;
     const int* filled = p.filled + (slab * p.blocks + row / p.own_rows) * p.splits;
-    const int d = (threadIdx.x % kLanes) * 4;
+    const int d = lane % kLanes * 4;
     const float2* stats = reinterpret_cast<const float2*>(p.part + rows * p.splits * DP) + at * p.splits;
     const float* part = p.part + at * p.splits * DP + d;
-    float top = -kInf, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+    float m = -kInf, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+    auto take = [&](float m2, float l2, const float (&y)[4]) {
+        const float top = fmaxf(m, m2), base = top == -kInf ? 0.f : top;
+        const float u = exp2_of(m - base), w = exp2_of(m2 - base);
+        m = top;
+        l = l * u + l2 * w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = x[e] * u + y[e] * w;
+    };
 #pragma unroll 4
-    for (int s = 0; s < p.splits; ++s)
-        if (filled[s]) top = fmaxf(top, stats[s].x);
-    const float base = top == -kInf ? 0.f : top;
-#pragma unroll 4
-    for (int s = 0; s < p.splits; ++s) {
-        if (!filled[s]) continue;
+    for (int s = lane / kLanes; s < p.splits; s += groups) {
+        const bool full = filled[s];
         const float2 ml = stats[s];
-        const float w = exp2_of(ml.x - base);
-        const float4 y = *reinterpret_cast<const float4*>(part + (int64_t)s * DP);
-        l += w * ml.y;
-        x[0] += w * y.x;
-        x[1] += w * y.y;
-        x[2] += w * y.z;
-        x[3] += w * y.w;
+        const float4 y4 = *reinterpret_cast<const float4*>(part + (int64_t)s * DP);
+        const float y[4] = {full ? y4.x : 0.f, full ? y4.y : 0.f, full ? y4.z : 0.f, full ? y4.w : 0.f};
+        take(full ? ml.x : -kInf, full ? ml.y : 0.f, y);
     }
+    for (int k = kLanes; k < kLanes * groups; k *= 2) {
+        float y[4];
+        const float m2 = __shfl_xor(m, k, 64), l2 = __shfl_xor(l, k, 64);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = __shfl_xor(x[e], k, 64);
+        take(m2, l2, y);
+    }
+    if (lane >= kLanes) return;
     const int64_t n = slab / p.Mkv;
     const int head = (int)(slab - n * p.Mkv) * p.G + row - i * p.G;
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] *= inv;
     store_four(static_cast<T*>(p.out) + ((n * p.Lq + i) * p.M + head) * p.D, d, p.D, x);
-    if (p.lse && d == 0)
-        p.lse[(n * p.M + head) * p.Lq + i] = l == 0.f ? -kInf : (top + __builtin_amdgcn_logf(l)) * kLn2;
+    if (p.lse && d == 0) p.lse[(n * p.M + head) * p.Lq + i] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // Documents of the tiles and blocks of each table of a call, one wave for each.
@@ -238,8 +247,10 @@ hipError_t launch_typed(const AttnParams& p, int waves, hipStream_t stream) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.splits == 1) return e;
         const int64_t rows = (int64_t)p.N * p.Mkv * p.R;
-        hipLaunchKernelGGL((attn_join_kernel<T, DP>), dim3((unsigned)((rows * (DP / 4) + 255) / 256)), dim3(256), 0,
-                           stream, p);
+        int groups = 1;  // at most four splits to a lane, where a wave has the lanes
+        while (groups < 256 / DP && groups * 4 < p.splits) groups *= 2;
+        hipLaunchKernelGGL((attn_join_kernel<T, DP>), dim3((unsigned)((rows * (DP / 4 * groups) + 255) / 256)), dim3(256),
+                           0, stream, p, groups);
         return hipGetLastError();
     });
 }
@@ -257,13 +268,14 @@ AttnPlan attn_plan(const AttnParams& p, int dtype, AttnKernel kernel) {
     a.tile = attn_tile(dtype, a.waves);
     a.blocks = (int)((own + 32 * a.waves - 1) / (32 * a.waves));
     const int64_t tiles = (across + a.tile - 1) / a.tile, waves = slabs * a.blocks * a.waves;
-    // Waves that the card holds at once, by the kernels' registers (a lone wave's by its LDS); twice as many keep it
-    // full while workgroups of different lengths end. With one split each, DETR-encoder self-attention over 4947
+    // Waves that the card holds at once, by the kernels' registers (a lone wave's by its LDS), where one split's are few;
+    // twice as many keep it full while the last workgroups end. With one split each, DETR-encoder self-attention over 4947
     // pixels (2496 waves) took 203, 202 and 248 us in the three kernels, with three 123, 143 and 206.
     const int per_simd = a.waves == 1 ? 1 : DP == 32 ? (kernel == kForward ? 4 : 3) : DP == 64 ? (kernel == kForward ? 3 : 2)
                                                                                    : kernel == kGradKV ? 1 : 2;
-    int64_t splits = waves > 0 ? (2048 * per_simd + waves - 1) / waves : 1;
-    const bool full = waves >= 1024 * per_simd;
+    const int64_t room = 1024 * per_simd;
+    int64_t splits = waves > 0 ? ((4 * waves < room ? 1 : 2) * room + waves - 1) / waves : 1;
+    const bool full = waves >= room;
     // runs shorter than this do not pay for the workgroup's start and its partial results
     const int64_t least = full ? 16 : 4;
     // and the partial results of all splits have to fit into half a GB

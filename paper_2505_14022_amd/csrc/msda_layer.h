@@ -30,6 +30,7 @@ struct NormParams {
     int C, blocks;
     float eps;
     bool vec;                   // rows are whole 16-byte pieces, 16-byte aligned
+    bool columns;               // weight and bias are 16-byte aligned
 };
 
 // Workgroups of the backward kernel, each with a row of partial sums.

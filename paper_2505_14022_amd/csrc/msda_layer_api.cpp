@@ -76,6 +76,7 @@ msda_status_t msda_layernorm_forward(const void* x, const void* residual, const 
     p.C = (int)C;
     p.eps = eps;
     p.vec = norm_pieces(C, dtype, x, residual, (const void*)out, (const void*)sum);
+    p.columns = is_aligned(weight, 16) && is_aligned(bias, 16);
     hipError_t e = msda::launch_layernorm_forward(p, dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "layer norm launch: %s", hipGetErrorString(e));
     return ok();
@@ -129,6 +130,7 @@ msda_status_t msda_layernorm_backward(const void* x, const void* residual, const
     p.C = (int)C;
     p.blocks = msda::norm_backward_blocks(rows, C, dtype);
     p.vec = norm_pieces(C, dtype, x, residual, grad_out, grad_sum, (const void*)grad_x);
+    p.columns = is_aligned(weight, 16);
     hipError_t e = msda::launch_layernorm_backward(p, dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "layer norm backward launch: %s", hipGetErrorString(e));
     return ok();

@@ -39,6 +39,31 @@ __device__ __forceinline__ void row_sums(float (&x)[NX], float* red) {
     }
 }
 
+// The lane's columns of weight or bias (`none` without one), in 16-byte pieces if `pieces`.
+template <int VEC, int G, int NV>
+__device__ __forceinline__ void load_columns(float (&w)[NV][VEC], const float* from, float none, int g, int C, bool pieces) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * G + g) * VEC;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) w[j][i] = none;
+        if (!from || c >= C) continue;
+        if (VEC % 4 == 0 && pieces) {
+#pragma unroll
+            for (int i = 0; i + 3 < VEC; i += 4) {
+                const float4 x = *reinterpret_cast<const float4*>(from + c + i);
+                w[j][i] = x.x;
+                w[j][i + 1] = x.y;
+                w[j][i + 2] = x.z;
+                w[j][i + 3] = x.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[j][i] = from[c + i];
+        }
+    }
+}
+
 template <typename T, int VEC, int NT, int G, int NV>
 __global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
     __shared__ float red[NT / 64];
@@ -46,37 +71,41 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
     const int C = p.C;
     const float inv_c = 1.f / (float)C;
     float w[NV][VEC], b[NV][VEC];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int c = (j * G + g) * VEC;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            w[j][i] = p.weight && c + i < C ? p.weight[c + i] : 1.f;
-            b[j][i] = p.bias && c + i < C ? p.bias[c + i] : 0.f;
-        }
-    }
+    load_columns<VEC, G, NV>(w, p.weight, 1.f, g, C, p.columns);
+    load_columns<VEC, G, NV>(b, p.bias, 0.f, g, C, p.columns);
     const T* x = static_cast<const T*>(p.x);
     const T* r = static_cast<const T*>(p.residual);
-    for (int64_t row = (int64_t)blockIdx.x * (NT / G) + threadIdx.x / G; row < p.rows;
-         row += (int64_t)gridDim.x * (NT / G)) {
+    const int64_t step = (int64_t)gridDim.x * (NT / G);
+    int64_t row = (int64_t)blockIdx.x * (NT / G) + threadIdx.x / G;
+    // the next row's pieces are on their way while a row is reduced
+    Piece<T, VEC> nx[NV], nr[NV];
+    auto fetch = [&](int64_t of) {
+        if (of >= p.rows) return;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * G + g) * VEC;
+            if (c < C) {
+                nx[j] = *reinterpret_cast<const Piece<T, VEC>*>(x + of * C + c);
+                if (r) nr[j] = *reinterpret_cast<const Piece<T, VEC>*>(r + of * C + c);
+            }
+        }
+    };
+    fetch(row);
+    for (; row < p.rows; row += step) {
         const int64_t at = row * C;
         float s[NV][VEC];
         float sum[1] = {0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * G + g) * VEC;
-            if (c < C) {
-                load_piece(s[j], x + at + c);
-                if (r) {
-                    float y[VEC];
-                    load_piece(y, r + at + c);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) s[j][i] += y[i];
-                }
+            for (int i = 0; i < VEC; ++i) s[j][i] = (float)nx[j].v[i] + (r ? (float)nr[j].v[i] : 0.f);
+            if (c < C) {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) sum[0] += s[j][i];
             }
         }
+        fetch(row + step);
         row_sums<NT, G>(sum, red);
         const float mean = sum[0] * inv_c;
         float sq[1] = {0.f};
@@ -119,15 +148,11 @@ __global__ __launch_bounds__(NT) void norm_bwd_kernel(NormParams p) {
     const int C = p.C;
     const float inv_c = 1.f / (float)C;
     float w[NV][VEC], gw[NV][VEC], gb[NV][VEC];
+    load_columns<VEC, G, NV>(w, p.weight, 1.f, g, C, p.columns);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int c = (j * G + g) * VEC;
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            w[j][i] = p.weight && c + i < C ? p.weight[c + i] : 1.f;
-            gw[j][i] = gb[j][i] = 0.f;
-        }
-    }
+        for (int i = 0; i < VEC; ++i) gw[j][i] = gb[j][i] = 0.f;
     const T* x = static_cast<const T*>(p.x);
     const T* r = static_cast<const T*>(p.residual);
     const T* go = static_cast<const T*>(p.grad_out);
@@ -218,8 +243,10 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float* partial, fl
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
     const float* col = partial + (int64_t)blockIdx.y * blocks * C + c;
     float t = 0.f;
-    if (c < C)
+    if (c < C) {
+#pragma unroll 8
         for (int b = k; b < blocks; b += 32) t += col[(int64_t)b * C];
+    }
     s[k][threadIdx.x & 31] = t;
     __syncthreads();
     if (k == 0 && c < C) {

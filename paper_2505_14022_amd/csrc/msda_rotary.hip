@@ -49,11 +49,81 @@ Div16 make_div16(int d) { return {(uint32_t)((((uint64_t)1 << 32) + d - 1) / d),
 
 // VEC pairs per item (two 16-byte pieces), or one. An item of a head beyond the pairs copies VEC channels.
 template <typename T, int VEC>
+struct Item {
+    int64_t from, to;  // of its head's first channel
+    int c0, c1, pair;  // first channels of its pieces (c1 < 0: one piece, copied), and its first pair in LDS
+    Piece<T, VEC> u, v;
+};
+
+template <typename T, int VEC>
+__device__ __forceinline__ void take_item(const RotaryParams& p, Item<T, VEC>& it, const T* x, int i, Div16 per_token, Div16 items) {
+    const int t = div16(i, per_token), j = i - t * per_token.d;
+    const int m = div16(j, items), k = j - m * items.d;
+    const int r = k * VEC;
+    it.from = t * p.xs[1] + m * p.xs[2];
+    it.to = t * p.os[1] + m * p.os[2];
+    it.pair = t * p.R + r;
+    if (r >= p.R) {
+        it.c0 = p.R + r;  // 2R + the channels of the copying items before
+        it.c1 = -1;
+    } else {
+        it.c0 = p.interleaved ? 2 * r : r;
+        it.c1 = p.interleaved ? 2 * r + VEC : p.R + r;
+        it.v = *reinterpret_cast<const Piece<T, VEC>*>(x + it.from + it.c1);
+    }
+    it.u = *reinterpret_cast<const Piece<T, VEC>*>(x + it.from + it.c0);
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ void turn_item(const RotaryParams& p, const Item<T, VEC>& it, T* out, const float* s_cos, const float* s_sin) {
+    float u[VEC], v[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        u[j] = (float)it.u.v[j];
+        v[j] = (float)it.v.v[j];
+    }
+    T* to = out + it.to;
+    if (it.c1 < 0) {
+        store_piece(to + it.c0, u);
+        return;
+    }
+    const float* cs = s_cos + it.pair;
+    const float* sn = s_sin + it.pair;
+    if (VEC > 1 && p.interleaved) {
+        // u and v are the item's first VEC / 2 pairs and its others
+#pragma unroll
+        for (int j = 0; j < VEC / 2; ++j) {
+            const float a = u[2 * j], b = u[2 * j + 1];
+            u[2 * j] = a * cs[j] - b * sn[j];
+            u[2 * j + 1] = a * sn[j] + b * cs[j];
+            const float d = v[2 * j], e = v[2 * j + 1];
+            v[2 * j] = d * cs[VEC / 2 + j] - e * sn[VEC / 2 + j];
+            v[2 * j + 1] = d * sn[VEC / 2 + j] + e * cs[VEC / 2 + j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float a = u[j], b = v[j];
+            u[j] = a * cs[j] - b * sn[j];
+            v[j] = a * sn[j] + b * cs[j];
+        }
+    }
+    store_piece(to + it.c0, u);
+    store_piece(to + it.c1, v);
+}
+
+// A thread's first item is on its way while the workgroup forms the cosines and sines.
+template <typename T, int VEC>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p, int tokens, Div16 per_token, Div16 items) {
     __shared__ float s_cos[kPairs], s_sin[kPairs];
     const int64_t t0 = (int64_t)blockIdx.x * tokens;
     const int n = blockIdx.y;
     const int nt = (int)(p.T - t0 < tokens ? p.T - t0 : tokens);
+    const T* x = static_cast<const T*>(p.x) + n * p.xs[0] + t0 * p.xs[1];
+    T* out = static_cast<T*>(p.out) + n * p.os[0] + t0 * p.os[1];
+    const int count = nt * per_token.d;  // at most 2^16
+    Item<T, VEC> first;
+    if ((int)threadIdx.x < count) take_item(p, first, x, threadIdx.x, per_token, items);
     const float* pos = p.pos + n * p.pos_item + t0 * p.A;
     for (int i = threadIdx.x; i < nt * p.R; i += 256) {
         const int t = i / p.R, r = i - t * p.R;
@@ -65,57 +135,19 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p, int tokens,
         s_sin[i] = p.sign * s;
     }
     __syncthreads();
-    const T* x = static_cast<const T*>(p.x) + n * p.xs[0] + t0 * p.xs[1];
-    T* out = static_cast<T*>(p.out) + n * p.os[0] + t0 * p.os[1];
-    const int pair_items = p.R / VEC;
-    for (int i = threadIdx.x; i < nt * per_token.d; i += 256) {  // at most 2^16 items
-        const int t = div16(i, per_token), j = i - t * per_token.d;
-        const int m = div16(j, items), k = j - m * items.d;
-        const T* xr = x + t * p.xs[1] + m * p.xs[2];
-        T* yr = out + t * p.os[1] + m * p.os[2];
-        if (k >= pair_items) {
-            const int c = 2 * p.R + (k - pair_items) * VEC;
-            float v[VEC];
-            load_piece(v, xr + c);
-            store_piece(yr + c, v);
-            continue;
-        }
-        const int r = k * VEC;
-        const int c0 = p.interleaved ? 2 * r : r, c1 = p.interleaved ? 2 * r + VEC : p.R + r;
-        float u[VEC], v[VEC];
-        load_piece(u, xr + c0);
-        load_piece(v, xr + c1);
-        const float* cs = s_cos + t * p.R + r;
-        const float* sn = s_sin + t * p.R + r;
-        if (VEC > 1 && p.interleaved) {
-            // u and v are pairs r .. r + VEC / 2 - 1 and the VEC / 2 after them
-#pragma unroll
-            for (int j = 0; j < VEC / 2; ++j) {
-                const float a = u[2 * j], b = u[2 * j + 1];
-                u[2 * j] = a * cs[j] - b * sn[j];
-                u[2 * j + 1] = a * sn[j] + b * cs[j];
-                const float d = v[2 * j], e = v[2 * j + 1];
-                v[2 * j] = d * cs[VEC / 2 + j] - e * sn[VEC / 2 + j];
-                v[2 * j + 1] = d * sn[VEC / 2 + j] + e * cs[VEC / 2 + j];
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float a = u[j], b = v[j];
-                u[j] = a * cs[j] - b * sn[j];
-                v[j] = a * sn[j] + b * cs[j];
-            }
-        }
-        store_piece(yr + c0, u);
-        store_piece(yr + c1, v);
+    if ((int)threadIdx.x < count) turn_item(p, first, out, s_cos, s_sin);
+    for (int i = threadIdx.x + 256; i < count; i += 256) {
+        Item<T, VEC> it;
+        take_item(p, it, x, i, per_token, items);
+        turn_item(p, it, out, s_cos, s_sin);
     }
 }
 
 template <typename T, int VEC>
 hipError_t launch_typed(const RotaryParams& p, hipStream_t stream) {
     const int items = p.R / VEC + (p.D - 2 * p.R) / VEC;
-    // tokens per workgroup: about four items a thread, as many pairs as LDS holds, and enough workgroups
-    int tokens = 1024 / (items * p.M);
+    // tokens per workgroup: about one item a thread, as many pairs as LDS holds, and enough workgroups
+    int tokens = 256 / (items * p.M);
     if (p.R > 0 && tokens > kPairs / p.R) tokens = kPairs / p.R;
     if (tokens < 1) tokens = 1;
     while (tokens > 1 && (p.T + tokens - 1) / tokens * p.N < 1024) tokens = (tokens + 1) / 2;
