@@ -21,19 +21,13 @@ __device__ __forceinline__ void load_piece(float (&f)[VEC], const T* p) {
     for (int i = 0; i < VEC; ++i) f[i] = (float)x.v[i];
 }
 
-// Elements are rounded to nearest-even.
+// Elements are rounded to nearest-even. For waves that store whole cache lines: a streaming store that leaves lines in
+// part goes to memory in parts.
 template <typename T, int VEC>
-__device__ __forceinline__ Piece<T, VEC> to_piece(const float (&f)[VEC]) {
+__device__ __forceinline__ void store_piece(T* p, const float (&f)[VEC]) {
     Piece<T, VEC> x;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) x.v[i] = (T)f[i];
-    return x;
-}
-
-// For waves that store whole cache lines: a streaming store that leaves lines in part goes to memory in parts.
-template <typename T, int VEC>
-__device__ __forceinline__ void store_piece(T* p, const float (&f)[VEC]) {
-    const Piece<T, VEC> x = to_piece<T>(f);
     if constexpr (sizeof(x) == 16) stream_store(reinterpret_cast<uint4*>(p), __builtin_bit_cast(uint4, x));
     else *reinterpret_cast<Piece<T, VEC>*>(p) = x;
 }

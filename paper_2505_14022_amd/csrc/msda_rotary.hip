@@ -47,87 +47,8 @@ __device__ __forceinline__ int div16(int n, Div16 v) {
 }
 Div16 make_div16(int d) { return {(uint32_t)((((uint64_t)1 << 32) + d - 1) / d), d}; }
 
-// VEC pairs per item (two 16-byte pieces), or one. An item of a head beyond the pairs copies VEC channels.
-template <typename T, int VEC>
-struct Item {
-    int64_t from, to;  // of its head's first channel
-    int c0, c1, pair;  // first channels of its pieces (c1 < 0: one piece, copied), and its first pair in LDS
-    Piece<T, VEC> u, v;
-};
-
-template <typename T, int VEC>
-__device__ __forceinline__ void take_item(const RotaryParams& p, Item<T, VEC>& it, const T* x, int i, Div16 per_token, Div16 items) {
-    const int t = div16(i, per_token), j = i - t * per_token.d;
-    const int m = div16(j, items), k = j - m * items.d;
-    const int r = k * VEC;
-    it.from = t * p.xs[1] + m * p.xs[2];
-    it.to = t * p.os[1] + m * p.os[2];
-    it.pair = t * p.R + r;
-    if (r >= p.R) {
-        it.c0 = p.R + r;  // 2R + the channels of the copying items before
-        it.c1 = -1;
-    } else {
-        it.c0 = p.interleaved ? 2 * r : r;
-        it.c1 = p.interleaved ? 2 * r + VEC : p.R + r;
-        it.v = *reinterpret_cast<const Piece<T, VEC>*>(x + it.from + it.c1);
-    }
-    it.u = *reinterpret_cast<const Piece<T, VEC>*>(x + it.from + it.c0);
-}
-
-template <typename T, int VEC>
-__device__ __forceinline__ void turn_item(const RotaryParams& p, const Item<T, VEC>& it, T* out, const float* s_cos, const float* s_sin) {
-    float u[VEC], v[VEC];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-        u[j] = (float)it.u.v[j];
-        v[j] = (float)it.v.v[j];
-    }
-    // plain stores: a wave writes every other 16 or 32 bytes, and the rest of the lines with its next store (streaming
-    // stores took 83 us in place of 65 for 8 x 40000 tokens of 8 x 32 channels in bf16)
-    auto put = [](T* to, const float (&f)[VEC]) { *reinterpret_cast<Piece<T, VEC>*>(to) = to_piece<T>(f); };
-    T* to = out + it.to;
-    if (it.c1 < 0) {
-        put(to + it.c0, u);
-        return;
-    }
-    const float* cs = s_cos + it.pair;
-    const float* sn = s_sin + it.pair;
-    if (VEC > 1 && p.interleaved) {
-        // u and v are the item's first VEC / 2 pairs and its others
-#pragma unroll
-        for (int j = 0; j < VEC / 2; ++j) {
-            const float a = u[2 * j], b = u[2 * j + 1];
-            u[2 * j] = a * cs[j] - b * sn[j];
-            u[2 * j + 1] = a * sn[j] + b * cs[j];
-            const float d = v[2 * j], e = v[2 * j + 1];
-            v[2 * j] = d * cs[VEC / 2 + j] - e * sn[VEC / 2 + j];
-            v[2 * j + 1] = d * sn[VEC / 2 + j] + e * cs[VEC / 2 + j];
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const float a = u[j], b = v[j];
-            u[j] = a * cs[j] - b * sn[j];
-            v[j] = a * sn[j] + b * cs[j];
-        }
-    }
-    put(to + it.c0, u);
-    put(to + it.c1, v);
-}
-
-// A thread's first item is on its way while the workgroup forms the cosines and sines.
-template <typename T, int VEC>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p, int tokens, Div16 per_token, Div16 items) {
-    __shared__ float s_cos[kPairs], s_sin[kPairs];
-    const int64_t t0 = (int64_t)blockIdx.x * tokens;
-    const int n = blockIdx.y;
-    const int nt = (int)(p.T - t0 < tokens ? p.T - t0 : tokens);
-    const T* x = static_cast<const T*>(p.x) + n * p.xs[0] + t0 * p.xs[1];
-    T* out = static_cast<T*>(p.out) + n * p.os[0] + t0 * p.os[1];
-    const int count = nt * per_token.d;  // at most 2^16
-    Item<T, VEC> first;
-    if ((int)threadIdx.x < count) take_item(p, first, x, threadIdx.x, per_token, items);
-    const float* pos = p.pos + n * p.pos_item + t0 * p.A;
+// The cosines and sines of the workgroup's tokens, into LDS.
+__device__ __forceinline__ void form_angles(const RotaryParams& p, const float* pos, int nt, float* s_cos, float* s_sin) {
     for (int i = threadIdx.x; i < nt * p.R; i += 256) {
         const int t = i / p.R, r = i - t * p.R;
         double turns = 0.0;
@@ -137,20 +58,90 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p, int tokens,
         s_cos[i] = c;
         s_sin[i] = p.sign * s;
     }
+}
+
+// Heads of whole 16-byte pieces: a thread writes one piece at a time, so that a wave's stores are whole cache lines.
+// With the pairs in halves it reads its piece's partner too, which a neighbour's read brings into the cache. (Both
+// pieces of a pair in one thread: its stores are every other 32 bytes of a head of 32 channels, and both passes over
+// 8 x 40000 x 8 x 32 in bf16 take 165 us, 170 to 176 with more loads ahead, in place of 134.)
+// In place, a piece is read by two threads before either writes: each turn takes whole heads, and the barrier is between.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void rotary_pieces_kernel(RotaryParams p, int tokens, Div16 per_token, Div16 per_head) {
+    __shared__ float s_cos[kPairs], s_sin[kPairs];
+    const int64_t t0 = (int64_t)blockIdx.x * tokens;
+    const int n = blockIdx.y, nt = (int)(p.T - t0 < tokens ? p.T - t0 : tokens);
+    const T* x = static_cast<const T*>(p.x) + n * p.xs[0] + t0 * p.xs[1];
+    T* out = static_cast<T*>(p.out) + n * p.os[0] + t0 * p.os[1];
+    const int count = nt * per_token.d;              // at most 2^16
+    const int width = 256 / per_head.d * per_head.d; // pieces of whole heads that 256 threads take
+    const int half = p.R / VEC, turned = 2 * half;   // pieces of a head from a pair's one channel to the other, and all turned
+    for (int base = 0; base < count; base += width) {
+        const int i = base + threadIdx.x;
+        const bool mine = (int)threadIdx.x < width && i < count;
+        const int t = div16(i, per_token), j = i - t * per_token.d, m = div16(j, per_head), k = j - m * per_head.d;
+        const bool beside = p.interleaved, lower = k < half;
+        const int pair = t * p.R + (beside ? k * (VEC / 2) : (lower ? k : k - half) * VEC);
+        Piece<T, VEC> u, v;
+        if (mine) {
+            const T* from = x + t * p.xs[1] + m * p.xs[2] + k * VEC;
+            u = *reinterpret_cast<const Piece<T, VEC>*>(from);
+            if (!beside && k < turned) v = *reinterpret_cast<const Piece<T, VEC>*>(from + (lower ? half : -half) * VEC);
+        }
+        // the first pieces are on their way meanwhile
+        if (base == 0) form_angles(p, p.pos + n * p.pos_item + t0 * p.A, nt, s_cos, s_sin);
+        __syncthreads();
+        if (!mine) continue;
+        float y[VEC];
+        if (k >= turned) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) y[e] = (float)u.v[e];
+        } else if (beside) {
+#pragma unroll
+            for (int e = 0; e < VEC / 2; ++e) {
+                const float a = (float)u.v[2 * e], b = (float)u.v[2 * e + 1], c = s_cos[pair + e], s = s_sin[pair + e];
+                y[2 * e] = a * c - b * s;
+                y[2 * e + 1] = a * s + b * c;
+            }
+        } else {
+            const float sign = lower ? -1.f : 1.f;  // a c - b s, and b c + a s
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                y[e] = (float)u.v[e] * s_cos[pair + e] + sign * ((float)v.v[e] * s_sin[pair + e]);
+        }
+        store_piece(out + t * p.os[1] + m * p.os[2] + k * VEC, y);
+    }
+}
+
+// Other heads: a thread turns one pair at a time, or copies one channel.
+template <typename T>
+__global__ __launch_bounds__(256) void rotary_pairs_kernel(RotaryParams p, int tokens, Div16 per_token, Div16 per_head) {
+    __shared__ float s_cos[kPairs], s_sin[kPairs];
+    const int64_t t0 = (int64_t)blockIdx.x * tokens;
+    const int n = blockIdx.y, nt = (int)(p.T - t0 < tokens ? p.T - t0 : tokens);
+    form_angles(p, p.pos + n * p.pos_item + t0 * p.A, nt, s_cos, s_sin);
     __syncthreads();
-    if ((int)threadIdx.x < count) turn_item(p, first, out, s_cos, s_sin);
-    for (int i = threadIdx.x + 256; i < count; i += 256) {
-        Item<T, VEC> it;
-        take_item(p, it, x, i, per_token, items);
-        turn_item(p, it, out, s_cos, s_sin);
+    const T* x = static_cast<const T*>(p.x) + n * p.xs[0] + t0 * p.xs[1];
+    T* out = static_cast<T*>(p.out) + n * p.os[0] + t0 * p.os[1];
+    for (int i = threadIdx.x; i < nt * per_token.d; i += 256) {  // at most 2^16
+        const int t = div16(i, per_token), j = i - t * per_token.d, m = div16(j, per_head), k = j - m * per_head.d;
+        const T* from = x + t * p.xs[1] + m * p.xs[2];
+        T* to = out + t * p.os[1] + m * p.os[2];
+        if (k >= p.R) {
+            to[p.R + k] = from[p.R + k];
+            continue;
+        }
+        const int c0 = p.interleaved ? 2 * k : k, c1 = p.interleaved ? 2 * k + 1 : p.R + k;
+        const float a = (float)from[c0], b = (float)from[c1], c = s_cos[t * p.R + k], s = s_sin[t * p.R + k];
+        to[c0] = (T)(a * c - b * s);
+        to[c1] = (T)(a * s + b * c);
     }
 }
 
 template <typename T, int VEC>
 hipError_t launch_typed(const RotaryParams& p, hipStream_t stream) {
-    const int items = p.R / VEC + (p.D - 2 * p.R) / VEC;
-    // tokens per workgroup: about two items a thread, as many pairs as LDS holds, and enough workgroups
-    int tokens = 512 / (items * p.M);
+    const int items = VEC > 1 ? p.D / VEC : p.D - p.R;  // of a head
+    // tokens per workgroup: about four items a thread, as many pairs as LDS holds, and enough workgroups
+    int tokens = 1024 / (items * p.M);
     if (p.R > 0 && tokens > kPairs / p.R) tokens = kPairs / p.R;
     if (tokens < 1) tokens = 1;
     while (tokens > 1 && (p.T + tokens - 1) / tokens * p.N < 1024) tokens = (tokens + 1) / 2;
@@ -163,8 +154,11 @@ hipError_t launch_typed(const RotaryParams& p, hipStream_t stream) {
         c.x = static_cast<const T*>(p.x) + n0 * p.xs[0];
         c.out = static_cast<T*>(p.out) + n0 * p.os[0];
         c.pos = p.pos + n0 * p.pos_item;
-        hipLaunchKernelGGL((rotary_kernel<T, VEC>), dim3((unsigned)gx, c.N), dim3(256), 0, stream, c, tokens,
-                           make_div16(items * p.M), make_div16(items));
+        const dim3 grid((unsigned)gx, c.N);
+        const Div16 per_token = make_div16(items * p.M), per_head = make_div16(items);
+        if constexpr (VEC > 1)
+            hipLaunchKernelGGL((rotary_pieces_kernel<T, VEC>), grid, dim3(256), 0, stream, c, tokens, per_token, per_head);
+        else hipLaunchKernelGGL((rotary_pairs_kernel<T>), grid, dim3(256), 0, stream, c, tokens, per_token, per_head);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -462,7 +462,8 @@ def _layer_dtype(t) -> int:
 def _expect(name, t, shape, dtype, like, strided=False):
     """Checks one tensor argument: its shape and dtype, the device of `like`, and contiguity (with
     `strided`, of the channels alone). None passes."""
-    if t is None:
+    if t is None or (t.shape == shape and t.dtype is dtype and t.is_cuda and t.get_device() == like.get_device() and
+                     (t.is_contiguous() or (strided and t.stride(-1) == 1))):
         return
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
@@ -470,24 +471,29 @@ def _expect(name, t, shape, dtype, like, strided=False):
         raise ValueError(f"{name} is on {t.device}, expected {like.device}")
     if not t.is_cuda:
         raise ValueError("tensor arguments must be device tensors")
-    if strided:
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError(f"the channels of {name} must be contiguous")
-    elif not t.is_contiguous():
+    if not strided:
         raise ValueError(f"{name} must be contiguous")
+    if t.shape[-1] > 1:
+        raise ValueError(f"the channels of {name} must be contiguous")
 
 
-@contextlib.contextmanager
 def _launching(t, stream):
-    """Makes the device of `t` current and yields the stream handle of a call on it: `stream`, or torch's
-    current stream of that device. Memory that torch allocates meanwhile is for use on that stream."""
+    """A context in which the device of `t` is current and torch allocates memory for use on the call's
+    stream, and that stream's handle: `stream`, or torch's current stream of the device."""
     import torch
 
+    index = t.get_device()
+    here = index == torch.cuda.current_device()
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(index)  # current_stream(index).cuda_stream, without the 3 us object
+        return _NO_CONTEXT if here else torch.cuda.device(index), handle
     if isinstance(stream, torch.cuda.Stream) and stream.device != t.device:
         raise ValueError(f"the stream is of {stream.device}, the tensors are on {t.device}")
-    here = t.device.index == torch.cuda.current_device()
-    with _NO_CONTEXT if here else torch.cuda.device(t.device), _on(stream):
-        yield _stream(stream)
+    context = contextlib.ExitStack()
+    if not here:
+        context.enter_context(torch.cuda.device(index))
+    context.enter_context(_on(stream))
+    return context, _stream(stream)
 
 
 def _address(t) -> Optional[int]:
@@ -548,7 +554,8 @@ def layernorm_forward(x, weight=None, bias=None, residual=None, eps=1e-5, want_s
         _expect(name, t, (C,), torch.float32, x)
     for name, t in (("mean", mean), ("rstd", rstd)):
         _expect(name, t, x.shape[:-1], torch.float32, x)
-    with _launching(x, stream) as s:
+    context, s = _launching(x, stream)
+    with context:
         out = torch.empty_like(x) if out is None else out
         mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if mean is None else mean
         rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
@@ -576,7 +583,8 @@ def layernorm_backward(x, grad_out, mean, rstd, weight=None, residual=None, grad
         _expect(name, t, (C,), torch.float32, x)
     for name, t in (("mean", mean), ("rstd", rstd)):
         _expect(name, t, x.shape[:-1], torch.float32, x)
-    with _launching(x, stream) as s:
+    context, s = _launching(x, stream)
+    with context:
         grad_x = torch.empty_like(x) if grad_x is None else grad_x
         if want_weight_grads:
             grad_weight = torch.empty(C, dtype=torch.float32, device=x.device) if grad_weight is None else grad_weight
@@ -604,7 +612,8 @@ def _rotate(entry, in_name, x, pos, freqs, interleaved, out_name, out, stream):
     _expect(out_name, out, x.shape, x.dtype, x, strided=True)
     _expect("pos", pos, (T, A) if shared else (N, T, A), torch.float32, x)
     _expect("freqs", freqs, (A, R), torch.float32, x)
-    with _launching(x, stream) as s:
+    context, s = _launching(x, stream)
+    with context:
         out = torch.empty((N, T, M, D), dtype=x.dtype, device=x.device) if out is None else out
         r = getattr(lib(), entry)(_address(x), _strides(x), _address(pos), _address(freqs), _address(out), _strides(out),
                                   N, T, M, D, A, R, 1 if shared else N, int(bool(interleaved)), code, s)
@@ -684,7 +693,8 @@ def attention_forward(q, k, v, scale=None, softcap: float = 0.0, slopes=None, q_
     a = _attention(q, k, v, scale, softcap, slopes, q_pos, k_pos, q_doc, k_doc, prefix, causal)
     _expect("out", out, q.shape, q.dtype, q)
     _expect("lse", lse, (a.N, a.M, a.Lq), torch.float32, q)
-    with _launching(q, stream) as s:
+    context, s = _launching(q, stream)
+    with context:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
         if lse is None and want_lse:
             lse = torch.empty((a.N, a.M, a.Lq), dtype=torch.float32, device=q.device)
@@ -707,7 +717,8 @@ def attention_backward(q, k, v, out, lse, grad_out, scale=None, softcap: float =
     _expect("lse", lse, (a.N, a.M, a.Lq), torch.float32, q)
     for name, t in (("grad_k", grad_k), ("grad_v", grad_v)):
         _expect(name, t, k.shape, q.dtype, q)
-    with _launching(q, stream) as s:
+    context, s = _launching(q, stream)
+    with context:
         grad_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if grad_q is None else grad_q
         grad_k = torch.empty(k.shape, dtype=q.dtype, device=q.device) if grad_k is None else grad_k
         grad_v = torch.empty(k.shape, dtype=q.dtype, device=q.device) if grad_v is None else grad_v
