@@ -386,7 +386,7 @@ struct Row32 {
         x.last = x.doc < 0 ? -1 : p.causal ? max(x.i + w.off, w.common - 1) : p.Lk - 1;
         x.slope = 0.f;
         x.pos = make_float2(0.f, 0.f);
-        if (biased && p.slopes) {
+        if (biased) {
             x.slope = p.slopes[x.head] * kLog2e;
             x.pos = reinterpret_cast<const float2*>(p.q_pos)[(int64_t)w.n * p.Lq + x.i];
         }
@@ -481,7 +481,7 @@ struct KeyTiles {
                 if (docs) doc_x[a] = docs[min(j, p.Lk - 1)];
             }
         }
-        if (BIASED && p.slopes) {
+        if (BIASED) {
 #pragma unroll
             for (int a = 0; a < Tile::kLoads; ++a)
                 if (Tile::channel() == 0)
@@ -525,13 +525,18 @@ struct KeyTiles {
             }
         }
     }
+    // Whether something that was staged in buffer b was not finite.
+    __device__ __forceinline__ bool any_odd(int b) const {
+        int some = 0;
+        if (masks) {
+#pragma unroll
+            for (int i = 0; i < NW; ++i) some |= sh.odd[b][i];
+        }
+        return some;
+    }
     // Notes what the weights of the block of 32 keys from key j0 on meet that was not finite in buffer b.
     __device__ __forceinline__ void note_odd(Odd<DP>& odd, const acc_t& weight, int b, int j0) const {
-        if (!masks) return;
-        int some = 0;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) some |= sh.odd[b][i];
-        if (some)
+        if (any_odd(b))
             odd.template note<T>(weight, p.D, lane, [&](int r) {
                 return SUM_VALUES ? v + (j0 + r) * p.vs[1] : k + (j0 + r) * p.ks[1];
             });
@@ -546,15 +551,18 @@ struct KeyTiles {
     }
 };
 
+// What is done to the scores, each with kernels of its own: nothing, capping, or a bias (and capping, if asked for).
+enum Extras { kPlain, kCap, kBias };
+
 // The row of the register r of a 32 x 32 block.
 __device__ __forceinline__ int block_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
 // Raw scores of a block made scores in units of log 2, but for a factor, which is returned and left to the
 // exponent: the scale, or the cap, of which `s` holds the tanh then. `ds` (if given) is multiplied by the cap's
 // derivative 1 - tanh^2.
-template <typename T>
+template <typename T, int EXTRAS>
 __device__ __forceinline__ float cap_scores(const AttnParams& p, acc_t& s, acc_t* ds) {
-    if (!(p.softcap > 0.f)) return p.scale * kLog2e;
+    if (EXTRAS == kBias && !(p.softcap > 0.f)) return p.scale * kLog2e;
     const float a = p.scale / p.softcap, a2 = 2.f * kLog2e * a;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {

@@ -21,10 +21,10 @@ constexpr int kProbShift = std::is_same_v<T, _Float16> ? 8 : 0;
 constexpr int grad_q_waves(int DP, size_t element) { return DP == 32 ? 3 : DP == 128 && element == 4 ? 1 : 2; }
 constexpr int grad_kv_waves(int DP) { return DP == 32 ? 3 : DP == 64 ? 2 : 1; }
 
-template <typename T, int DP, int NW, bool EXTRAS>
+template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_grad_q_kernel(AttnParams p) {
     using O = Op<T>;
-    using Keys = KeyTiles<T, DP, NW, EXTRAS, false>;
+    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, false>;
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
     __shared__ uint32_t odd_words[32 * NW * Odd<DP>::kWords];
@@ -34,7 +34,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
     Keys keys(sh, p, w, lane);
     const bool any = w.note_split(p, keys.any());
     if (!any && w.split > 0) return;  // the first split writes delta
-    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS);
+    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS == kBias);
     typename O::Frag q[DP / O::K], go[DP / O::K];
     float delta = 0.f;
     {
@@ -62,34 +62,26 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
     for (int u = 0; u < DP / 32; ++u) gq[u] = acc_t{};
     Odd<DP> odd;
     odd.start(odd_words, wave * 32 + (lane & 31), lane, p.q_doc || p.causal);
-    keys.fetch();
-    for (int b = 0; keys.t >= 0; b ^= 1) {
-        keys.stage(b);
-        const bool whole = keys.whole(own);
-        const int j0 = keys.t * Tile::kRows;
-        __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
-        keys.fetch();
+    auto body = [&](int b, int j0, bool partial) {
 #pragma unroll
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
             const T* kt = sh.k[b] + kb * 32 * Tile::kStride;
             acc_t s = row_product<T, DP>(kt, Tile::kStride, q, lane, p.D, acc_t{});
             acc_t ds = row_product<T, DP>(sh.v[b] + kb * 32 * Tile::kStride, Tile::kStride, go, lane, p.D, minus_delta);
             float unit = p.scale * kLog2e;
-            if constexpr (EXTRAS) {
-                unit = cap_scores<T>(p, s, &ds);
-                if (p.slopes) {
+            if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s, &ds);
+            if constexpr (EXTRAS == kBias) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float2 kp = sh.pos[b][kb * 32 + block_row(r, h)];
-                        const float dx = own.pos.x - kp.x, dy = own.pos.y - kp.y;
-                        s[r] = s[r] * unit - own.slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
-                    }
-                    unit = 1.f;
+                for (int r = 0; r < 16; ++r) {
+                    const float2 kp = sh.pos[b][kb * 32 + block_row(r, h)];
+                    const float dx = own.pos.x - kp.x, dy = own.pos.y - kp.y;
+                    s[r] = s[r] * unit - own.slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
                 }
+                unit = 1.f;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) ds[r] *= exp2_of(__builtin_fmaf(s[r], unit, -lse));
-            if (!whole) {
+            if (partial) {
                 acc_t x[1] = {ds};
                 hide(x, 0.f, kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
                 ds = x[0];
@@ -97,6 +89,15 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
             add_product<T, DP>(gq, ds, kt, Tile::kStride, lane);
             keys.note_odd(odd, ds, b, j0 + kb * 32);
         }
+    };
+    keys.fetch();
+    for (int b = 0; keys.t >= 0; b ^= 1) {
+        keys.stage(b);
+        const bool whole = keys.whole(own);
+        const int j0 = keys.t * Tile::kRows;
+        __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
+        keys.fetch();
+        body(b, j0, !whole);
     }
     if (own.row >= p.R) return;
     float* part = p.part + (((int64_t)w.slab * p.R + own.row) * p.splits + w.split) * DP;
@@ -115,15 +116,15 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
         }
 }
 
-template <typename T, int DP, int NW, bool EXTRAS>
+template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kernel(AttnParams p) {
     using O = Op<T>;
     using Tile = TileOf<T, DP, NW>;
     __shared__ __attribute__((aligned(16))) T s_q[2][Tile::kElems], s_g[2][Tile::kElems];
     __shared__ __attribute__((aligned(16))) float s_lse[2][Tile::kRows], s_delta[2][Tile::kRows];
     __shared__ __attribute__((aligned(16))) int s_doc[2][Tile::kRows], s_last[2][Tile::kRows];
-    __shared__ __attribute__((aligned(16))) float s_slope[2][EXTRAS ? Tile::kRows : 1];
-    __shared__ __attribute__((aligned(16))) float2 s_pos[2][EXTRAS ? Tile::kRows : 1];
+    __shared__ __attribute__((aligned(16))) float s_slope[2][EXTRAS == kBias ? Tile::kRows : 1];
+    __shared__ __attribute__((aligned(16))) float2 s_pos[2][EXTRAS == kBias ? Tile::kRows : 1];
     __shared__ int s_odd[2][NW];
     __shared__ uint32_t odd_words[2][32 * NW * Odd<DP>::kWords];
     Work w(p, false);  // the first keys have the most rows
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
         }
     }
     float2 pos = make_float2(0.f, 0.f);
-    if (EXTRAS && p.slopes) pos = reinterpret_cast<const float2*>(p.k_pos)[(int64_t)w.n * p.Lk + j];
+    if (EXTRAS == kBias) pos = reinterpret_cast<const float2*>(p.k_pos)[(int64_t)w.n * p.Lk + j];
     const bool is_common = key < w.common;
     const int key_code = pad ? 0x7fffffff : key;  // past the last key that any row sees
 
@@ -209,7 +210,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
                 delta_x = p.delta[at];
                 doc_x = p.q_doc ? p.q_doc[(int64_t)w.n * p.Lq + i] : 0;
                 last_x = p.causal ? max(i + w.off, w.common - 1) : p.Lk - 1;
-                if (EXTRAS && p.slopes) {
+                if (EXTRAS == kBias) {
                     slope_x = p.slopes[head] * kLog2e;
                     pos_x = reinterpret_cast<const float2*>(p.q_pos)[(int64_t)w.n * p.Lq + i];
                 }
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             s_delta[b][threadIdx.x] = -delta_x;
             s_doc[b][threadIdx.x] = doc_x;
             s_last[b][threadIdx.x] = doc_x < 0 ? -1 : last_x;
-            if (EXTRAS) {
+            if (EXTRAS == kBias) {
                 s_slope[b][threadIdx.x] = slope_x;
                 s_pos[b][threadIdx.x] = pos_x;
             }
@@ -262,17 +263,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     Odd<DP> odd_k, odd_v;
     odd_k.start(odd_words[0], wave * 32 + (lane & 31), lane, masks);
     odd_v.start(odd_words[1], wave * 32 + (lane & 31), lane, masks);
-    fetch();
-    for (int b = 0; ; b ^= 1) {
-        if (t < 0) break;
-        stage(b);
-        // rows past the last have p = 0, keys past the last are not written
-        const int r0 = t * Tile::kRows;
-        bool whole = !p.causal || wave_last <= r0 / p.G + w.off || wave_last < w.common;
-        if (p.q_doc)
-            whole = whole && rr.whole && ((one_doc && rr.lo == doc0 && rr.hi == doc0) || (no_pad && wave_last < w.common));
-        __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
-        fetch();
+    auto body = [&](int b, int r0, int some, bool partial) {
 #pragma unroll
         for (int rb = 0; rb < Tile::kBlocks; ++rb) {
             const T* qt = s_q[b] + rb * 32 * Tile::kStride;
@@ -283,18 +274,16 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             acc_t s = row_product<T, DP>(qt, Tile::kStride, k, lane, p.D, acc_t{});
             ds = row_product<T, DP>(gt, Tile::kStride, v, lane, p.D, ds);
             float unit = p.scale * kLog2e;
-            if constexpr (EXTRAS) {
-                unit = cap_scores<T>(p, s, &ds);
-                if (p.slopes) {
+            if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s, &ds);
+            if constexpr (EXTRAS == kBias) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int at = rb * 32 + block_row(r, h);
-                        const float2 qp = s_pos[b][at];
-                        const float dx = qp.x - pos.x, dy = qp.y - pos.y;
-                        s[r] = s[r] * unit - s_slope[b][at] * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
-                    }
-                    unit = 1.f;
+                for (int r = 0; r < 16; ++r) {
+                    const int at = rb * 32 + block_row(r, h);
+                    const float2 qp = s_pos[b][at];
+                    const float dx = qp.x - pos.x, dy = qp.y - pos.y;
+                    s[r] = s[r] * unit - s_slope[b][at] * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
                 }
+                unit = 1.f;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -302,7 +291,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
                 ds[r] *= s[r];
                 if constexpr (kProbShift<T> != 0) ds[r] *= 1.f / (1 << kProbShift<T>);
             }
-            if (!whole) {
+            if (partial) {
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {  // four at a time, as in hide()
                     const int at = rb * 32 + 8 * g + 4 * h;
@@ -319,16 +308,29 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             }
             add_product<T, DP>(gv, s, gt, Tile::kStride, lane);
             add_product<T, DP>(gk, ds, qt, Tile::kStride, lane);
-            if (masks) {
-                int some = 0;
-#pragma unroll
-                for (int i = 0; i < NW; ++i) some |= s_odd[b][i];
-                if (some) {
-                    odd_v.template note<T>(s, p.D, lane, [&](int r) { return grad_row(r0 + rb * 32 + r); });
-                    odd_k.template note<T>(ds, p.D, lane, [&](int r) { return query_row(r0 + rb * 32 + r); });
-                }
+            if (some) {
+                odd_v.template note<T>(s, p.D, lane, [&](int r) { return grad_row(r0 + rb * 32 + r); });
+                odd_k.template note<T>(ds, p.D, lane, [&](int r) { return query_row(r0 + rb * 32 + r); });
             }
         }
+    };
+    fetch();
+    for (int b = 0; ; b ^= 1) {
+        if (t < 0) break;
+        stage(b);
+        // rows past the last have p = 0, keys past the last are not written
+        const int r0 = t * Tile::kRows;
+        bool whole = !p.causal || wave_last <= r0 / p.G + w.off || wave_last < w.common;
+        if (p.q_doc)
+            whole = whole && rr.whole && ((one_doc && rr.lo == doc0 && rr.hi == doc0) || (no_pad && wave_last < w.common));
+        __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
+        fetch();
+        int some = 0;
+        if (masks) {
+#pragma unroll
+            for (int i = 0; i < NW; ++i) some |= s_odd[b][i];
+        }
+        body(b, r0, some, !whole);
     }
     if (key >= p.Lk) return;
     const float v_unit = 1.f / (1 << kProbShift<T>);
@@ -390,7 +392,7 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(AttnParams p) {
     store_four(out, e0 % DP, p.D, x);
 }
 
-template <typename T, int DP, bool KV, bool EXTRAS>
+template <typename T, int DP, bool KV, int EXTRAS>
 void launch_owners(const AttnParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)xcd_grid((int64_t)p.N * p.Mkv * p.blocks * p.splits));
     if constexpr (KV) hipLaunchKernelGGL((attn_grad_kv_kernel<T, DP, 4, EXTRAS>), grid, dim3(256), 0, stream, p);
@@ -401,8 +403,9 @@ template <typename T, bool KV>
 hipError_t launch_typed(const AttnParams& p, hipStream_t stream) {
     return by_channels(p.D, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        if (p.softcap > 0.f || p.slopes) launch_owners<T, DP, KV, true>(p, stream);
-        else launch_owners<T, DP, KV, false>(p, stream);
+        if (p.slopes) launch_owners<T, DP, KV, kBias>(p, stream);
+        else if (p.softcap > 0.f) launch_owners<T, DP, KV, kCap>(p, stream);
+        else launch_owners<T, DP, KV, kPlain>(p, stream);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.splits == 1) return e;
         const int64_t lanes = (int64_t)p.N * p.Mkv * (KV ? (int64_t)p.Lk * 2 : p.R) * (DP / 4);

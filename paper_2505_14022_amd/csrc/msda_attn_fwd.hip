@@ -14,10 +14,10 @@ namespace {
 // Waves per SIMD that the registers of a kernel that owns rows have to leave room for.
 constexpr int row_waves(int DP, int NW) { return NW == 1 ? (DP > 32 ? 1 : 2) : DP == 32 ? 4 : DP == 64 ? 3 : 2; }
 
-template <typename T, int DP, int NW, bool EXTRAS>
+template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(AttnParams p) {
     using O = Op<T>;
-    using Keys = KeyTiles<T, DP, NW, EXTRAS, true>;
+    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, true>;
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
     __shared__ uint32_t odd_words[32 * NW * Odd<DP>::kWords];
@@ -26,7 +26,7 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
     const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
     Keys keys(sh, p, w, lane);
     if (!w.note_split(p, keys.any())) return;
-    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS);
+    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS == kBias);
     typename O::Frag q[DP / O::K];
     const T* qr = static_cast<const T*>(p.q) + w.n * p.qs[0] + own.i * p.qs[1] + own.head * p.qs[2];
 #pragma unroll
@@ -39,32 +39,23 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
     float m = -kInf, l = 0.f;
     Odd<DP> odd;
     odd.start(odd_words, wave * 32 + (lane & 31), lane, p.q_doc || p.causal);
-    keys.fetch();
-    for (int b = 0; keys.t >= 0; b ^= 1) {
-        keys.stage(b);
-        const bool whole = keys.whole(own);
-        const int j0 = keys.t * Tile::kRows;
-        __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
-        keys.fetch();
-
+    auto body = [&](int b, int j0, bool partial) {
         acc_t s[Tile::kBlocks];
         float unit = p.scale * kLog2e;  // of the raw scores, left to the exponent where nothing comes between
 #pragma unroll
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
             s[kb] = row_product<T, DP>(sh.k[b] + kb * 32 * Tile::kStride, Tile::kStride, q, lane, p.D, acc_t{});
-            if constexpr (EXTRAS) {
-                unit = cap_scores<T>(p, s[kb], nullptr);
-                if (p.slopes) {
+            if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s[kb], nullptr);
+            if constexpr (EXTRAS == kBias) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float2 kp = sh.pos[b][kb * 32 + block_row(r, h)];
-                        const float dx = own.pos.x - kp.x, dy = own.pos.y - kp.y;
-                        s[kb][r] = s[kb][r] * unit - own.slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
-                    }
-                    unit = 1.f;
+                for (int r = 0; r < 16; ++r) {
+                    const float2 kp = sh.pos[b][kb * 32 + block_row(r, h)];
+                    const float dx = own.pos.x - kp.x, dy = own.pos.y - kp.y;
+                    s[kb][r] = s[kb][r] * unit - own.slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
                 }
+                unit = 1.f;
             }
-            if (!whole) {
+            if (partial) {
                 acc_t x[1] = {s[kb]};
                 hide(x, -kInf, kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
                 s[kb] = x[0];
@@ -97,6 +88,16 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
             add_product<T, DP>(o, s[kb], sh.v[b] + kb * 32 * Tile::kStride, Tile::kStride, lane);
             keys.note_odd(odd, s[kb], b, j0 + kb * 32);
         }
+    };
+    keys.fetch();
+    for (int b = 0; keys.t >= 0; b ^= 1) {
+        keys.stage(b);
+        const bool whole = keys.whole(own);
+        const int j0 = keys.t * Tile::kRows;
+        __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
+        keys.fetch();
+
+        body(b, j0, !whole);
     }
     l = halves_sum(l);
     if (own.row >= p.R) return;
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(256) void attn_pack_kernel(AttnPack c) {
     *reinterpret_cast<Piece<T, kPer>*>(static_cast<T*>(c.to) + row * c.width + d) = x;
 }
 
-template <typename T, int DP, bool EXTRAS>
+template <typename T, int DP, int EXTRAS>
 void launch_rows(const AttnParams& p, int waves, hipStream_t stream) {
     const dim3 grid((unsigned)xcd_grid((int64_t)p.N * p.Mkv * p.blocks * p.splits));
     if (waves == 4) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, 4, EXTRAS>), grid, dim3(256), 0, stream, p);
@@ -242,8 +243,9 @@ template <typename T>
 hipError_t launch_typed(const AttnParams& p, int waves, hipStream_t stream) {
     return by_channels(p.D, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        if (p.softcap > 0.f || p.slopes) launch_rows<T, DP, true>(p, waves, stream);
-        else launch_rows<T, DP, false>(p, waves, stream);
+        if (p.slopes) launch_rows<T, DP, kBias>(p, waves, stream);
+        else if (p.softcap > 0.f) launch_rows<T, DP, kCap>(p, waves, stream);
+        else launch_rows<T, DP, kPlain>(p, waves, stream);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.splits == 1) return e;
         const int64_t rows = (int64_t)p.N * p.Mkv * p.R;
