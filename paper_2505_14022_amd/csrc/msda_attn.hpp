@@ -409,11 +409,13 @@ constexpr int kCommon = -2;
 template <typename T, int DP, int NW, bool BIASED, bool SUM_VALUES>
 struct KeyTiles {
     using Tile = TileOf<T, DP, NW>;
+    // a lone wave has read a tile before it writes the next: one buffer, so that twice as many waves fit
+    static constexpr int kBuffers = NW == 1 ? 1 : 2;
     struct Shared {
-        T k[2][Tile::kElems], v[2][Tile::kElems];
-        int doc[2][Tile::kRows];
-        float2 pos[2][BIASED ? Tile::kRows : 1];
-        int odd[2][NW];  // per wave: some of what it staged was not finite
+        T k[kBuffers][Tile::kElems], v[kBuffers][Tile::kElems];
+        int doc[kBuffers][Tile::kRows];
+        float2 pos[kBuffers][BIASED ? Tile::kRows : 1];
+        int odd[kBuffers][NW];  // per wave: some of what it staged was not finite
     };
     Shared& sh;
     const AttnParams& p;

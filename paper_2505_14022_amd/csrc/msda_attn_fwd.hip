@@ -12,7 +12,7 @@ namespace msda {
 namespace {
 
 // Waves per SIMD that the registers of a kernel that owns rows have to leave room for.
-constexpr int row_waves(int DP, int NW) { return NW == 1 ? (DP > 32 ? 1 : 2) : DP == 32 ? 4 : DP == 64 ? 3 : 2; }
+constexpr int row_waves(int DP, int NW) { return NW == 1 ? 2 : DP == 32 ? 4 : DP == 64 ? 3 : 2; }
 
 template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(AttnParams p) {
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
         }
     };
     keys.fetch();
-    for (int b = 0; keys.t >= 0; b ^= 1) {
+    for (int b = 0; keys.t >= 0; b ^= Keys::kBuffers - 1) {
         keys.stage(b);
         const bool whole = keys.whole(own);
         const int j0 = keys.t * Tile::kRows;
@@ -273,7 +273,7 @@ AttnPlan attn_plan(const AttnParams& p, int dtype, AttnKernel kernel) {
     // Waves that the card holds at once, by the kernels' registers (a lone wave's by its LDS), where one split's are few;
     // twice as many keep it full while the last workgroups end. With one split each, DETR-encoder self-attention over 4947
     // pixels (2496 waves) took 203, 202 and 248 us in the three kernels, with three 123, 143 and 206.
-    const int per_simd = a.waves == 1 ? 1 : DP == 32 ? (kernel == kForward ? 4 : 3) : DP == 64 ? (kernel == kForward ? 3 : 2)
+    const int per_simd = a.waves == 1 ? 2 : DP == 32 ? (kernel == kForward ? 4 : 3) : DP == 64 ? (kernel == kForward ? 3 : 2)
                                                                                    : kernel == kGradKV ? 1 : 2;
     const int64_t room = 1024 * per_simd;
     int64_t splits = waves > 0 ? ((4 * waves < room ? 1 : 2) * room + waves - 1) / waves : 1;
