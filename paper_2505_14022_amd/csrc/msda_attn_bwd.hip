@@ -62,18 +62,18 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
     for (int u = 0; u < DP / 32; ++u) gq[u] = acc_t{};
     Odd<DP> odd;
     odd.start(odd_words, wave * 32 + (lane & 31), lane, p.q_doc || p.causal);
-    auto body = [&](int b, int j0, bool partial) {
+    auto body = [&](int b, int j0, int sub, bool partial) {  // the tile's keys from sub on
 #pragma unroll
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
-            const T* kt = sh.k[b] + kb * 32 * Tile::kStride;
+            const T* kt = sh.k[b] + (sub + kb * 32) * Tile::kStride;
             acc_t s = row_product<T, DP>(kt, Tile::kStride, q, lane, p.D, acc_t{});
-            acc_t ds = row_product<T, DP>(sh.v[b] + kb * 32 * Tile::kStride, Tile::kStride, go, lane, p.D, minus_delta);
+            acc_t ds = row_product<T, DP>(sh.v[b] + (sub + kb * 32) * Tile::kStride, Tile::kStride, go, lane, p.D, minus_delta);
             float unit = p.scale * kLog2e;
             if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s, &ds);
             if constexpr (EXTRAS == kBias) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float2 kp = sh.pos[b][kb * 32 + block_row(r, h)];
+                    const float2 kp = sh.pos[b][sub + kb * 32 + block_row(r, h)];
                     const float dx = own.pos.x - kp.x, dy = own.pos.y - kp.y;
                     s[r] = s[r] * unit - own.slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
                 }
@@ -83,11 +83,11 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
             for (int r = 0; r < 16; ++r) ds[r] *= exp2_of(__builtin_fmaf(s[r], unit, -lse));
             if (partial) {
                 acc_t x[1] = {ds};
-                hide(x, 0.f, kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
+                hide(x, 0.f, sub + kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
                 ds = x[0];
             }
             add_product<T, DP>(gq, ds, kt, Tile::kStride, lane);
-            keys.note_odd(odd, ds, b, j0 + kb * 32);
+            keys.note_odd(odd, ds, b, j0 + sub + kb * 32);
         }
     };
     keys.fetch();
@@ -97,7 +97,8 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
         const int j0 = keys.t * Tile::kRows;
         __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
         keys.fetch();
-        body(b, j0, !whole);
+#pragma unroll 1
+        for (int sub = 0; sub < Tile::kRows; sub += 32 * Tile::kBlocks) body(b, j0, sub, !whole);
     }
     if (own.row >= p.R) return;
     float* part = p.part + (((int64_t)w.slab * p.R + own.row) * p.splits + w.split) * DP;
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
 template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kernel(AttnParams p) {
     using O = Op<T>;
-    using Tile = TileOf<T, DP, NW>;
+    using Tile = TileOf<T, DP, NW, true>;
     __shared__ __attribute__((aligned(16))) T s_q[2][Tile::kElems], s_g[2][Tile::kElems];
     __shared__ __attribute__((aligned(16))) float s_lse[2][Tile::kRows], s_delta[2][Tile::kRows];
     __shared__ __attribute__((aligned(16))) int s_doc[2][Tile::kRows], s_last[2][Tile::kRows];
@@ -263,14 +264,15 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     Odd<DP> odd_k, odd_v;
     odd_k.start(odd_words[0], wave * 32 + (lane & 31), lane, masks);
     odd_v.start(odd_words[1], wave * 32 + (lane & 31), lane, masks);
-    auto body = [&](int b, int r0, int some, bool partial) {
+    auto body = [&](int b, int r0, int sub, int some, bool partial) {  // the tile's rows from sub on
 #pragma unroll
-        for (int rb = 0; rb < Tile::kBlocks; ++rb) {
-            const T* qt = s_q[b] + rb * 32 * Tile::kStride;
-            const T* gt = s_g[b] + rb * 32 * Tile::kStride;
+        for (int block = 0; block < Tile::kBlocks; ++block) {
+            const int first = sub + block * 32;
+            const T* qt = s_q[b] + first * Tile::kStride;
+            const T* gt = s_g[b] + first * Tile::kStride;
             acc_t ds;  // the sums of dP begin at -delta
 #pragma unroll
-            for (int r = 0; r < 16; ++r) ds[r] = s_delta[b][rb * 32 + block_row(r, h)];
+            for (int r = 0; r < 16; ++r) ds[r] = s_delta[b][first + block_row(r, h)];
             acc_t s = row_product<T, DP>(qt, Tile::kStride, k, lane, p.D, acc_t{});
             ds = row_product<T, DP>(gt, Tile::kStride, v, lane, p.D, ds);
             float unit = p.scale * kLog2e;
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             if constexpr (EXTRAS == kBias) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int at = rb * 32 + block_row(r, h);
+                    const int at = first + block_row(r, h);
                     const float2 qp = s_pos[b][at];
                     const float dx = qp.x - pos.x, dy = qp.y - pos.y;
                     s[r] = s[r] * unit - s_slope[b][at] * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
@@ -287,14 +289,14 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[r] = exp2_of(__builtin_fmaf(s[r], unit, s_lse[b][rb * 32 + block_row(r, h)]));
+                s[r] = exp2_of(__builtin_fmaf(s[r], unit, s_lse[b][first + block_row(r, h)]));
                 ds[r] *= s[r];
                 if constexpr (kProbShift<T> != 0) ds[r] *= 1.f / (1 << kProbShift<T>);
             }
             if (partial) {
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {  // four at a time, as in hide()
-                    const int at = rb * 32 + 8 * g + 4 * h;
+                    const int at = first + 8 * g + 4 * h;
                     const int4 l4 = *reinterpret_cast<const int4*>(&s_last[b][at]), d4 = *reinterpret_cast<const int4*>(&s_doc[b][at]);
                     const int last[4] = {l4.x, l4.y, l4.z, l4.w}, row_doc[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
@@ -309,8 +311,8 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             add_product<T, DP>(gv, s, gt, Tile::kStride, lane);
             add_product<T, DP>(gk, ds, qt, Tile::kStride, lane);
             if (some) {
-                odd_v.template note<T>(s, p.D, lane, [&](int r) { return grad_row(r0 + rb * 32 + r); });
-                odd_k.template note<T>(ds, p.D, lane, [&](int r) { return query_row(r0 + rb * 32 + r); });
+                odd_v.template note<T>(s, p.D, lane, [&](int r) { return grad_row(r0 + first + r); });
+                odd_k.template note<T>(ds, p.D, lane, [&](int r) { return query_row(r0 + first + r); });
             }
         }
     };
@@ -330,7 +332,8 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
 #pragma unroll
             for (int i = 0; i < NW; ++i) some |= s_odd[b][i];
         }
-        body(b, r0, some, !whole);
+#pragma unroll 1
+        for (int sub = 0; sub < Tile::kRows; sub += 32 * Tile::kBlocks) body(b, r0, sub, some, !whole);
     }
     if (key >= p.Lk) return;
     const float v_unit = 1.f / (1 << kProbShift<T>);

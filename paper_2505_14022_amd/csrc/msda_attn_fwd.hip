@@ -12,10 +12,10 @@ namespace msda {
 namespace {
 
 // Waves per SIMD that the registers of a kernel that owns rows have to leave room for.
-constexpr int row_waves(int DP, int NW) { return NW == 1 ? 2 : DP == 32 ? 4 : DP == 64 ? 3 : 2; }
+constexpr int row_waves(int DP, int NW, size_t element) { return NW == 1 ? (element == 4 && DP > 32 ? 1 : 2) : DP == 32 ? 4 : DP == 64 ? 3 : 2; }
 
 template <typename T, int DP, int NW, int EXTRAS>
-__global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(AttnParams p) {
+__global__ __launch_bounds__(64 * NW, row_waves(DP, NW, sizeof(T))) void attn_fwd_kernel(AttnParams p) {
     using O = Op<T>;
     using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, true>;
     using Tile = typename Keys::Tile;
@@ -39,17 +39,17 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
     float m = -kInf, l = 0.f;
     Odd<DP> odd;
     odd.start(odd_words, wave * 32 + (lane & 31), lane, p.q_doc || p.causal);
-    auto body = [&](int b, int j0, bool partial) {
+    auto body = [&](int b, int j0, int sub, bool partial) {  // the tile's keys from sub on
         acc_t s[Tile::kBlocks];
         float unit = p.scale * kLog2e;  // of the raw scores, left to the exponent where nothing comes between
 #pragma unroll
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
-            s[kb] = row_product<T, DP>(sh.k[b] + kb * 32 * Tile::kStride, Tile::kStride, q, lane, p.D, acc_t{});
+            s[kb] = row_product<T, DP>(sh.k[b] + (sub + kb * 32) * Tile::kStride, Tile::kStride, q, lane, p.D, acc_t{});
             if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s[kb], nullptr);
             if constexpr (EXTRAS == kBias) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float2 kp = sh.pos[b][kb * 32 + block_row(r, h)];
+                    const float2 kp = sh.pos[b][sub + kb * 32 + block_row(r, h)];
                     const float dx = own.pos.x - kp.x, dy = own.pos.y - kp.y;
                     s[kb][r] = s[kb][r] * unit - own.slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
                 }
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
             }
             if (partial) {
                 acc_t x[1] = {s[kb]};
-                hide(x, -kInf, kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
+                hide(x, -kInf, sub + kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
                 s[kb] = x[0];
             }
         }
@@ -85,8 +85,8 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
                 s[kb][r] = exp2_of(__builtin_fmaf(s[kb][r], unit, -base));
                 l += s[kb][r];
             }
-            add_product<T, DP>(o, s[kb], sh.v[b] + kb * 32 * Tile::kStride, Tile::kStride, lane);
-            keys.note_odd(odd, s[kb], b, j0 + kb * 32);
+            add_product<T, DP>(o, s[kb], sh.v[b] + (sub + kb * 32) * Tile::kStride, Tile::kStride, lane);
+            keys.note_odd(odd, s[kb], b, j0 + sub + kb * 32);
         }
     };
     keys.fetch();
@@ -97,7 +97,8 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW)) void attn_fwd_kernel(At
         __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
         keys.fetch();
 
-        body(b, j0, !whole);
+#pragma unroll 1
+        for (int sub = 0; sub < Tile::kRows; sub += 32 * Tile::kBlocks) body(b, j0, sub, !whole);
     }
     l = halves_sum(l);
     if (own.row >= p.R) return;
@@ -259,7 +260,10 @@ hipError_t launch_typed(const AttnParams& p, int waves, hipStream_t stream) {
 
 }  // namespace
 
-int attn_tile(int dtype, int waves) { return dtype == MSDA_F32 || waves == 1 ? 32 : Op<_Float16>::kTile; }
+// The kernels' tile: TileOf::kRows.
+static int attn_tile(int dtype, int waves, int DP, bool wide) {
+    return dtype == MSDA_F32 || waves == 1 ? 32 : wide && DP == 32 ? kWideTile : Op<_Float16>::kTile;
+}
 int attn_channels(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
 AttnPlan attn_plan(const AttnParams& p, int dtype, AttnKernel kernel) {
@@ -267,7 +271,7 @@ AttnPlan attn_plan(const AttnParams& p, int dtype, AttnKernel kernel) {
     const int64_t slabs = (int64_t)p.N * p.Mkv, own = kernel == kGradKV ? p.Lk : p.R, across = kernel == kGradKV ? p.R : p.Lk;
     AttnPlan a;
     a.waves = kernel == kForward && own <= 32 ? 1 : 4;
-    a.tile = attn_tile(dtype, a.waves);
+    a.tile = attn_tile(dtype, a.waves, DP, kernel != kForward);
     a.blocks = (int)((own + 32 * a.waves - 1) / (32 * a.waves));
     const int64_t tiles = (across + a.tile - 1) / a.tile, waves = slabs * a.blocks * a.waves;
     // Waves that the card holds at once, by the kernels' registers (a lone wave's by its LDS), where one split's are few;
