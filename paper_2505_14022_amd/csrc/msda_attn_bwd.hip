@@ -375,14 +375,21 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(AttnParams p) {
     const int e0 = (threadIdx.x % kLanes) * 4;
     const float* part = p.part + at * p.splits * (kLanes * 4) + e0;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < p.splits; ++s) {  // loads do not wait for one another: what is not filled is dropped
-        const bool full = filled[s];
-        const float4 y = *reinterpret_cast<const float4*>(part + (int64_t)s * (kLanes * 4));
-        x[0] += full ? y.x : 0.f;
-        x[1] += full ? y.y : 0.f;
-        x[2] += full ? y.z : 0.f;
-        x[3] += full ? y.w : 0.f;
+    for (int s0 = 0; s0 < p.splits; s0 += 4) {
+        int full[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) full[k] = s0 + k < p.splits ? filled[s0 + k] : 0;
+        float4 y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            y[k] = full[k] ? *reinterpret_cast<const float4*>(part + (int64_t)(s0 + k) * (kLanes * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[0] += y[k].x;
+            x[1] += y[k].y;
+            x[2] += y[k].z;
+            x[3] += y[k].w;
+        }
     }
     const bool values = KV && e0 >= DP;
     T* out;

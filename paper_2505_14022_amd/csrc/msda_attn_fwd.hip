@@ -282,6 +282,10 @@ AttnPlan attn_plan(const AttnParams& p, int dtype, AttnKernel kernel) {
     const int64_t room = 1024 * per_simd;
     int64_t splits = waves > 0 ? ((4 * waves < room ? 1 : 2) * room + waves - 1) / waves : 1;
     const bool full = waves >= room;
+    // Masks leave some workgroups many tiles and others few. Where a SIMD holds one wave, nothing else runs beside the
+    // longest ones: shorter runs (16 heads of 128 channels over 2 x 4096 packed causal tokens: 441 us -> 323 and 10 more
+    // to add the splits up). The others lose more by the partial results (the encoder's step above 433 us -> 536).
+    if (per_simd == 1) splits *= p.q_doc ? 8 : p.causal ? 2 : 1;
     // runs shorter than this do not pay for the workgroup's start and its partial results
     const int64_t least = full ? 16 : 4;
     // and the partial results of all splits have to fit into half a GB
