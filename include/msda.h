@@ -367,7 +367,8 @@ msda_status_t msda_rotary_backward(const void* grad_out, const int64_t* grad_out
  * query does not see has no effect on it, infinities and NaN included.
  */
 typedef struct {
-    int64_t N, Lq, Lk, M, Mkv, D; /* M a multiple of Mkv; 1 <= D <= MSDA_ATTENTION_MAX_D              */
+    int64_t N, Lq, Lk, M, Mkv, D; /* M a multiple of Mkv, at most 32768; 1 <= D <= MSDA_ATTENTION_MAX_D; */
+                                  /* Lk and Lq * M / Mkv below 2^31 - 1024; more: NOT_SUPPORTED       */
     int dtype;                    /* of q, k, v, out and the gradients                                */
     int causal;                   /* nonzero: the order rule above; needs Lk >= Lq                    */
     int unaligned;                /* nonzero: q, k and v may start off 16-byte boundaries; see below  */
@@ -375,7 +376,7 @@ typedef struct {
     float softcap;                /* finite, >= 0; 0: scores are not capped                           */
     int64_t q_stride[3];          /* strides of q [N, Lq, M, D] in elements: batch item, token, head; */
     int64_t k_stride[3];          /* the channels are contiguous. Likewise k [N, Lk, Mkv, D]          */
-    int64_t v_stride[3];          /* and v [N, Lk, Mkv, D]                                            */
+    int64_t v_stride[3];          /* and v [N, Lk, Mkv, D]; >= 0, and 0 repeats an entry              */
     const float* slopes;          /* DEVICE [M] fp32 or NULL: no bias; constants, they get no gradient */
     const float* q_pos;           /* DEVICE [N, Lq, 2] fp32 and [N, Lk, 2] fp32, with slopes: the     */
     const float* k_pos;           /* places between which the (Euclidean) distance is taken           */
@@ -386,7 +387,7 @@ typedef struct {
 #define MSDA_ATTENTION_MAX_D 128
 
 /* Workspace bytes of msda_attention_forward (backward == 0) or msda_attention_backward: host-only, from
- * the sizes, dtype and which tables are given. */
+ * the sizes, strides, dtype, causal, unaligned and which tables are given. */
 msda_status_t msda_attention_workspace_size(const msda_attention_t* a, int backward, size_t* bytes);
 
 /*
@@ -396,7 +397,8 @@ msda_status_t msda_attention_workspace_size(const msda_attention_t* a, int backw
  * msda_attention_workspace_size bytes, 16-byte aligned (may be NULL if that is 0), used by nothing
  * else until the enqueued work completes; a smaller one is MSDA_ERROR_INVALID_VALUE. Out is 16-byte
  * aligned. q, k and v are read in 16-byte pieces: each needs 16-byte alignment, unless its strides or
- * D channels are not multiples of 16 bytes or `unaligned` is set; it is copied into the workspace then.
+ * D channels are not multiples of 16 bytes, 129 of its tokens lie 2 GiB apart or `unaligned` is set; it
+ * is copied into the workspace then.
  * N * Lq == 0 is a no-op; Lk == 0 writes out = 0, lse = -inf.
  */
 msda_status_t msda_attention_forward(const msda_attention_t* a, const void* q, const void* k, const void* v,

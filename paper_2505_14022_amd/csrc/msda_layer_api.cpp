@@ -282,12 +282,12 @@ struct Attention {
 };
 
 // Whether rows of D channels with these strides are whole 16-byte pieces on 16-byte boundaries of their base, and
-// the rows of a tile (at most 65 tokens of `heads` heads) lie within the 31 bits of the kernels' offsets.
+// the rows of a tile (at most 129 tokens of `heads` heads) lie within the 31 bits of the kernels' offsets.
 bool row_pieces(const int64_t* stride, int64_t N, int64_t L, int64_t H, int64_t heads, int64_t D, int es) {
     const int64_t extent[3] = {N, L, H};
     bool yes = (D * es) % 16 == 0;
     for (int i = 0; i < 3; ++i) yes = yes && (extent[i] <= 1 || (stride[i] * es) % 16 == 0);
-    const double reach = (L > 1 ? 65.0 * fabs((double)stride[1]) : 0.0) + (double)(heads - 1) * fabs((double)stride[2]) + D;
+    const double reach = (L > 1 ? 129.0 * fabs((double)stride[1]) : 0.0) + (double)(heads - 1) * fabs((double)stride[2]) + D;
     return yes && reach * es < 2147483648.0;
 }
 

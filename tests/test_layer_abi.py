@@ -123,7 +123,7 @@ def backward(L, a, lse=0x5000, go=0x6000, gq=0x7000, gk=0x8000, gv=0x9000, ws=0x
     (dict(slopes=0x100), INVALID, "slopes"), (dict(slopes=0x100, q_pos=0x100, k_pos=0x104), INVALID, "misaligned"),
     (dict(prefix=0x102), INVALID, "misaligned"), (dict(Lk=1 << 31), UNSUPPORTED, "2^31"),
     (dict(Lq=1 << 30), UNSUPPORTED, "2^31"), (dict(N=1 << 30, M=1 << 10, Mkv=1 << 10), UNSUPPORTED, "launch"),
-    (dict(N=1 << 20, Lk=1 << 20), UNSUPPORTED, "launch"),
+    (dict(N=1 << 20, Lk=1 << 20), UNSUPPORTED, "launch"), (dict(M=32770), UNSUPPORTED, "32768"),
 ])
 def test_attention_refuses(L, no_gpu, kw, status, needle):
     a = description(**kw)
@@ -152,6 +152,33 @@ def test_attention_refuses_bad_pointers_and_workspaces(L, no_gpu):
         assert backward(L, a, **kw) == INVALID, kw
     assert L.msda_attention_forward(None, None, None, None, None, None, None, 0, None) == INVALID
     assert L.msda_attention_workspace_size(ctypes.byref(a), 0, None) == INVALID
+
+
+@pytest.mark.parametrize("which", ["q_stride", "k_stride", "v_stride"])
+def test_attention_refuses_negative_strides(L, no_gpu, which):
+    for i in range(3):
+        a = description()
+        getattr(a, which)[i] = -8
+        assert forward(L, a) == INVALID and "strides" in msda.last_error()
+        assert backward(L, a) == INVALID and "strides" in msda.last_error()
+
+
+@pytest.mark.parametrize("which,rows", [("q_stride", 70 * 4), ("k_stride", 90 * 2), ("v_stride", 90 * 2)])
+def test_attention_copies_rows_that_lie_far_apart(L, which, rows):
+    """The kernels' offsets within a tile of 128 tokens have 31 bits: tokens of 2^24 bytes are copied to rows of 64."""
+    def need(stride, backward):
+        a = description()
+        if stride:
+            getattr(a, which)[1] = stride
+            getattr(a, which)[0] = stride * 90
+        size = ctypes.c_size_t(0)
+        assert L.msda_attention_workspace_size(ctypes.byref(a), backward, ctypes.byref(size)) == OK
+        return size.value
+
+    for b in (0, 1):
+        assert need(1 << 22, b) == need(0, b)
+        for stride in (1 << 23, 3 << 22, 1 << 24, 1 << 33):
+            assert need(stride, b) >= need(0, b) + 2 * rows * 64
 
 
 def test_attention_empty_is_a_no_op(L):
