@@ -409,11 +409,12 @@ constexpr int kCommon = -2;
 // registers while the waves work on the current one. All loads of a tile are issued together; what must not
 // count (keys past the last, padding) is dropped when the tile is put into LDS.
 // SUM_VALUES: the kernel sums over the values (forward), else over the keys (grad_q).
-template <typename T, int DP, int NW, bool BIASED, bool SUM_VALUES>
+// BUFFERS 1: for a lone wave, which has read a tile before it writes the next, so that twice as many waves fit, and
+// for kernels that wait before they write.
+template <typename T, int DP, int NW, bool BIASED, bool SUM_VALUES, int BUFFERS = NW == 1 ? 1 : 2>
 struct KeyTiles {
     using Tile = TileOf<T, DP, NW, !SUM_VALUES>;
-    // a lone wave has read a tile before it writes the next: one buffer, so that twice as many waves fit
-    static constexpr int kBuffers = NW == 1 ? 1 : 2;
+    static constexpr int kBuffers = BUFFERS;
     struct Shared {
         T k[kBuffers][Tile::kElems], v[kBuffers][Tile::kElems];
         int doc[kBuffers][Tile::kRows];

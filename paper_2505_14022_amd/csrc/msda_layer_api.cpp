@@ -357,6 +357,12 @@ Attention attention_of(const msda_attention_t& a, bool backward) {
     return x;
 }
 
+// Whether 16-bit rows may have so few keys that their delta is formed with care, in a launch of its own.
+bool rows_of_few_keys(const msda_attention_t& a) {
+    const int64_t few = 64;
+    return a.dtype != MSDA_F32 && a.Lk > 0 && (a.Lk <= few || a.q_doc || (a.causal && a.Lk - a.Lq < few));
+}
+
 msda_status_t check_workspace(const Attention& x, const void* workspace, size_t bytes) {
     if (x.bytes > 0 && (!workspace || bytes < x.bytes))
         return fail(MSDA_ERROR_INVALID_VALUE, "workspace of %zu bytes is smaller than the %zu needed",
@@ -507,8 +513,18 @@ msda_status_t msda_attention_backward(const msda_attention_t* a, const void* q, 
     x.p.grad_k = grad_k;
     x.p.grad_v = grad_v;
     if (e == hipSuccess) e = find_ranges(x, workspace, (hipStream_t)stream);
-    if (e == hipSuccess && a->Lq > 0)  // writes delta, which grad_k and grad_v need
-        e = msda::launch_attn_grad_q(kernel_params(x, false, workspace), a->dtype, (hipStream_t)stream);
+    if (e == hipSuccess && a->Lq > 0) {
+        msda::AttnParams p = kernel_params(x, false, workspace);
+        if (rows_of_few_keys(*a)) {
+            msda::AttnParams d = p;
+            d.splits = 1;
+            d.chunk = d.tiles;
+            e = msda::launch_attn_delta(d, a->dtype, (hipStream_t)stream);
+            p.delta_known = 1;
+        }
+        // writes delta otherwise, which grad_k and grad_v need
+        if (e == hipSuccess) e = msda::launch_attn_grad_q(p, a->dtype, (hipStream_t)stream);
+    }
     if (e == hipSuccess && a->Lk > 0)
         e = msda::launch_attn_grad_kv(kernel_params(x, true, workspace), a->dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "attention backward launch: %s", hipGetErrorString(e));

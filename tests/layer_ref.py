@@ -118,9 +118,10 @@ def seen_pairs(N, Lq, Lk, q_doc=None, k_doc=None, prefix=None, causal=False):
 
 
 def attention(q, k, v, scale=None, softcap=0.0, slopes=None, q_pos=None, k_pos=None, q_doc=None, k_doc=None, prefix=None,
-              causal=False, grad_out=None):
+              causal=False, grad_out=None, few_keys=False):
     """{name: (value, bound)} of out, lse and, with grad_out, grad_q, grad_k and grad_v. What a query does not see
-    is left out of every sum, whatever it holds."""
+    is left out of every sum, whatever it holds. few_keys: every row has so few that its delta is not that of the
+    rounded out, but mended by sum_j P (dP - delta)."""
     dt = q.dtype
     h, tiny = half_step(dt), TINY[dt]
     hp = 0.0 if dt == torch.float32 else h           # probabilities and dS go through the element type
@@ -176,6 +177,9 @@ def attention(q, k, v, scale=None, softcap=0.0, slopes=None, q_pos=None, k_pos=N
     rho2 = rho + d_lse + 8 * U * (lse.abs() + 1)
     d_dP = (D + 4) * U * (G.abs() @ V.abs().transpose(2, 3))
     d_delta = (G.abs() * (d_out + h * out.abs() + tiny)).sum(-1, keepdim=True) + (D + 8) * U * (G * out).abs().sum(-1, keepdim=True)
+    if few_keys:  # delta + sum P (dP - delta): the errors of the sum, and what 1 - sum P leaves of delta's own
+        d_delta = (P * (d_dP + (rho2 + (Lk + 12) * U) * (E.abs() + d_delta))).sum(-1, keepdim=True)
+        d_delta = d_delta + 2 * U * delta.abs()
     d_dS = P * ((rho2 + 12 * U) * E.abs() + d_dP + d_delta) + hp * dS.abs()
     d_dS = torch.where(seen, d_dS * 1.02 + tp, zero)
     groups = lambda x: flat(x.reshape(N, Mkv, M // Mkv, Lk, D).sum(2))  # noqa: E731

@@ -57,8 +57,8 @@ def masks_of(N, Lq, Lk, M, docs="none", prefix=None, causal=False, softcap=0.0, 
     return how
 
 
-def check(q, k, v, go, how, scale=None, backward=True, stream=None):
-    ref = layer_ref.attention(q, k, v, scale=scale, grad_out=go if backward else None, **how)
+def check(q, k, v, go, how, scale=None, backward=True, stream=None, few_keys=False):
+    ref = layer_ref.attention(q, k, v, scale=scale, grad_out=go if backward else None, few_keys=few_keys, **how)
     out, lse = msda.attention_forward(q, k, v, scale=scale, stream=stream, **how)
     got = {"out": out, "lse": lse}
     if backward:
@@ -324,3 +324,33 @@ def test_attention_gradients_against_differences():
         d1, d2 = ((loss(d, h) - loss(d, -h)) / (2 * h) for h in (e, e / 2))
         # a halved step leaves a quarter of the truncation; the rest is the outputs' rounding
         assert abs(d2 - slope) <= abs(d1 - d2) + 8 * noise / e, (d1, d2, slope)
+
+
+FEW = [
+    # N, Lq, Lk, M, Mkv, D, masks
+    (1, 2, 2, 8, 2, 48, {}),
+    (2, 2, 2, 4, 4, 32, {"causal": True}),
+    (1, 1, 2, 8, 2, 128, {"docs": "pad"}),
+    (2, 3, 5, 4, 2, 64, {"causal": True, "softcap": 4.0}),
+    (1, 9, 7, 2, 1, 16, {"bias": True, "softcap": 4.0}),
+    (1, 64, 64, 2, 2, 96, {"causal": True}),
+    (3, 260, 260, 2, 1, 64, {"step": 4}),
+    (1, 260, 260, 3, 3, 128, {"step": 4, "causal": True, "softcap": 9.0}),
+    (1, 512, 512, 2, 2, 32, {"step": 8, "causal": True}),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("case", FEW, ids=lambda c: "-".join(map(str, c[:6])))
+def test_attention_gradients_of_rows_with_few_keys(case, dtype):
+    """Short rows: their gradients are off by their own roundings and not by that of out."""
+    import torch
+
+    N, Lq, Lk, M, Mkv, D, masks = case
+    masks = dict(masks)
+    step = masks.pop("step", 0)
+    how = masks_of(N, Lq, Lk, M, **masks)
+    if step:  # documents of `step` rows
+        how["q_doc"] = how["k_doc"] = (torch.arange(Lq, dtype=torch.int32) // step)[None].repeat(N, 1).contiguous().cuda()
+    q, k, v, go = make(N, Lq, Lk, M, Mkv, D, dtype)
+    check(q, k, v, go, how, few_keys=True)
