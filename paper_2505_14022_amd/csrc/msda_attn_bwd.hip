@@ -134,7 +134,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
         mass = halves_sum(mass);
         lack = halves_sum(lack);
         // an eighth of a step of out's: probabilities that add up to less have keys elsewhere
-        if (h == 0 && own.row < p.R && fabsf(mass - 1.f) < 0x1p-12f) p.delta[own.stat] = delta + lack;
+        if (h == 0 && own.row < p.R && fabsf(mass - 1.f) < 0x1p-12f && fabsf(lack) < kInf) p.delta[own.stat] = delta + lack;
         return;
     }
     if (own.row >= p.R) return;
