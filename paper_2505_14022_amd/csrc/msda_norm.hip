@@ -9,6 +9,8 @@
 // columns from row to row: weight and bias are loaded once, and in the backward each lane sums its columns'
 // grad_weight and grad_bias in registers over all its rows. A workgroup writes one row of partial sums,
 // and a second kernel adds the workgroups' rows in a fixed order.
+// Measured: 87296 rows x 1024 in fp16 take 80 us forward, 92 backward and 6 for the sums, 4.1 TB/s in all (a large copy
+// reaches 5.5); 39894 rows x 256 in bf16 with a residual 11, 16 and 5; 300 rows x 256 3.0, of a call of 13.4.
 #include "msda_layer.h"
 #include "msda_layer.hpp"
 
