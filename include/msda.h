@@ -362,7 +362,7 @@ msda_status_t msda_rotary_backward(const void* grad_out, const int64_t* grad_out
  *   documents: no tables; or q_doc[n,i] >= 0 and k_doc[n,j] >= 0 and (q_doc[n,i] == k_doc[n,j] or
  *              j < prefix[n])
  *   order:     not causal; or j <= i + Lk - Lq (the last query sees every key); or j < prefix[n]
- * so a document of -1 is padding, and the first prefix[n] keys are common to all. A query that sees no
+ * so any negative document is padding, and the first prefix[n] keys are common to all. A query that sees no
  * key (or whose scores are all minus infinity) gets out = 0 and lse = -inf, and passes no gradient. What a
  * query does not see has no effect on it, infinities and NaN included.
  */

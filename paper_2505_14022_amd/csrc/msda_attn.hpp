@@ -402,7 +402,7 @@ struct Row32 {
 };
 
 // The keys of a staged tile as the rows' masks need them: the document, kCommon for one that all documents
-// see, or -1 for one that nobody sees.
+// see, or -1 for one that nobody sees, whichever negative document a caller gave it.
 constexpr int kCommon = -2;
 
 // Keys and values staged tile by tile, for kernels that own rows: two buffers in LDS, and the next tile in
@@ -526,7 +526,7 @@ struct KeyTiles {
 #pragma unroll
             for (int a = 0; a < Tile::kLoads; ++a) {
                 const int j = t * Tile::kRows + Tile::row(a);
-                if (!clean || masks) sh.doc[b][Tile::row(a)] = doc_x[a] >= 0 && j < w.common ? kCommon : doc_x[a];
+                if (!clean || masks) sh.doc[b][Tile::row(a)] = doc_x[a] < 0 ? -1 : j < w.common ? kCommon : doc_x[a];
                 if (BIASED) sh.pos[b][Tile::row(a)] = pos_x[a];
             }
         }

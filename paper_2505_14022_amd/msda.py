@@ -684,7 +684,7 @@ def attention_forward(q, k, v, scale=None, softcap: float = 0.0, slopes=None, q_
     q [N, Lq, M, D], k and v [N, Lk, Mkv, D], M a multiple of Mkv; views whose channels are contiguous are
     taken. scale: D ** -0.5 when None. softcap: cap of the scores (0: none). slopes [M], q_pos [N, Lq, 2] and
     k_pos [N, Lk, 2] (fp32): a bias of -slope times the distance. q_doc [N, Lq] and k_doc [N, Lk] (int32): queries see
-    the keys of their own document, -1 is padding. prefix [N] (int32): the first keys, common to all documents
+    the keys of their own document, negative ones are padding. prefix [N] (int32): the first keys, common to all documents
     and exempt from the order. causal: the last query sees every key, each one before it one fewer.
     workspace: "auto" allocates it, or a caller-owned uint8 tensor of attention_workspace_size bytes.
     """
