@@ -243,8 +243,8 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
         }
         if ((int)threadIdx.x < Tile::kRows) {
             const int x = g0 + (int)threadIdx.x, i = i0 + small_div(x, inv_g), head = w.kv * p.G + x - (i - i0) * p.G;
-            lse_x = kInf;  // rows past the last: p = 0
-            delta_x = 0.f;
+            lse_x = delta_x = slope_x = 0.f;
+            pos_x = make_float2(0.f, 0.f);
             last_x = doc_x = -1;
             if (r0 + (int)threadIdx.x < p.R) {
                 const int64_t at = ((int64_t)w.n * p.M + head) * p.Lq + i;
@@ -361,9 +361,10 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     for (int b = 0; ; b ^= 1) {
         if (t < 0) break;
         stage(b);
-        // rows past the last have p = 0, keys past the last are not written
+        // Rows past the last are hidden: their scores may be anything, as a key may hold an infinity. Keys past the last
+        // are not written.
         const int r0 = t * Tile::kRows;
-        bool whole = !p.causal || wave_last <= r0 / p.G + w.off || wave_last < w.common;
+        bool whole = r0 + Tile::kRows <= p.R && (!p.causal || wave_last <= r0 / p.G + w.off || wave_last < w.common);
         if (p.q_doc)
             whole = whole && rr.whole && ((one_doc && rr.lo == doc0 && rr.hi == doc0) || (no_pad && wave_last < w.common));
         __syncthreads();  // buffer b is written, and every wave has read the other one, which is next

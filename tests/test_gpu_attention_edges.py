@@ -2,6 +2,8 @@
 attention (tests/layer_ref.py)."""
 import pytest
 
+import layer_ref
+from layer_ref import assert_within
 from paper_2505_14022_amd import msda
 from gpu_util import require_gpu, say
 from test_gpu_attention import check, make, masks_of
@@ -34,3 +36,62 @@ def test_attention_any_negative_document_is_padding(dtype, D, prefix):
     how = masks_of(1, 90, 90, 2, docs="one", prefix=prefix)
     how["q_doc"][:, 70:] = how["k_doc"][:, 70:] = -2
     check(*make(1, 90, 90, 2, 2, D, dtype, seed=1), how)
+
+
+@pytest.mark.parametrize("dtype,D", [("f32", 32), ("f16", 64), ("bf16", 64), ("bf16", 128), ("bf16", 32)])
+def test_attention_padding_before_a_last_tile_in_part(dtype, D):
+    # padded queries at places that are no numbers, in the tile before the one that ends behind the last row
+    import torch
+
+    say(f"attention of left-padded queries without places, {dtype} D={D}")
+    for L in (70, 134, 200):
+        how = masks_of(1, L, L, 1, docs="one", bias=True)
+        how["q_doc"][:, :20] = -1
+        for bad in (float("nan"), float("inf")):
+            how["q_pos"][:, :20] = bad
+            check(*make(1, L, L, 1, 1, D, dtype, seed=L), how)
+
+
+def _without_key(L, M, key):
+    import torch
+
+    doc = torch.zeros(1, L, dtype=torch.int32, device="cuda")
+    k_doc = doc.clone()
+    k_doc[:, key] = -1
+    return {"q_doc": doc, "k_doc": k_doc}
+
+
+@pytest.mark.parametrize("dtype,D", [("f32", 32), ("f16", 64), ("bf16", 32), ("bf16", 128)])
+def test_attention_of_a_key_that_all_score_minus_infinity(dtype, D):
+    # such a key has no weight: grad_k and grad_v of all keys are as if it were padding
+    say(f"attention of a key with a score of minus infinity, {dtype} D={D}")
+    L, M, key, c = 70, 2, 37, 5
+    q, k, v, go = make(1, L, L, M, M, D, dtype, seed=3)
+    q[..., c] = q[..., c].abs() + 0.25
+    k[:, key, :, c] = float("-inf")
+    ref = layer_ref.attention(q, k, v, grad_out=go, **_without_key(L, M, key))
+    out, lse = msda.attention_forward(q, k, v)
+    _, gk, gv = msda.attention_backward(q, k, v, out, lse, go)
+    for name, t in (("out", out), ("lse", lse), ("grad_k", gk), ("grad_v", gv)):
+        assert_within(name, t, *ref[name])
+
+
+@pytest.mark.parametrize("dtype,D", [("f32", 32), ("f16", 64), ("bf16", 32), ("bf16", 128)])
+def test_attention_infinities_in_a_last_tile_in_part(dtype, D):
+    # the last rows and some keys of one document hold infinities; the other document's results have none
+    import torch
+
+    say(f"attention with infinities in the last rows, {dtype} D={D}")
+    L = 70
+    q, k, v, go = make(1, L, L, 2, 1, D, dtype, seed=4)
+    doc = (torch.arange(L) >= 60).int()[None].cuda()
+    how = {"q_doc": doc, "k_doc": doc, "causal": True}
+    for t in (q, k, v, go):
+        t[:, 65:, :, 1] = float("inf")
+        t[:, 66, :, 3] = float("nan")
+    ref = layer_ref.attention(q, k, v, grad_out=go, **how)
+    out, lse = msda.attention_forward(q, k, v, **how)
+    grads = msda.attention_backward(q, k, v, out, lse, go, **how)
+    for name, t in zip(("out", "grad_q", "grad_k", "grad_v"), (out,) + grads):
+        assert_within(name, t[:, :60], ref[name][0][:, :60], ref[name][1][:, :60])
+    assert not bool(torch.isfinite(out[:, 66:]).all())
