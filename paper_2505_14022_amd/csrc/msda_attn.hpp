@@ -224,6 +224,7 @@ struct Odd {
     // Adds what was noted to channels d .. d + 3 of the owner's result.
     __device__ __forceinline__ void apply(float (&x)[4], int d) const {
         if (!any) return;
+        wave_lds_sync();  // each half wave has noted every other word
         const uint32_t codes = mine[d >> 4] >> (2 * (d & 15));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {

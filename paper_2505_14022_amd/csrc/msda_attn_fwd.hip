@@ -105,6 +105,7 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW, sizeof(T))) void attn_fw
 
 #pragma unroll 1
         for (int sub = 0; sub < Tile::kRows; sub += 32 * Tile::kBlocks) body(b, j0, sub, !whole);
+        if constexpr (Keys::kBuffers == 1) wave_lds_sync();  // the wave has read the buffer, which is next again
     }
     l = halves_sum(l);
     if (own.row >= p.R) return;

@@ -95,3 +95,21 @@ def test_attention_infinities_in_a_last_tile_in_part(dtype, D):
     for name, t in zip(("out", "grad_q", "grad_k", "grad_v"), (out,) + grads):
         assert_within(name, t[:, :60], ref[name][0][:, :60], ref[name][1][:, :60])
     assert not bool(torch.isfinite(out[:, 66:]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("D", [20, 32, 64, 128])
+def test_attention_of_one_wave_over_many_tiles(D, dtype):
+    # up to 32 rows a head are one wave's, which stages every tile in the same place
+    import torch
+
+    say(f"attention of few rows over many tiles, {dtype} D={D}")
+    for rows, Lk in ((1, 333), (4, 1999), (8, 640)):
+        q, k, v, go = make(1, rows, Lk, 8, 2, D, dtype, seed=Lk)
+        v += torch.arange(Lk, device="cuda")[None, :, None, None].to(v.dtype) % 17 - 8  # a tile read late shows
+        how = masks_of(1, rows, Lk, 8, causal=True)
+        first = check(q, k, v, go, how, backward=False)
+        v[:, 100, 1, 3] = float("inf")  # noted by one half wave, added by both
+        out = msda.attention_forward(q, k, v, **how)[0]
+        assert torch.equal(out[..., :3], first["out"][..., :3]) and torch.equal(out[..., 4:], first["out"][..., 4:])
+        assert bool((out[:, :, 4:, 3] == float("inf")).all()) and torch.equal(out[:, :, :4], first["out"][:, :, :4])
