@@ -339,7 +339,8 @@ msda_status_t msda_layernorm_backward(const void* x, const void* residual, const
  *   freqs  [A, R] fp32
  * out == x with the same strides rotates in place; otherwise they must not overlap. An output stride
  * of 0 over more than one entry is MSDA_ERROR_INVALID_VALUE. 1 <= A <= 4, 0 <= 2R <= D;
- * D > MSDA_ROTARY_MAX_D or M * D > 65536 is MSDA_ERROR_NOT_SUPPORTED. N * T == 0 is a no-op.
+ * D > MSDA_ROTARY_MAX_D, M * D > 65536 or a batch item of 2^24 workgroups (each a token of more than 512 16-byte
+ * pieces or pairs, or up to 1024 of those) is MSDA_ERROR_NOT_SUPPORTED. N * T == 0 is a no-op.
  */
 #define MSDA_ROTARY_MAX_D 1024
 msda_status_t msda_rotary_forward(const void* x, const int64_t* x_stride, const float* pos,
@@ -368,7 +369,10 @@ msda_status_t msda_rotary_backward(const void* grad_out, const int64_t* grad_out
  */
 typedef struct {
     int64_t N, Lq, Lk, M, Mkv, D; /* M a multiple of Mkv, at most 32768; 1 <= D <= MSDA_ATTENTION_MAX_D; */
-                                  /* Lk and Lq * M / Mkv below 2^31 - 1024; more: NOT_SUPPORTED       */
+                                  /* Lk and Lq * M / Mkv below 2^31 - 1024; fewer than 2^24 blocks of  */
+                                  /* 128 rows or keys of a key head (2^26 of at most 32 rows in the    */
+                                  /* forward), N times the tables' runs of documents below 2^26 and    */
+                                  /* copied 16-byte pieces below 2^32; more: NOT_SUPPORTED             */
     int dtype;                    /* of q, k, v, out and the gradients                                */
     int causal;                   /* nonzero: the order rule above; needs Lk >= Lq                    */
     int unaligned;                /* nonzero: q, k and v may start off 16-byte boundaries; see below  */

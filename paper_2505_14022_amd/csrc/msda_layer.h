@@ -50,6 +50,7 @@ struct RotaryParams {
     bool interleaved, vec;      // vec: 16-byte pieces of pairs and of copied channels
     float sign;                 // 1 forward, -1 backward
 };
+int64_t rotary_workgroups(const RotaryParams& p, int dtype);  // of a launch for one batch item
 hipError_t launch_rotary(const RotaryParams& p, int dtype, hipStream_t stream);
 
 // ---------------------------------------------------------------- dense attention

@@ -16,6 +16,8 @@ using msda::ok;
 namespace {
 
 constexpr int64_t kMaxInt = 0x7fffffff;
+constexpr int64_t kMaxWorkItems = 0xffffffff;             // of a grid: the runtime takes fewer than 2^32
+constexpr int64_t kMaxWorkgroups = kMaxWorkItems / 256;   // of 256
 
 msda_status_t check_dtype(int dtype) {
     if (dtype != MSDA_F32 && dtype != MSDA_F16 && dtype != MSDA_BF16)
@@ -194,6 +196,9 @@ msda_status_t rotary(const char* in_name, const void* x, const int64_t* x_stride
     p.interleaved = interleaved != 0;
     p.vec = pieces && R % per == 0 && D % per == 0;
     p.sign = sign;
+    if (msda::rotary_workgroups(p, dtype) > kMaxWorkgroups)
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "T=%lld tokens of M*D=%lld channels are too many for one launch", (long long)T,
+                    (long long)(M * D));
     hipError_t e = msda::launch_rotary(p, dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "rotary launch: %s", hipGetErrorString(e));
     return ok();
@@ -250,8 +255,8 @@ msda_status_t check_attention(const msda_attention_t* a) {
         return fail(MSDA_ERROR_NOT_SUPPORTED, "M=%lld heads exceeds 32768", (long long)a->M);
     if (a->N > kMaxInt || a->Lk > kMaxInt - 1024 || a->Lq > (kMaxInt - 1024) / (a->M / a->Mkv))
         return fail(MSDA_ERROR_NOT_SUPPORTED, "N, Lk or Lq * M / Mkv exceeds 2^31");
-    // every launch is one grid: at most 2^30 slabs (batch item, key head) and 2^33 of their rows or keys, in at
-    // least 32 per workgroup of the attention kernels and 4 of the ones that add splits
+    // slabs (batch item, key head) and their rows and keys: what is counted from them stays within 64 bits, and
+    // check_launches looks at the grids
     const double slabs = (double)a->N * (double)a->Mkv, rows = (double)a->Lq * (double)(a->M / a->Mkv);
     if (slabs > 1073741824.0 || slabs * rows > 8589934592.0 || slabs * (double)a->Lk > 8589934592.0)
         return fail(MSDA_ERROR_NOT_SUPPORTED, "N * Mkv heads of these lengths are too many for one launch");
@@ -355,6 +360,28 @@ Attention attention_of(const msda_attention_t& a, bool backward) {
     }
     x.bytes = at + part * sizeof(float);
     return x;
+}
+
+// Every launch is one grid: a call that needs a larger one than the runtime takes is refused before any of its kernels is
+// enqueued.
+msda_status_t check_launches(const Attention& x, const msda_attention_t& a, bool backward) {
+    const int64_t slabs = a.N * a.Mkv, DP = msda::attn_channels((int)a.D);
+    int64_t most = 0;
+    auto launch = [&](int64_t items) { most = items > most ? items : most; };
+    const msda::AttnPlan* plans[2] = {&x.rows, &x.keys};
+    for (int i = 0; i < 2; ++i) {
+        const msda::AttnPlan& plan = *plans[i];
+        launch(ceil_div(slabs * plan.blocks * plan.splits, 8) * 8 * 64 * plan.waves);
+        // four channels of each result a lane, or in the forward's join up to a wave for a row
+        if (plan.splits > 1) launch(i ? slabs * a.Lk * 2 * (DP / 4) : slabs * x.p.R * (backward ? DP / 4 : 64));
+    }
+    if (x.p.q_doc) launch(a.N * (x.rows.tiles + x.rows.blocks + x.keys.tiles + x.keys.blocks) * 64);
+    for (int i = 0; i < 5; ++i)
+        if (x.pack[i]) launch(a.N * (i == 1 || i == 2 ? a.Lk * a.Mkv : a.Lq * a.M) * (x.width * dtype_size(a.dtype) / 16));
+    if (most + 255 > kMaxWorkItems)
+        return fail(MSDA_ERROR_NOT_SUPPORTED, "N * Mkv heads of these lengths are too many for one launch (%lld work items)",
+                    (long long)most);
+    return MSDA_SUCCESS;
 }
 
 // Whether 16-bit rows may have so few keys that their delta is formed with care, in a launch of its own.
@@ -465,7 +492,11 @@ msda_status_t msda_attention_workspace_size(const msda_attention_t* a, int backw
     *bytes = 0;
     msda_status_t st = check_attention(a);
     if (st != MSDA_SUCCESS) return st;
-    if (a->N > 0) *bytes = attention_of(*a, backward != 0).bytes;
+    if (a->N > 0) {
+        const Attention x = attention_of(*a, backward != 0);
+        if ((st = check_launches(x, *a, backward != 0)) != MSDA_SUCCESS) return st;
+        *bytes = x.bytes;
+    }
     return ok();
 }
 
@@ -479,6 +510,7 @@ msda_status_t msda_attention_forward(const msda_attention_t* a, const void* q, c
     if (!is_aligned(out, 16) || !is_aligned(lse, 4))
         return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: out needs 16 bytes, lse 4");
     Attention x = attention_of(*a, false);
+    if ((st = check_launches(x, *a, false)) != MSDA_SUCCESS) return st;
     if ((st = check_bases(*a, x, q, k, v)) != MSDA_SUCCESS) return st;
     if ((st = check_workspace(x, workspace, workspace_bytes)) != MSDA_SUCCESS) return st;
     hipError_t e = bind(x, *a, q, k, v, nullptr, nullptr, workspace, (hipStream_t)stream);
@@ -505,6 +537,7 @@ msda_status_t msda_attention_backward(const msda_attention_t* a, const void* q, 
         !is_aligned(grad_k, 16) || !is_aligned(grad_v, 16))
         return fail(MSDA_ERROR_INVALID_VALUE, "misaligned pointer: out and the gradients need 16 bytes, lse 4");
     Attention x = attention_of(*a, true);
+    if ((st = check_launches(x, *a, true)) != MSDA_SUCCESS) return st;
     if ((st = check_bases(*a, x, q, k, v)) != MSDA_SUCCESS) return st;
     if ((st = check_workspace(x, workspace, workspace_bytes)) != MSDA_SUCCESS) return st;
     hipError_t e = bind(x, *a, q, k, v, out, grad_out, workspace, (hipStream_t)stream);

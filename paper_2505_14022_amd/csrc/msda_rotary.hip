@@ -137,16 +137,22 @@ __global__ __launch_bounds__(256) void rotary_pairs_kernel(RotaryParams p, int t
     }
 }
 
-template <typename T, int VEC>
-hipError_t launch_typed(const RotaryParams& p, hipStream_t stream) {
-    const int items = VEC > 1 ? p.D / VEC : p.D - p.R;  // of a head
-    // tokens per workgroup: about four items a thread, as many pairs as LDS holds, and enough workgroups
+// What a head is to the threads: pieces of `vec` channels, or pairs and copied channels.
+int items_of_head(const RotaryParams& p, int vec) { return vec > 1 ? p.D / vec : p.D - p.R; }
+
+// Tokens per workgroup: about four items a thread, as many pairs as LDS holds, and enough workgroups.
+int tokens_of_workgroup(const RotaryParams& p, int items) {
     int tokens = 1024 / (items * p.M);
     if (p.R > 0 && tokens > kPairs / p.R) tokens = kPairs / p.R;
     if (tokens < 1) tokens = 1;
     while (tokens > 1 && (p.T + tokens - 1) / tokens * p.N < 1024) tokens = (tokens + 1) / 2;
+    return tokens;
+}
+
+template <typename T, int VEC>
+hipError_t launch_typed(const RotaryParams& p, hipStream_t stream) {
+    const int items = items_of_head(p, VEC), tokens = tokens_of_workgroup(p, items);
     const int64_t gx = (p.T + tokens - 1) / tokens;
-    if (gx > 0x7fffffff) return hipErrorInvalidValue;
     const int most = 65535;  // batch items of a launch
     for (int n0 = 0; n0 < p.N; n0 += most) {
         RotaryParams c = p;
@@ -166,6 +172,11 @@ hipError_t launch_typed(const RotaryParams& p, hipStream_t stream) {
 }
 
 }  // namespace
+
+int64_t rotary_workgroups(const RotaryParams& p, int dtype) {
+    const int tokens = tokens_of_workgroup(p, items_of_head(p, p.vec ? 16 / dtype_size(dtype) : 1));
+    return (p.T + tokens - 1) / tokens;
+}
 
 hipError_t launch_rotary(const RotaryParams& p, int dtype, hipStream_t stream) {
     if (dtype == MSDA_F32) return p.vec ? launch_typed<float, 4>(p, stream) : launch_typed<float, 1>(p, stream);

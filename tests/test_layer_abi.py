@@ -202,3 +202,33 @@ def test_python_checks_its_tensors(L):
         msda.attention_forward(q, q, q)
     with pytest.raises(ValueError, match="k must be|q must be"):
         msda.attention_forward(q, x, x)
+
+
+def attention_size(L, grads, **kw):
+    size = ctypes.c_size_t(0)
+    return L.msda_attention_workspace_size(ctypes.byref(description(**kw)), grads, ctypes.byref(size))
+
+
+@pytest.mark.parametrize("most,grads,kw", [
+    # a workgroup of 256 a head in the backward, of 64 in the forward of few rows
+    (2 ** 21 - 1, 1, dict(M=8, Mkv=8, Lq=1, Lk=1)), (2 ** 23 - 1, 0, dict(M=8, Mkv=8, Lq=1, Lk=1)),
+    # tables of documents, a wave for each tile and block of a batch item: 2 in the forward, 4 with the backward's
+    (2 ** 25 - 2, 0, dict(M=1, Mkv=1, Lq=1, Lk=1, q_doc=0x100, k_doc=0x200)),
+    # copies of 16 bytes, of 2^22 an item here
+    (2 ** 10 - 1, 0, dict(M=32, Mkv=4, Lq=2 ** 15, Lk=100, unaligned=1)),
+])
+def test_attention_refuses_grids_that_the_runtime_does_not_take(L, no_gpu, most, grads, kw):
+    call = backward if grads else forward
+    assert attention_size(L, grads, N=most, **kw) == OK
+    for n in (most + 1, most + 9, 2 * most):
+        assert attention_size(L, grads, N=n, **kw) == UNSUPPORTED and "launch" in msda.last_error()
+        # with all pointers and a workspace said to be large enough: refused before anything is enqueued
+        assert call(L, description(N=n, **kw), nbytes=1 << 60) == UNSUPPORTED and "launch" in msda.last_error()
+
+
+@pytest.mark.parametrize("entry", ["msda_rotary_forward", "msda_rotary_backward"])
+@pytest.mark.parametrize("kw", [dict(M=8, D=1024, R=0, dtype=1), dict(M=8, D=1024, R=64, dtype=0, x=0x1004),
+                                dict(M=513, D=1, R=0, dtype=2)])
+def test_rotary_refuses_grids_that_the_runtime_does_not_take(L, no_gpu, entry, kw):
+    assert rotary(L, entry=entry, N=1, T=2 ** 24, A=1, items=1, **kw) == UNSUPPORTED and "launch" in msda.last_error()
+    assert rotary(L, entry=entry, N=1, T=2 ** 24 - 1, A=1, items=1, **kw) == msda.MSDA_ERROR_LAUNCH_FAILED  # there is no GPU
