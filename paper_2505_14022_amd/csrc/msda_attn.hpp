@@ -513,6 +513,10 @@ struct KeyTiles {
 #pragma unroll
                 for (int a = 0; a < Tile::kLoads; ++a) {
                     uint4& x = SUM_VALUES ? vx[a] : kx[a];
+                    if (!SUM_VALUES) {  // such a key is nobody's: see attn_grad_q_kernel
+                        const uint64_t row = __ballot(not_finite<T>(x)) >> (lane / Tile::kChunks * Tile::kChunks);
+                        if (row & (((uint64_t)1 << Tile::kChunks) - 1)) doc_x[a] = -1;
+                    }
                     x = finite_only<T>(x);
                 }
             }
@@ -541,12 +545,9 @@ struct KeyTiles {
         }
         return some;
     }
-    // Notes what the weights of the block of 32 keys from key j0 on meet that was not finite in buffer b.
+    // Notes what the weights of the block of 32 values from key j0 on meet that was not finite in buffer b.
     __device__ __forceinline__ void note_odd(Odd<DP>& odd, const acc_t& weight, int b, int j0) const {
-        if (any_odd(b))
-            odd.template note<T>(weight, p.D, lane, [&](int r) {
-                return SUM_VALUES ? v + (j0 + r) * p.vs[1] : k + (j0 + r) * p.ks[1];
-            });
+        if (any_odd(b)) odd.template note<T>(weight, p.D, lane, [&](int r) { return v + (j0 + r) * p.vs[1]; });
     }
     // Whether all rows of the wave see all keys of the tile just loaded.
     __device__ __forceinline__ bool whole(const Row32& own) const {

@@ -32,13 +32,16 @@ constexpr int grad_kv_waves(int DP) { return DP == 32 ? 3 : DP == 64 ? 2 : 1; }
 // are causal, and mends the delta of rows whose keys were all among them. A row of n keys gains 1 part in n of its
 // error, so there is nothing to be had of longer ones. 11 us in the first shape above and 33 in the second; grad_q reads
 // delta in place of out then.
+//
+// In calls with masks, a key that holds an infinity or a NaN is taken as hidden: its products with zeros (of pairs that
+// are) must not reach grad_q, and nothing else is lost. A row that sees it has a score of minus infinity, or of plus or minus
+// the cap, with which it passes no gradient; or one of plus infinity or NaN, and then its lse is NaN and so is its gradient.
 template <typename T, int DP, int NW, int EXTRAS, bool DELTA>
 __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP == 32)) void attn_grad_q_kernel(AttnParams p) {
     using O = Op<T>;
     using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, false, DELTA ? 1 : 2>;
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
-    __shared__ uint32_t odd_words[32 * NW * Odd<DP>::kWords];
     Work w(p, true);
     if (!w.any) return;
     const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
@@ -77,8 +80,6 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
     for (int r = 0; r < 16; ++r) minus_delta[r] = -delta;  // where the sums of dP begin
 #pragma unroll
     for (int u = 0; u < DP / 32; ++u) gq[u] = acc_t{};
-    Odd<DP> odd;
-    odd.start(odd_words, wave * 32 + (lane & 31), lane, p.q_doc || p.causal);
     float mass = 0.f, lack = 0.f;
     auto body = [&](int b, int j0, int sub, bool partial) {  // the tile's keys from sub on
 #pragma unroll
@@ -117,7 +118,6 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
                 ds = x[0];
             }
             add_product<T, DP>(gq, ds, kt, Tile::kStride, lane);
-            keys.note_odd(odd, ds, b, j0 + sub + kb * 32);
         }
     };
     keys.fetch();
@@ -126,9 +126,10 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
         const bool whole = keys.whole(own);
         const int j0 = keys.t * Tile::kRows;
         __syncthreads();  // buffer b is written, and every wave has read the other one, which is next
+        const bool partial = !whole || keys.any_odd(b);
         keys.fetch();
 #pragma unroll 1
-        for (int sub = 0; sub < Tile::kRows; sub += 32 * Tile::kBlocks) body(b, j0, sub, !whole);
+        for (int sub = 0; sub < Tile::kRows; sub += 32 * Tile::kBlocks) body(b, j0, sub, partial);
         if constexpr (DELTA) {
             if (--visits == 0) break;
             __syncthreads();  // every wave has read the buffer
@@ -151,8 +152,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
             const int d = u * 32 + 8 * g + 4 * h;
             float x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = gq[u][4 * g + e] * p.scale;
-            odd.apply(x, d);
+            for (int e = 0; e < 4; ++e) x[e] = lse == lse ? gq[u][4 * g + e] * p.scale : lse;
             if (p.splits > 1) *reinterpret_cast<float4*>(part + d) = make_float4(x[0], x[1], x[2], x[3]);
             else store_four(out, d, p.D, x);
         }

@@ -113,3 +113,41 @@ def test_attention_of_one_wave_over_many_tiles(D, dtype):
         out = msda.attention_forward(q, k, v, **how)[0]
         assert torch.equal(out[..., :3], first["out"][..., :3]) and torch.equal(out[..., 4:], first["out"][..., 4:])
         assert bool((out[:, :, 4:, 3] == float("inf")).all()) and torch.equal(out[:, :, :4], first["out"][:, :, :4])
+
+
+@pytest.mark.parametrize("softcap", [0.0, 3.0])
+@pytest.mark.parametrize("dtype,D", [("f32", 32), ("f16", 64), ("bf16", 32), ("bf16", 128), ("f32", 128)])
+def test_attention_masked_with_a_seen_key_of_minus_infinity(dtype, D, softcap):
+    # a masked call's key that all who see it give a score of minus infinity, or of minus the cap: grad_q as without it
+    # or, capped, as with a key far out; and NaN where it is seen with a score that is none
+    import torch
+
+    say(f"attention, masked, with a seen key of minus infinity, {dtype} D={D} softcap {softcap}")
+    L, M, key, c = 128, 2, 37, 5
+    q, k, v, go = make(1, L, L, M, M, D, dtype, seed=3)
+    q[..., c] = q[..., c].abs() + 0.25
+    how = {"causal": True, "softcap": softcap}
+    k[:, key, :, c] = -30000.0
+    ref = layer_ref.attention(q, k, v, grad_out=go, **how)
+    k[:, key, :, c] = float("-inf")
+    out, lse = msda.attention_forward(q, k, v, **how)
+    gq, gk, gv = msda.attention_backward(q, k, v, out, lse, go, **how)
+    rest = [d for d in range(D) if d != c]
+    for name, t in (("out", out), ("grad_q", gq[..., rest]), ("grad_k", gk), ("grad_v", gv)):
+        value, bound = ref[name]
+        if name == "grad_q":
+            value, bound = value[..., rest], bound[..., rest]
+        if softcap == 0.0:  # from layer_ref of the call without the key: the rounding of a score of 30000 is not there
+            plain = layer_ref.attention(q, k, v, grad_out=go, q_doc=torch.zeros(1, L).int(), softcap=softcap, causal=True,
+                                        k_doc=-(torch.arange(L) == key).int()[None])
+            value, bound = plain[name]
+            if name == "grad_q":
+                value, bound = value[..., rest], bound[..., rest]
+        assert_within(name, t, value, bound)
+    q[:, 100:, :, c] = -q[:, 100:, :, c]  # a score of plus infinity from query 100 on
+    out, lse = msda.attention_forward(q, k, v, **how)
+    gq = msda.attention_backward(q, k, v, out, lse, go, **how)[0]
+    if softcap == 0.0:
+        assert bool(torch.isnan(gq[:, 100:]).all()) and bool(torch.isfinite(gq[:, :100][..., rest]).all())
+    else:
+        assert bool(torch.isfinite(gq[..., rest]).all())
