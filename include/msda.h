@@ -365,7 +365,9 @@ msda_status_t msda_rotary_backward(const void* grad_out, const int64_t* grad_out
  *   order:     not causal; or j <= i + Lk - Lq (the last query sees every key); or j < prefix[n]
  * so any negative document is padding, and the first prefix[n] keys are common to all. A query that sees no
  * key (or whose scores are all minus infinity) gets out = 0 and lse = -inf, and passes no gradient. What a
- * query does not see has no effect on it, infinities and NaN included.
+ * query does not see has no effect on it, infinities and NaN included. Those that it does see reach it as in
+ * the formulas (which of NaN and an infinity, is not fixed), but in calls with documents or an order a pair whose
+ * weight is exactly 0 adds nothing, where 0 times an infinity is NaN.
  */
 typedef struct {
     int64_t N, Lq, Lk, M, Mkv, D; /* M a multiple of Mkv, at most 32768; 1 <= D <= MSDA_ATTENTION_MAX_D; */

@@ -305,6 +305,25 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     Odd<DP> odd_k, odd_v;
     odd_k.start(odd_words[0], wave * 32 + (lane & 31), lane, masks);
     odd_v.start(odd_words[1], wave * 32 + (lane & 31), lane, masks);
+    // A query that holds an infinity has weights where its scores are capped; the staged copy, which is summed over, is
+    // without the infinity. Adds what it gives to the scores of 32 rows from `first` on.
+    const T* own_key = static_cast<const T*>(p.k) + w.n * p.ks[0] + j * p.ks[1] + w.kv * p.ks[2];
+    auto add_infinities = [&](acc_t& s, int first) {
+#pragma unroll 1
+        for (int r = 0; r < 16; ++r) {
+            const int row = first + block_row(r, h);
+            if (row >= p.R) continue;
+            const T* qr = query_row(row);
+            float more = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < p.D; ++c) {
+                const float x = (float)qr[c];
+                if (!(fabsf(x) < kInf)) more += x * (float)own_key[c];
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] += i == r ? more : 0.f;
+        }
+    };
     auto body = [&](int b, int r0, int sub, int some, bool partial) {  // the tile's rows from sub on
 #pragma unroll
         for (int block = 0; block < Tile::kBlocks; ++block) {
@@ -317,7 +336,10 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             acc_t s = row_product<T, DP>(qt, Tile::kStride, k, lane, p.D, acc_t{});
             ds = row_product<T, DP>(gt, Tile::kStride, v, lane, p.D, ds);
             float unit = p.scale * kLog2e;
-            if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s, &ds);
+            if constexpr (EXTRAS >= kCap) {
+                if (some) add_infinities(s, r0 + first);
+                unit = cap_scores<T, EXTRAS>(p, s, &ds);
+            }
             if constexpr (EXTRAS == kBias) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {

@@ -151,3 +151,23 @@ def test_attention_masked_with_a_seen_key_of_minus_infinity(dtype, D, softcap):
         assert bool(torch.isnan(gq[:, 100:]).all()) and bool(torch.isfinite(gq[:, :100][..., rest]).all())
     else:
         assert bool(torch.isfinite(gq[..., rest]).all())
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("dtype,D", [("f32", 32), ("f16", 64), ("bf16", 32), ("bf16", 128), ("f32", 48)])
+def test_attention_masked_and_capped_with_an_infinite_query(dtype, D, bias):
+    # its scores are plus and minus the cap, its weights numbers: as with a query far out
+    say(f"attention, masked and capped, with an infinite query, {dtype} D={D} bias {bias}")
+    L, M, row, c = 128, 2, 90, 5
+    q, k, v, go = make(1, L, L, M, M, D, dtype, seed=5)
+    k[..., c] += k[..., c].sign() * 0.25
+    how = masks_of(1, L, L, M, docs="runs", causal=True, softcap=2.0, bias=bias)
+    q[:, row, :, c] = 30000.0
+    ref = layer_ref.attention(q, k, v, grad_out=go, **how)
+    q[:, row, :, c] = float("inf")
+    out, lse = msda.attention_forward(q, k, v, **how)
+    gq, gk, gv = msda.attention_backward(q, k, v, out, lse, go, **how)
+    rest = [d for d in range(D) if d != c]
+    for name, t in (("out", out), ("lse", lse), ("grad_q", gq), ("grad_v", gv)):
+        assert_within(name, t, *ref[name])
+    assert_within("grad_k", gk[..., rest], *(x[..., rest] for x in ref["grad_k"]))
