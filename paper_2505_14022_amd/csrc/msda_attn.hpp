@@ -303,6 +303,11 @@ struct TileWalk {
         }
         return true;
     }
+    // Drops the tiles found so far that `test` does not accept any more.
+    template <typename F>
+    __device__ __forceinline__ void test_again(int lane, F test) {
+        left &= __ballot(test(at - 64 + lane, held));
+    }
     // The next tile or -1; its documents into `of` (with `ranges`).
     template <typename F>
     __device__ __forceinline__ int next(int lane, const int4* ranges, Range& of, F test) {
@@ -409,12 +414,13 @@ constexpr int kCommon = -2;
 // Keys and values staged tile by tile, for kernels that own rows: two buffers in LDS, and the next tile in
 // registers while the waves work on the current one. All loads of a tile are issued together; what must not
 // count (keys past the last, padding) is dropped when the tile is put into LDS.
-// SUM_VALUES: the kernel sums over the values (forward), else over the keys (grad_q).
+// SUMMED: what the kernel sums over: the values (forward), the keys (grad_q) or nothing (delta).
 // BUFFERS 1: for a lone wave, which has read a tile before it writes the next, so that twice as many waves fit, and
 // for kernels that wait before they write.
-template <typename T, int DP, int NW, bool BIASED, bool SUM_VALUES, int BUFFERS = NW == 1 ? 1 : 2>
+enum Summed { kValues, kKeys, kNothing };
+template <typename T, int DP, int NW, bool BIASED, Summed SUMMED, int BUFFERS = NW == 1 ? 1 : 2>
 struct KeyTiles {
-    using Tile = TileOf<T, DP, NW, !SUM_VALUES>;
+    using Tile = TileOf<T, DP, NW, SUMMED != kValues>;
     static constexpr int kBuffers = BUFFERS;
     struct Shared {
         T k[kBuffers][Tile::kElems], v[kBuffers][Tile::kElems];
@@ -453,6 +459,11 @@ struct KeyTiles {
     // Whether the workgroup's rows see any of its run of tiles.
     __device__ __forceinline__ bool any() {
         return w.walk.more(lane, w.tile_ranges(p), [&](int u, Range of) { return sees(p, w, i_last, w.docs, u * Tile::kRows, of); });
+    }
+    // Leaves the tiles that rows of documents `docs` do not see. (The tile that has been fetched stays.)
+    __device__ __forceinline__ void only(Range docs) {
+        w.docs = docs;
+        w.walk.test_again(lane, [&](int u, Range of) { return sees(p, w, i_last, w.docs, u * Tile::kRows, of); });
     }
     // Finds the next tile that the workgroup's rows see, and loads it.
     __device__ __forceinline__ void fetch() {
@@ -504,16 +515,16 @@ struct KeyTiles {
                 if (doc_x[a] < 0) kx[a] = vx[a] = make_uint4(0, 0, 0, 0);
             }
         }
-        if (masks) {
+        if (masks && SUMMED != kNothing) {
             bool odd = false;
 #pragma unroll
-            for (int a = 0; a < Tile::kLoads; ++a) odd |= not_finite<T>(SUM_VALUES ? vx[a] : kx[a]);
+            for (int a = 0; a < Tile::kLoads; ++a) odd |= not_finite<T>(SUMMED == kValues ? vx[a] : kx[a]);
             const bool some = __any(odd);
             if (some) {
 #pragma unroll
                 for (int a = 0; a < Tile::kLoads; ++a) {
-                    uint4& x = SUM_VALUES ? vx[a] : kx[a];
-                    if (!SUM_VALUES) {  // such a key is nobody's: see attn_grad_q_kernel
+                    uint4& x = SUMMED == kValues ? vx[a] : kx[a];
+                    if (SUMMED == kKeys) {  // such a key is nobody's: see attn_grad_q_kernel
                         const uint64_t row = __ballot(not_finite<T>(x)) >> (lane / Tile::kChunks * Tile::kChunks);
                         if (row & (((uint64_t)1 << Tile::kChunks) - 1)) doc_x[a] = -1;
                     }

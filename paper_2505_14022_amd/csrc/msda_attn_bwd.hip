@@ -25,28 +25,19 @@ constexpr int kProbShift = std::is_same_v<T, _Float16> ? 8 : 0;
 constexpr int grad_q_waves(int DP, size_t element) { return DP == 32 ? 3 : DP == 128 && element == 4 ? 1 : 2; }
 constexpr int grad_kv_waves(int DP) { return DP == 32 ? 3 : DP == 64 ? 2 : 1; }
 
-// Where a row has few keys, dP - delta is small beside dP, and the rounding of out to 16 bits, which delta holds, is
-// the largest part of the gradients' error: of two keys, grad_q and grad_k were 4 times as far off as by their own
-// roundings. As a row's probabilities add up to one, sum_j P (dP - delta) is what delta lacks. DELTA: the kernel forms
-// that sum in place of grad_q, and writes delta. It visits 128 keys, those at the block's own queries where rows
-// are causal, and mends the delta of rows whose keys were all among them. A row of n keys gains 1 part in n of its
-// error, so there is nothing to be had of longer ones. 11 us in the first shape above and 33 in the second; grad_q reads
-// delta in place of out then.
-//
 // In calls with masks, a key that holds an infinity or a NaN is taken as hidden: its products with zeros (of pairs that
 // are) must not reach grad_q, and nothing else is lost. A row that sees it has a score of minus infinity, or of plus or minus
 // the cap, with which it passes no gradient; or one of plus infinity or NaN, and then its lse is NaN and so is its gradient.
-template <typename T, int DP, int NW, int EXTRAS, bool DELTA>
-__global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP == 32)) void attn_grad_q_kernel(AttnParams p) {
+template <typename T, int DP, int NW, int EXTRAS>
+__global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_grad_q_kernel(AttnParams p) {
     using O = Op<T>;
-    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, false, DELTA ? 1 : 2>;
+    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, kKeys>;
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
     Work w(p, true);
     if (!w.any) return;
     const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
     Keys keys(sh, p, w, lane);
-    if (DELTA && p.causal) w.walk.at = max(w.block * 32 * NW / p.G + w.off, 0) / Tile::kRows;
     const bool any = w.note_split(p, keys.any());
     if (!any && w.split > 0) return;  // the first split writes delta
     const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS == kBias);
@@ -61,12 +52,12 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
             const int d = c * O::K + h * (O::K / 2);
             q[c] = __builtin_bit_cast(typename O::Frag, load_chunk(qr, d, p.D));
             go[c] = __builtin_bit_cast(typename O::Frag, load_chunk(gr, d, p.D));
-            if (!DELTA && p.delta_known) continue;
+            if (p.delta_known) continue;
             const auto o = __builtin_bit_cast(typename O::Frag, load_chunk(orow, d, p.D));
 #pragma unroll
             for (int e = 0; e < O::K / 2; ++e) delta += (float)go[c][e] * (float)o[e];
         }
-        if (!DELTA && p.delta_known) {
+        if (p.delta_known) {
             delta = p.delta[own.stat];
         } else {
             delta = halves_sum(delta);
@@ -80,7 +71,6 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
     for (int r = 0; r < 16; ++r) minus_delta[r] = -delta;  // where the sums of dP begin
 #pragma unroll
     for (int u = 0; u < DP / 32; ++u) gq[u] = acc_t{};
-    float mass = 0.f, lack = 0.f;
     auto body = [&](int b, int j0, int sub, bool partial) {  // the tile's keys from sub on
 #pragma unroll
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
@@ -88,7 +78,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
             acc_t s = row_product<T, DP>(kt, Tile::kStride, q, lane, p.D, acc_t{});
             acc_t ds = row_product<T, DP>(sh.v[b] + (sub + kb * 32) * Tile::kStride, Tile::kStride, go, lane, p.D, minus_delta);
             float unit = p.scale * kLog2e;
-            if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s, DELTA ? nullptr : &ds);
+            if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s, &ds);
             if constexpr (EXTRAS == kBias) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -97,18 +87,6 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
                     s[r] = s[r] * unit - own.slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
                 }
                 unit = 1.f;
-            }
-            if constexpr (DELTA) {
-                acc_t x[1];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) x[0][r] = exp2_of(__builtin_fmaf(s[r], unit, -lse));
-                if (partial) hide(x, 0.f, sub + kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    mass += x[0][r];
-                    if (x[0][r] > 0.f) lack += x[0][r] * ds[r];  // padding's dP may be anything
-                }
-                continue;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) ds[r] *= exp2_of(__builtin_fmaf(s[r], unit, -lse));
@@ -121,7 +99,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
         }
     };
     keys.fetch();
-    for (int b = 0, visits = 128 / Tile::kRows; keys.t >= 0; b ^= Keys::kBuffers - 1) {
+    for (int b = 0; keys.t >= 0; b ^= 1) {
         keys.stage(b);
         const bool whole = keys.whole(own);
         const int j0 = keys.t * Tile::kRows;
@@ -130,17 +108,6 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
         keys.fetch();
 #pragma unroll 1
         for (int sub = 0; sub < Tile::kRows; sub += 32 * Tile::kBlocks) body(b, j0, sub, partial);
-        if constexpr (DELTA) {
-            if (--visits == 0) break;
-            __syncthreads();  // every wave has read the buffer
-        }
-    }
-    if constexpr (DELTA) {
-        mass = halves_sum(mass);
-        lack = halves_sum(lack);
-        // an eighth of a step of out's: probabilities that add up to less have keys elsewhere
-        if (h == 0 && own.row < p.R && fabsf(mass - 1.f) < 0x1p-12f && fabsf(lack) < kInf) p.delta[own.stat] = delta + lack;
-        return;
     }
     if (own.row >= p.R) return;
     float* part = p.part + (((int64_t)w.slab * p.R + own.row) * p.splits + w.split) * DP;
@@ -156,6 +123,134 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T)) + (DELTA && DP
             if (p.splits > 1) *reinterpret_cast<float4*>(part + d) = make_float4(x[0], x[1], x[2], x[3]);
             else store_four(out, d, p.D, x);
         }
+}
+
+// Where a row has few keys, dP - delta is small beside dP, and the rounding of out to 16 bits, which delta holds, is
+// the largest part of the gradients' error: of two keys, grad_q and grad_k were 4 times as far off as by their own
+// roundings. As a row's probabilities add up to one, sum_j P (dP - delta) is what delta lacks. This kernel writes delta, and
+// mends that of the rows that see at most kFewKeys keys: a row of n keys gains 1 part in n of its error, so there is nothing
+// to be had of longer ones. A workgroup walks over the tiles that its rows see, wherever they are, and leaves those that only
+// rows with more keys see: long rows cost it a tile or two, or none where the tables of documents say that they are. A
+// row is mended once all of its keys have been visited: one that is left out may have a value that outweighs its probability.
+template <typename T, int DP, int NW, int EXTRAS>
+__global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_delta_kernel(AttnParams p) {
+    using O = Op<T>;
+    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, kNothing, 1>;
+    using Tile = typename Keys::Tile;
+    __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
+    __shared__ int2 s_open[NW];
+    Work w(p, true);
+    if (!w.any) return;
+    const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
+    Keys keys(sh, p, w, lane);
+    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS == kBias);
+    typename O::Frag q[DP / O::K], go[DP / O::K];
+    const T* gr = static_cast<const T*>(p.grad_out) + own.at * p.row_width;
+    const T* orow = static_cast<const T*>(p.o) + own.at * p.row_width;
+    float delta = 0.f;
+#pragma unroll
+    for (int c = 0; c < DP / O::K; ++c) {
+        const int d = c * O::K + h * (O::K / 2);
+        go[c] = __builtin_bit_cast(typename O::Frag, load_chunk(gr, d, p.D));
+        const auto o = __builtin_bit_cast(typename O::Frag, load_chunk(orow, d, p.D));
+#pragma unroll
+        for (int e = 0; e < O::K / 2; ++e) delta += (float)go[c][e] * (float)o[e];
+    }
+    delta = halves_sum(delta);
+    const float lse = p.lse[own.stat] == -kInf ? kInf : p.lse[own.stat] * kLog2e;
+    acc_t minus_delta;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) minus_delta[r] = -delta;
+    float lack = 0.f, met = 0.f;  // met: keys seen so far, of this half wave's
+    // rows that may turn out to have few keys; without documents a row's place says how many it sees
+    bool open = own.row < p.R && own.last >= 0 && (p.q_doc || own.last < kFewKeys);
+    if (p.tile_ranges) {  // not if the tiles that are of its document, or common, from end to end are enough
+        const int4* ranges = w.tile_ranges(p);
+        int enough = kFewKeys;
+        for (int t0 = 0; t0 < p.tiles && __any(open); t0 += 64) {
+            const int t = t0 + lane;
+            int4 x = make_int4(0, -1, 0, 0);
+            if (t < p.tiles && (t + 1) * Tile::kRows <= p.Lk) x = ranges[t];
+            uint64_t all = __ballot(x.z && ((x.x == x.y && w.docs.lo <= x.x && x.x <= w.docs.hi) || (t + 1) * Tile::kRows <= w.common));
+            for (; all && __any(open); all &= all - 1) {
+                const int b = __builtin_ctzll(all), end = (t0 + b + 1) * Tile::kRows;
+                const bool seen = end - 1 <= own.last && (end <= w.common || __builtin_amdgcn_readlane(x.x, b) == own.doc);
+                enough -= seen ? Tile::kRows : 0;
+                open = open && enough >= 0;
+            }
+        }
+    }
+    // Whether a row of the workgroup is open; the walk goes on with what such rows see.
+    auto any_open = [&]() {
+        int lo = open ? own.doc : 0x7fffffff, hi = open ? own.doc : -1;
+#pragma unroll
+        for (int m = 16; m; m >>= 1) {  // both half waves hold the same rows
+            lo = min(lo, __shfl_xor(lo, m, 64));
+            hi = max(hi, __shfl_xor(hi, m, 64));
+        }
+        if (lane == 0) s_open[wave] = make_int2(lo, hi);
+        __syncthreads();  // and every wave has read the tile
+        for (int i = 0; i < NW; ++i) {
+            lo = min(lo, s_open[i].x);
+            hi = max(hi, s_open[i].y);
+        }
+        keys.only({__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi), 1});
+        return w.docs.hi >= 0;
+    };
+    auto body = [&](int j0, int sub, bool partial) {  // the tile's keys from sub on
+#pragma unroll
+        for (int kb = 0; kb < Tile::kBlocks; ++kb) {
+            acc_t s = row_product<T, DP>(sh.k[0] + (sub + kb * 32) * Tile::kStride, Tile::kStride, q, lane, p.D, acc_t{});
+            const acc_t e = row_product<T, DP>(sh.v[0] + (sub + kb * 32) * Tile::kStride, Tile::kStride, go, lane, p.D, minus_delta);
+            float unit = p.scale * kLog2e;
+            if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s, nullptr);
+            if constexpr (EXTRAS == kBias) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float2 kp = sh.pos[0][sub + kb * 32 + block_row(r, h)];
+                    const float dx = own.pos.x - kp.x, dy = own.pos.y - kp.y;
+                    s[r] = s[r] * unit - own.slope * __builtin_amdgcn_sqrtf(dx * dx + dy * dy);
+                }
+                unit = 1.f;
+            }
+            acc_t x[2];  // the probabilities, and a one for each
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                x[0][r] = exp2_of(__builtin_fmaf(s[r], unit, -lse));
+                x[1][r] = 1.f;
+            }
+            if (partial) hide(x, 0.f, sub + kb * 32, h, own.last - j0, own.doc, sh.doc[0]);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                if (x[0][r] > 0.f) lack += x[0][r] * e[r];  // padding's dP may be anything
+                met += x[1][r];
+            }
+        }
+    };
+    if (any_open()) {
+        const T* qr = static_cast<const T*>(p.q) + w.n * p.qs[0] + own.i * p.qs[1] + own.head * p.qs[2];
+#pragma unroll
+        for (int c = 0; c < DP / O::K; ++c)
+            q[c] = __builtin_bit_cast(typename O::Frag, load_chunk(qr, c * O::K + h * (O::K / 2), p.D));
+        keys.fetch();
+        while (keys.t >= 0) {
+            keys.stage(0);
+            const bool whole = keys.whole(own);
+            const int j0 = keys.t * Tile::kRows;
+            __syncthreads();  // the tile is written
+            keys.fetch();
+            if (whole && Tile::kRows > kFewKeys) {
+                open = false;
+            } else if (__any(open)) {
+#pragma unroll 1
+                for (int sub = 0; sub < Tile::kRows; sub += 32 * Tile::kBlocks) body(j0, sub, !whole);
+                open = open && halves_sum(met) <= kFewKeys;
+            }
+            if (!any_open()) break;
+        }
+    }
+    lack = halves_sum(lack);
+    if (h == 0 && own.row < p.R) p.delta[own.stat] = open && fabsf(lack) < kInf ? delta + lack : delta;
 }
 
 template <typename T, int DP, int NW, int EXTRAS>
@@ -472,7 +567,8 @@ template <typename T, int DP, Launch WHICH, int EXTRAS>
 void launch_owners(const AttnParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)xcd_grid((int64_t)p.N * p.Mkv * p.blocks * p.splits));
     if constexpr (WHICH == kKeyGrad) hipLaunchKernelGGL((attn_grad_kv_kernel<T, DP, 4, EXTRAS>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((attn_grad_q_kernel<T, DP, 4, EXTRAS, WHICH == kRowDelta>), grid, dim3(256), 0, stream, p);
+    else if constexpr (WHICH == kRowGrad) hipLaunchKernelGGL((attn_grad_q_kernel<T, DP, 4, EXTRAS>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((attn_delta_kernel<T, DP, 4, EXTRAS>), grid, dim3(256), 0, stream, p);
 }
 
 template <typename T, Launch WHICH>

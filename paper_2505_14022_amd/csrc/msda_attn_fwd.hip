@@ -23,7 +23,7 @@ constexpr int row_waves(int DP, int NW, size_t element) { return NW == 1 ? (elem
 template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, row_waves(DP, NW, sizeof(T))) void attn_fwd_kernel(AttnParams p) {
     using O = Op<T>;
-    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, true>;
+    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, kValues>;
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
     __shared__ uint32_t odd_words[32 * NW * Odd<DP>::kWords];

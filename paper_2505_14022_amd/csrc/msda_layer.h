@@ -75,7 +75,7 @@ struct AttnParams {
     int blocks, own_rows;         // workgroups of a slab's owners, and the owners of each
     int tiles, chunk, splits;     // tiles of the other axis, in runs of `chunk` for each of `splits` workgroups
     int causal;
-    int delta_known;              // grad_q reads delta, which it writes otherwise
+    int delta_known;              // grad_q reads delta (of launch_attn_delta), which it writes otherwise
     float scale, softcap;
 };
 
@@ -109,6 +109,7 @@ struct AttnRanges {
 };
 hipError_t launch_attn_ranges(const AttnRanges& c, hipStream_t stream);
 hipError_t launch_attn_forward(const AttnParams& p, int dtype, int waves, hipStream_t stream);
+constexpr int kFewKeys = 64;  // rows of at most so many have their delta formed with care
 hipError_t launch_attn_delta(const AttnParams& p, int dtype, hipStream_t stream);  // 16-bit types; splits == 1
 hipError_t launch_attn_grad_q(const AttnParams& p, int dtype, hipStream_t stream);
 hipError_t launch_attn_grad_kv(const AttnParams& p, int dtype, hipStream_t stream);

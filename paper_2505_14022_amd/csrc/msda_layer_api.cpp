@@ -386,7 +386,7 @@ msda_status_t check_launches(const Attention& x, const msda_attention_t& a, bool
 
 // Whether 16-bit rows may have so few keys that their delta is formed with care, in a launch of its own.
 bool rows_of_few_keys(const msda_attention_t& a) {
-    const int64_t few = 64;
+    const int64_t few = msda::kFewKeys;
     return a.dtype != MSDA_F32 && a.Lk > 0 && (a.Lk <= few || a.q_doc || (a.causal && a.Lk - a.Lq < few));
 }
 

@@ -171,3 +171,62 @@ def test_attention_masked_and_capped_with_an_infinite_query(dtype, D, bias):
     for name, t in (("out", out), ("lse", lse), ("grad_q", gq), ("grad_v", gv)):
         assert_within(name, t, *ref[name])
     assert_within("grad_k", gk[..., rest], *(x[..., rest] for x in ref["grad_k"]))
+
+
+SHORT = [
+    # rows, documents' lengths from the first row on (the last is repeated), masks
+    (300, [1, 2], dict(causal=True)),                 # pairs that lie across blocks and tiles
+    (300, [1, 3], dict()),
+    (400, [150, 3], dict()),                          # short documents behind a long one, in one block with its end
+    (400, [150, 5], dict(causal=True)),
+    (700, [520, 2], dict(causal=True, softcap=5.0)),
+    (460, [200, 1, 180, 4], dict(bias=True)),
+    (330, [7], dict(prefix=40, causal=True)),         # short documents far behind common keys
+]
+
+
+@pytest.mark.parametrize("dtype,D,G", [("f16", 64, 1), ("bf16", 32, 1), ("bf16", 128, 4), ("bf16", 32, 3), ("f16", 20, 1)])
+@pytest.mark.parametrize("case", SHORT, ids=lambda c: f"{c[0]}-{c[1]}-{'-'.join(c[2])}")
+def test_attention_short_documents_wherever_they_lie(case, dtype, D, G):
+    # rows that see at most 64 keys are off by their own roundings and not by that of out, whatever is beside them
+    import torch
+
+    L, sizes, masks = case
+    say(f"attention of short documents {sizes} of {L}, {masks} {dtype} D={D} G={G}")
+    how = masks_of(1, L, L, G, **masks)
+    doc, n = [], 0
+    while len(doc) < L:
+        doc += [n] * sizes[min(n, len(sizes) - 1)]
+        n += 1
+    doc = torch.tensor(doc[:L]).int()[None].cuda()
+    how["q_doc"] = how["k_doc"] = doc
+    q, k, v, go = make(1, L, L, G, 1, D, dtype, seed=L)
+    v += 3  # an offset that all keys share: dP - delta is without it, the rounding of out with it
+    rows = layer_ref.seen_pairs(1, L, L, **{x: how.get(x) for x in ("q_doc", "k_doc", "prefix")},
+                                causal=how["causal"])[0].sum(1) <= 64
+    keys = torch.tensor([bool(rows[(doc[0] == d).cpu()].all()) for d in doc[0]])
+    if "prefix" in how:
+        keys[:40] = False
+    assert rows.any() and keys.any()
+    ref = layer_ref.attention(q, k, v, grad_out=go, few_keys=True, **how)
+    out, lse = msda.attention_forward(q, k, v, **how)
+    gq, gk, gv = msda.attention_backward(q, k, v, out, lse, go, **how)
+    assert_within("grad_q", gq[:, rows.cuda()], *(x[:, rows] for x in ref["grad_q"]))
+    for name, t in (("grad_k", gk), ("grad_v", gv)):
+        assert_within(name, t[:, keys.cuda()], *(x[:, keys] for x in ref[name]))
+
+
+@pytest.mark.parametrize("dtype,D", [("f16", 64), ("bf16", 32), ("bf16", 128)])
+def test_attention_gradients_of_a_small_probability_with_a_large_value(dtype, D):
+    # nearly all of a row's probability is on an early key, the rest on a late one, whose value outweighs that
+    say(f"attention with a large value of small probability, {dtype} D={D}")
+    L = 400
+    q, k, v, go = make(1, L, L, 1, 1, D, dtype, seed=8)
+    q[..., 1:] = 0
+    q[..., 0] = 8
+    k[..., 0] = -25     # scores of -200, of 0 and of -9
+    k[:, 3, :, 0] = 0
+    k[:, 300, :, 0] = -1.125
+    v[:, 300] *= 1000
+    how = masks_of(1, L, L, 1, docs="one")
+    check(q, k, v, go, how, scale=1.0)
