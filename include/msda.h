@@ -414,8 +414,8 @@ msda_status_t msda_attention_forward(const msda_attention_t* a, const void* q, c
 /*
  * Backward pass, from the forward's inputs, out and lse: grad_q [N, Lq, M, D], grad_k and grad_v
  * [N, Lk, Mkv, D] (dtype, contiguous, 16-byte aligned, summed over the query heads that share a key head).
- * out and grad_out are contiguous and 16-byte aligned. P (dP - delta), the gradients of the scores, are rounded to
- * dtype: in fp16 they have to stay below 65504 like the results. N == 0 is a no-op; with Lq == 0 or Lk == 0 the
+ * out and grad_out are contiguous and 16-byte aligned. The gradients of the scores are rounded to dtype (in fp16 with a
+ * power of two, so that neither small nor large ones are lost). N == 0 is a no-op; with Lq == 0 or Lk == 0 the
  * gradients that exist are zeroed.
  */
 msda_status_t msda_attention_backward(const msda_attention_t* a, const void* q, const void* k, const void* v,

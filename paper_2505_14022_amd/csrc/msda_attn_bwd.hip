@@ -21,6 +21,40 @@ namespace {
 template <typename T>
 constexpr int kProbShift = std::is_same_v<T, _Float16> ? 8 : 0;
 
+// The power of two that an owner's score gradients carry as an operand in fp16, which holds 2^-14 .. 2^16 with all its bits:
+// P (dP - delta) is about grad_out / keys, so rows of 16 thousand keys and a grad_out of 1e-3 would be rounded to 3 % of
+// grad_q, and large ones would overflow. It is set by the largest so far, like a softmax's running maximum: that is kept
+// within 2^10 .. 2^15, and the sums follow where it has to come down. What is lost is then at most 2^-35 of the largest. bf16
+// has the exponents of fp32 and needs none.
+template <typename T, int DP>
+struct Carried {
+    static constexpr bool kAny = std::is_same_v<T, _Float16>;
+    float up = 0.f, unit = 1.f;  // its exponent, and itself
+    float limit = 0.f;           // of the operands that the power of two holds for; 0 before the first
+    // `w`: gradients of 32 scores of the lane's owner, which go into `sum`.
+    __device__ __forceinline__ void keep(acc_t& w, acc_t (&sum)[DP / 32]) {
+        if constexpr (!kAny) return;
+        float top = fabsf(w[0]);
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, fabsf(w[r]));
+        if (!__any(top > limit)) return;
+        top = halves_max(top);
+        if (!(top > limit && top < kInf)) return;
+        // at most 2^60: a dP of fp16 values is below 2^39, and what is below 2^-84 reaches no fp16 result
+        const int by = min(11 - __builtin_amdgcn_frexp_expf(top), 60 - (int)up);
+        up += (float)by;
+        unit = __builtin_ldexpf(1.f, (int)up);
+        limit = 0x1p15f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[r] = __builtin_ldexpf(w[r], by);
+#pragma unroll
+        for (int u = 0; u < DP / 32; ++u)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum[u][r] = __builtin_ldexpf(sum[u][r], by);
+    }
+    __device__ __forceinline__ float taken_out(float x) const { return kAny ? __builtin_ldexpf(x, -(int)up) : x; }
+};
+
 // Waves per SIMD that the kernels' registers have to leave room for.
 constexpr int grad_q_waves(int DP, size_t element) { return DP == 32 ? 3 : DP == 128 && element == 4 ? 1 : 2; }
 constexpr int grad_kv_waves(int DP) { return DP == 32 ? 3 : DP == 64 ? 2 : 1; }
@@ -71,6 +105,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
     for (int r = 0; r < 16; ++r) minus_delta[r] = -delta;  // where the sums of dP begin
 #pragma unroll
     for (int u = 0; u < DP / 32; ++u) gq[u] = acc_t{};
+    Carried<T, DP> carried;
     auto body = [&](int b, int j0, int sub, bool partial) {  // the tile's keys from sub on
 #pragma unroll
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
@@ -89,12 +124,13 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
                 unit = 1.f;
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) ds[r] *= exp2_of(__builtin_fmaf(s[r], unit, -lse));
+            for (int r = 0; r < 16; ++r) ds[r] *= exp2_of(__builtin_fmaf(s[r], unit, carried.up - lse));
             if (partial) {
                 acc_t x[1] = {ds};
                 hide(x, 0.f, sub + kb * 32, h, own.last - j0, own.doc, sh.doc[b]);
                 ds = x[0];
             }
+            carried.keep(ds, gq);
             add_product<T, DP>(gq, ds, kt, Tile::kStride, lane);
         }
     };
@@ -119,7 +155,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
             const int d = u * 32 + 8 * g + 4 * h;
             float x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = lse == lse ? gq[u][4 * g + e] * p.scale : lse;
+            for (int e = 0; e < 4; ++e) x[e] = lse == lse ? carried.taken_out(gq[u][4 * g + e]) * p.scale : lse;
             if (p.splits > 1) *reinterpret_cast<float4*>(part + d) = make_float4(x[0], x[1], x[2], x[3]);
             else store_four(out, d, p.D, x);
         }
@@ -419,6 +455,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             for (int i = 0; i < 16; ++i) s[i] += i == r ? more : 0.f;
         }
     };
+    Carried<T, DP> carried;
     auto body = [&](int b, int r0, int sub, int some, bool partial) {  // the tile's rows from sub on
 #pragma unroll
         for (int block = 0; block < Tile::kBlocks; ++block) {
@@ -449,7 +486,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             for (int r = 0; r < 16; ++r) {
                 s[r] = exp2_of(__builtin_fmaf(s[r], unit, s_lse[b][first + block_row(r, h)]));
                 ds[r] *= s[r];
-                if constexpr (kProbShift<T> != 0) ds[r] *= 1.f / (1 << kProbShift<T>);
+                if constexpr (Carried<T, DP>::kAny) ds[r] *= carried.unit * (1.f / (1 << kProbShift<T>));
             }
             if (partial) {
 #pragma unroll
@@ -466,6 +503,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
+            carried.keep(ds, gk);
             add_product<T, DP>(gv, s, gt, Tile::kStride, lane);
             add_product<T, DP>(gk, ds, qt, Tile::kStride, lane);
             if (some) {
@@ -506,7 +544,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             float x[4], y[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[e] = gk[u][4 * g + e] * p.scale;
+                x[e] = carried.taken_out(gk[u][4 * g + e]) * p.scale;
                 y[e] = gv[u][4 * g + e] * v_unit;
             }
             odd_k.apply(x, d);

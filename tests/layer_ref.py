@@ -118,10 +118,12 @@ def seen_pairs(N, Lq, Lk, q_doc=None, k_doc=None, prefix=None, causal=False):
 
 
 def attention(q, k, v, scale=None, softcap=0.0, slopes=None, q_pos=None, k_pos=None, q_doc=None, k_doc=None, prefix=None,
-              causal=False, grad_out=None, few_keys=False):
+              causal=False, grad_out=None, few_keys=False, carried=False):
     """{name: (value, bound)} of out, lse and, with grad_out, grad_q, grad_k and grad_v. What a query does not see
     is left out of every sum, whatever it holds. few_keys: every row has so few that its delta is not that of the
-    rounded out, but mended by sum_j P (dP - delta)."""
+    rounded out, but mended by sum_j P (dP - delta). carried: fp16 gradients of scores are rounded with a power of two that
+    holds the largest of a row (for grad_q) or key (grad_k) at 2^10 or more, so that half of fp16's smallest number, 2^-25, is
+    2^-35 of that."""
     dt = q.dtype
     h, tiny = half_step(dt), TINY[dt]
     hp = 0.0 if dt == torch.float32 else h           # probabilities and dS go through the element type
@@ -181,10 +183,15 @@ def attention(q, k, v, scale=None, softcap=0.0, slopes=None, q_pos=None, k_pos=N
         d_delta = (P * (d_dP + (rho2 + (Lk + 12) * U) * (E.abs() + d_delta))).sum(-1, keepdim=True)
         d_delta = d_delta + 2 * U * delta.abs()
     d_dS = P * ((rho2 + 12 * U) * E.abs() + d_dP + d_delta) + hp * dS.abs()
-    d_dS = torch.where(seen, d_dS * 1.02 + tp, zero)
+    lost_q = lost_k = torch.full((), tp, dtype=torch.float64)
+    if carried:
+        lost_q = dS.abs().amax(-1, keepdim=True) * (tp * 2.0 ** -10)
+        lost_k = dS.abs().reshape(N, Mkv, M // Mkv, Lq, Lk).amax((2, 3), keepdim=True).expand(N, Mkv, M // Mkv, 1, Lk)
+        lost_k = lost_k.reshape(N, M, 1, Lk) * (tp * 2.0 ** -10)
+    d_q, d_dS = (torch.where(seen, d_dS * 1.02 + lost, zero) for lost in (lost_q, lost_k))
     groups = lambda x: flat(x.reshape(N, Mkv, M // Mkv, Lk, D).sum(2))  # noqa: E731
     gq = dS @ K * scale
-    res["grad_q"] = (flat(gq), flat((d_dS + (Lk + 4) * U * dS.abs()) @ K.abs() * scale + h * gq.abs() * 1.02 + tiny))
+    res["grad_q"] = (flat(gq), flat((d_q + (Lk + 4) * U * dS.abs()) @ K.abs() * scale + h * gq.abs() * 1.02 + tiny))
     R = Lq * (M // Mkv)
     gk = groups(dS.transpose(2, 3) @ Q * scale)
     b_k = groups((d_dS + (R + 4) * U * dS.abs()).transpose(2, 3) @ Q.abs() * scale)

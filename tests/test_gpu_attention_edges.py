@@ -230,3 +230,48 @@ def test_attention_gradients_of_a_small_probability_with_a_large_value(dtype, D)
     v[:, 300] *= 1000
     how = masks_of(1, L, L, 1, docs="one")
     check(q, k, v, go, how, scale=1.0)
+
+
+@pytest.mark.parametrize("size", [1.0, 1e-2, 1e-3, 1e-4])
+@pytest.mark.parametrize("case", [(1, 8, 16384, 4, 2, 32, {}), (1, 40, 4099, 2, 1, 128, dict(causal=True)),
+                                  (1, 1030, 1030, 2, 1, 64, dict(docs="pad", softcap=5.0)), (1, 2048, 70, 3, 1, 32, dict(bias=True))],
+                         ids=lambda c: "-".join(map(str, c[:6])))
+def test_attention_small_gradients_in_fp16(case, size):
+    # gradients of scores are about grad_out / keys: below what fp16 holds with all its bits
+    N, Lq, Lk, M, Mkv, D, masks = case
+    say(f"attention's gradients of a grad_out of {size} in fp16, {case}")
+    how = masks_of(N, Lq, Lk, M, **masks)
+    q, k, v, go = make(N, Lq, Lk, M, Mkv, D, "f16", seed=Lk)
+    go = (go.float() * size).half()
+    out, lse = msda.attention_forward(q, k, v, **how)
+    got = msda.attention_backward(q, k, v, out, lse, go, **how)
+    ref = layer_ref.attention(q, k, v, grad_out=go, carried=True, **how)
+    for name, t in zip(("grad_q", "grad_k", "grad_v"), got):
+        assert_within(name, t, *ref[name])
+        # and normwise: the rounding of the result, and as much again for the roundings within
+        value = ref[name][0]
+        off = float((t.cpu().double() - value).norm() / value.norm())
+        own = float((value.half().double() - value).norm() / value.norm())
+        say(f"  {name}: {off:.2e}, rounded {own:.2e}")
+        assert off <= 2 * own + 2.0 ** -11, name
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_attention_large_gradients_of_scores_in_fp16(D):
+    # P (dP - delta) beyond fp16's largest number, with results within it; the largest come late
+    say(f"attention's gradients of scores beyond 65504 in fp16, D={D}")
+    q, k, v, go = make(1, 150, 200, 2, 1, D, "f16", seed=D)
+    k, v, go = k * 2.0 ** -10, v * 300, go * 300
+    v[:, 150:] *= 30
+    how = masks_of(1, 150, 200, 2, docs="mixed", prefix=9)
+    ref = layer_ref.attention(q, k, v, grad_out=go, carried=True, **how)
+    out, lse = msda.attention_forward(q, k, v, **how)
+    gq, gk, gv = msda.attention_backward(q, k, v, out, lse, go, **how)
+    assert float(ref["grad_q"][0].abs().max()) < 60000
+    assert_within("grad_q", gq, *ref["grad_q"])
+    k, q = k * 2.0 ** 10, q * 2.0 ** -10
+    ref = layer_ref.attention(q, k, v, grad_out=go, carried=True, **how)
+    out, lse = msda.attention_forward(q, k, v, **how)
+    gq, gk, gv = msda.attention_backward(q, k, v, out, lse, go, **how)
+    assert float(ref["grad_k"][0].abs().max()) < 60000
+    assert_within("grad_k", gk, *ref["grad_k"])
