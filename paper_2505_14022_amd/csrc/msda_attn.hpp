@@ -24,6 +24,11 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 
+// The power of two by which probabilities (at most 1) are scaled as an operand: fp16 would round those below 6e-5, which
+// a row over many thousand keys is full of, to fewer bits.
+template <typename T>
+constexpr int kProbShift = std::is_same_v<T, _Float16> ? 15 : 0;
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // tanh(x) = 1 - 2 / (e^2x + 1), off by an fp32 rounding of 1; with fp32 operands, where that shows in

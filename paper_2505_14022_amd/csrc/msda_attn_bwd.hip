@@ -16,11 +16,6 @@
 namespace msda {
 namespace {
 
-// The power of two by which probabilities are scaled for the product with grad_out: fp16 would round those below 6e-5
-// (any row over 16 thousand keys) to fewer bits.
-template <typename T>
-constexpr int kProbShift = std::is_same_v<T, _Float16> ? 8 : 0;
-
 // The power of two that an owner's score gradients carry as an operand in fp16, which holds 2^-14 .. 2^16 with all its bits:
 // P (dP - delta) is about grad_out / keys, so rows of 16 thousand keys and a grad_out of 1e-3 would be rounded to 3 % of
 // grad_q, and large ones would overflow. It is set by the largest so far, like a softmax's running maximum: that is kept

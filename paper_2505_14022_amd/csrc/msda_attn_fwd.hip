@@ -3,8 +3,8 @@
 // One pass over the keys with a running maximum and sum (kept in units of log 2 and in fp32): a workgroup
 // owns 32 rows per wave, stages one tile of keys and values after the other in LDS (the next tile's loads
 // run while a tile is worked on), and skips the tiles of which its rows see nothing. Probabilities
-// are rounded to the operands' type for the product with the values, unnormalized (at most 1), while their sum
-// is taken before the rounding: the result's error is then the rounding's, averaged over the keys.
+// are rounded to the operands' type for the product with the values, unnormalized (at most 1, times kProbShift's power), while
+// their sum is taken before the rounding: the result's error is then the rounding's, averaged over the keys.
 // With few rows the keys are split over workgroups, whose partial results a second kernel joins.
 // Measured, with the products of the pairs that are seen: bf16, 2 x 4947 rows x 8 heads x 32, padded: 125 us, 280 TFLOP/s,
 // bound by the vector work between the products (maximum, exponent, sum and conversion of each pair, which 32
@@ -19,6 +19,12 @@ namespace {
 // Waves per SIMD that the registers of a kernel that owns rows have to leave room for. (A lone wave of 128 channels keeps 25
 // registers in memory for it, but with one wave per SIMD and none there a token over 16411 keys takes 155 us, not 130.)
 constexpr int row_waves(int DP, int NW, size_t element) { return NW == 1 ? (element == 4 && DP > 32 ? 1 : 2) : DP == 32 ? 4 : DP == 64 ? 3 : 2; }
+
+// lse of a row's maximum and sum, both as the kernels hold them.
+template <typename T>
+__device__ __forceinline__ float lse_of(float m, float l) {
+    return l == 0.f ? -kInf : (m + (__builtin_amdgcn_logf(l) - kProbShift<T>)) * kLn2;
+}
 
 template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, row_waves(DP, NW, sizeof(T))) void attn_fwd_kernel(AttnParams p) {
@@ -83,7 +89,7 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW, sizeof(T))) void attn_fw
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[u][r] *= fade;
         }
-        const float base = m == -kInf ? 0.f : m;  // a row that has seen nothing yet
+        const float base = (m == -kInf ? 0.f : m) - kProbShift<T>;  // a row that has seen nothing yet: any
 #pragma unroll
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
 #pragma unroll
@@ -139,7 +145,7 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW, sizeof(T))) void attn_fw
             odd.apply(x, u * 32 + 8 * g + 4 * h);
             store_four(out, u * 32 + 8 * g + 4 * h, p.D, x);
         }
-    if (p.lse && h == 0) p.lse[own.stat] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    if (p.lse && h == 0) p.lse[own.stat] = lse_of<T>(m, l);
 }
 
 // Joins the splits of a row: DP / 4 lanes of four channels each, times `groups` (a power of two, a wave holds whole
@@ -188,7 +194,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams p, int groups
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] *= inv;
     store_four(static_cast<T*>(p.out) + ((n * p.Lq + i) * p.M + head) * p.D, d, p.D, x);
-    if (p.lse && d == 0) p.lse[(n * p.M + head) * p.Lq + i] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    if (p.lse && d == 0) p.lse[(n * p.M + head) * p.Lq + i] = lse_of<T>(m, l);
 }
 
 // Documents of the tiles and blocks of each table of a call, one wave for each.

@@ -275,3 +275,35 @@ def test_attention_large_gradients_of_scores_in_fp16(D):
     gq, gk, gv = msda.attention_backward(q, k, v, out, lse, go, **how)
     assert float(ref["grad_k"][0].abs().max()) < 60000
     assert_within("grad_k", gk, *ref["grad_k"])
+
+
+@pytest.mark.parametrize("Lq,Lk", [(1, 1024), (40, 1500), (300, 4096)])
+def test_attention_of_small_probabilities_in_fp16(Lq, Lk):
+    # one key of weight 1 and no value, and many whose weights are less than two of fp16's smallest numbers
+    say(f"attention of {Lk} small probabilities in fp16, {Lq} queries")
+    q, k, v, go = make(1, Lq, Lk, 1, 1, 32, "f16", seed=3)
+    q[..., 1:] = 0
+    q[..., 0] = 8
+    k[..., 0] = -2.0332  # scores of -16.27, weights of 1.45 times 2^-24
+    k[:, 17, :, 0] = 0
+    v += 1
+    v *= 100
+    v[:, 17] = 0
+    ref = layer_ref.attention(q, k, v, scale=1.0, carried=True)
+    out, lse = msda.attention_forward(q, k, v, scale=1.0)
+    for name, t in (("out", out), ("lse", lse)):
+        assert_within(name, t, *ref[name])
+
+
+def test_attention_grad_v_of_small_probabilities_in_fp16():
+    say("attention's grad_v of small probabilities in fp16")
+    q, k, v, go = make(1, 64, 500, 1, 1, 32, "f16", seed=4)
+    q[..., 1:] = 0
+    q[..., 0] = 8
+    k[..., 0] = -2.2932  # 1.45 times 2^-27
+    k[:, 17, :, 0] = 0
+    go = go.abs() * 1000
+    ref = layer_ref.attention(q, k, v, grad_out=go, scale=1.0, carried=True)
+    out, lse = msda.attention_forward(q, k, v, scale=1.0)
+    gv = msda.attention_backward(q, k, v, out, lse, go, scale=1.0)[2]
+    assert_within("grad_v", gv, *ref["grad_v"])
