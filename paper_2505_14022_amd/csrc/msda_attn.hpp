@@ -31,15 +31,16 @@ constexpr int kProbShift = std::is_same_v<T, _Float16> ? 15 : 0;
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh(x) = 1 - 2 / (e^2x + 1), off by an fp32 rounding of 1; with fp32 operands, where that shows in
-// the result, |x| < 1/4 goes through the series x - x^3/3 + 2x^5/15 - 17x^7/315 (next term: 8e-8 of x).
-// Of s * a, with a2 = 2 log2(e) a.
+// tanh(x) = 1 - 2 / (e^2x + 1), off by an fp32 rounding or two of 1. Where that shows in the result (SERIES: with fp32 operands, or
+// a large cap, which it is multiplied by), |x| < 1/4 goes through the series x - x^3/3 + 2x^5/15 - 17x^7/315 + 62x^9/2835 (next
+// term: 8.5e-9 of x). Of s * a, with a2 = 2 log2(e) a.
 template <bool SERIES>
 __device__ __forceinline__ float tanh_of(float s, float a, float a2) {
     const float t = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(exp2_of(s * a2) + 1.f), 1.f);
     if constexpr (!SERIES) return t;
     const float x = s * a, x2 = x * x;
-    float y = __builtin_fmaf(x2, -17.f / 315.f, 2.f / 15.f);
+    float y = __builtin_fmaf(x2, 62.f / 2835.f, -17.f / 315.f);
+    y = __builtin_fmaf(y, x2, 2.f / 15.f);
     y = __builtin_fmaf(y, x2, -1.f / 3.f);
     y = __builtin_fmaf(y * x2, x, x);
     return fabsf(x) < 0.25f ? y : t;
@@ -400,7 +401,7 @@ struct Row32 {
         x.last = x.doc < 0 ? -1 : p.causal ? max(x.i + w.off, w.common - 1) : p.Lk - 1;
         x.slope = 0.f;
         x.pos = make_float2(0.f, 0.f);
-        if (biased) {
+        if (biased && p.slopes) {
             x.slope = p.slopes[x.head] * kLog2e;
             x.pos = reinterpret_cast<const float2*>(p.q_pos)[(int64_t)w.n * p.Lq + x.i];
         }
@@ -504,7 +505,7 @@ struct KeyTiles {
                 if (docs) doc_x[a] = docs[min(j, p.Lk - 1)];
             }
         }
-        if (BIASED) {
+        if (BIASED && p.slopes) {
 #pragma unroll
             for (int a = 0; a < Tile::kLoads; ++a)
                 if (Tile::channel() == 0)
@@ -575,8 +576,18 @@ struct KeyTiles {
     }
 };
 
-// What is done to the scores, each with kernels of its own: nothing, capping, or a bias (and capping, if asked for).
-enum Extras { kPlain, kCap, kBias };
+// What is done to the scores, each with kernels of its own: nothing, capping, a bias (and capping, if asked for), or capping far
+// out (and a bias, if asked for). With 16-bit operands, whose probabilities are rounded to 2^-11 or less, the short form of
+// tanh serves caps up to kShortCap, where a score is 2^-14 off; the last kernels take tanh's series. (Both forms in one kernel:
+// 666 us for 649 in the step of 2 x 4096 packed causal rows x 16 heads x 128, 143 for 137 for a token over 16411 keys; the series in
+// all biased kernels: 309 for 280 in a capped step of 2 x 2000 rows x 8 heads x 64.)
+enum Extras { kPlain, kCap, kBias, kFarCap };
+constexpr float kShortCap = 256.f;
+template <typename T>
+Extras extras_of(const AttnParams& p) {
+    if (sizeof(T) == 2 && p.softcap > kShortCap) return kFarCap;
+    return p.slopes ? kBias : p.softcap > 0.f ? kCap : kPlain;
+}
 
 // The row of the register r of a 32 x 32 block.
 __device__ __forceinline__ int block_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
@@ -586,11 +597,11 @@ __device__ __forceinline__ int block_row(int r, int h) { return 8 * (r >> 2) + 4
 // derivative 1 - tanh^2.
 template <typename T, int EXTRAS>
 __device__ __forceinline__ float cap_scores(const AttnParams& p, acc_t& s, acc_t* ds) {
-    if (EXTRAS == kBias && !(p.softcap > 0.f)) return p.scale * kLog2e;
+    if (EXTRAS >= kBias && !(p.softcap > 0.f)) return p.scale * kLog2e;
     const float a = p.scale / p.softcap, a2 = 2.f * kLog2e * a;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        s[r] = tanh_of<std::is_same_v<T, float>>(s[r], a, a2);
+        s[r] = tanh_of<std::is_same_v<T, float> || EXTRAS == kFarCap>(s[r], a, a2);
         if (ds) (*ds)[r] *= __builtin_fmaf(-s[r], s[r], 1.f);
     }
     return p.softcap * kLog2e;

@@ -60,7 +60,7 @@ constexpr int grad_kv_waves(int DP) { return DP == 32 ? 3 : DP == 64 ? 2 : 1; }
 template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_grad_q_kernel(AttnParams p) {
     using O = Op<T>;
-    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, kKeys>;
+    using Keys = KeyTiles<T, DP, NW, EXTRAS >= kBias, kKeys>;
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
     Work w(p, true);
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
     Keys keys(sh, p, w, lane);
     const bool any = w.note_split(p, keys.any());
     if (!any && w.split > 0) return;  // the first split writes delta
-    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS == kBias);
+    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS >= kBias);
     typename O::Frag q[DP / O::K], go[DP / O::K];
     float delta = 0.f;
     {
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
             acc_t ds = row_product<T, DP>(sh.v[b] + (sub + kb * 32) * Tile::kStride, Tile::kStride, go, lane, p.D, minus_delta);
             float unit = p.scale * kLog2e;
             if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s, &ds);
-            if constexpr (EXTRAS == kBias) {
+            if constexpr (EXTRAS >= kBias) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float2 kp = sh.pos[b][sub + kb * 32 + block_row(r, h)];
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
 template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_delta_kernel(AttnParams p) {
     using O = Op<T>;
-    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, kNothing, 1>;
+    using Keys = KeyTiles<T, DP, NW, EXTRAS >= kBias, kNothing, 1>;
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
     __shared__ int2 s_open[NW];
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_del
     if (!w.any) return;
     const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
     Keys keys(sh, p, w, lane);
-    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS == kBias);
+    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS >= kBias);
     typename O::Frag q[DP / O::K], go[DP / O::K];
     const T* gr = static_cast<const T*>(p.grad_out) + own.at * p.row_width;
     const T* orow = static_cast<const T*>(p.o) + own.at * p.row_width;
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_del
             const acc_t e = row_product<T, DP>(sh.v[0] + (sub + kb * 32) * Tile::kStride, Tile::kStride, go, lane, p.D, minus_delta);
             float unit = p.scale * kLog2e;
             if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s, nullptr);
-            if constexpr (EXTRAS == kBias) {
+            if constexpr (EXTRAS >= kBias) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float2 kp = sh.pos[0][sub + kb * 32 + block_row(r, h)];
@@ -291,8 +291,8 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
     __shared__ __attribute__((aligned(16))) T s_q[2][Tile::kElems], s_g[2][Tile::kElems];
     __shared__ __attribute__((aligned(16))) float s_lse[2][Tile::kRows], s_delta[2][Tile::kRows];
     __shared__ __attribute__((aligned(16))) int s_doc[2][Tile::kRows], s_last[2][Tile::kRows];
-    __shared__ __attribute__((aligned(16))) float s_slope[2][EXTRAS == kBias ? Tile::kRows : 1];
-    __shared__ __attribute__((aligned(16))) float2 s_pos[2][EXTRAS == kBias ? Tile::kRows : 1];
+    __shared__ __attribute__((aligned(16))) float s_slope[2][EXTRAS >= kBias ? Tile::kRows : 1];
+    __shared__ __attribute__((aligned(16))) float2 s_pos[2][EXTRAS >= kBias ? Tile::kRows : 1];
     __shared__ int s_odd[2][NW];
     __shared__ uint32_t odd_words[2][32 * NW * Odd<DP>::kWords];
     Work w(p, false);  // the first keys have the most rows
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
         }
     }
     float2 pos = make_float2(0.f, 0.f);
-    if (EXTRAS == kBias) pos = reinterpret_cast<const float2*>(p.k_pos)[(int64_t)w.n * p.Lk + j];
+    if (EXTRAS >= kBias && p.slopes) pos = reinterpret_cast<const float2*>(p.k_pos)[(int64_t)w.n * p.Lk + j];
     const bool is_common = key < w.common;
     const int key_code = pad ? 0x7fffffff : key;  // past the last key that any row sees
 
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
                 delta_x = p.delta[at];
                 doc_x = p.q_doc ? p.q_doc[(int64_t)w.n * p.Lq + i] : 0;
                 last_x = p.causal ? max(i + w.off, w.common - 1) : p.Lk - 1;
-                if (EXTRAS == kBias) {
+                if (EXTRAS >= kBias && p.slopes) {
                     slope_x = p.slopes[head] * kLog2e;
                     pos_x = reinterpret_cast<const float2*>(p.q_pos)[(int64_t)w.n * p.Lq + i];
                 }
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
             s_delta[b][threadIdx.x] = -delta_x;
             s_doc[b][threadIdx.x] = doc_x;
             s_last[b][threadIdx.x] = doc_x < 0 ? -1 : last_x;
-            if (EXTRAS == kBias) {
+            if (EXTRAS >= kBias) {
                 s_slope[b][threadIdx.x] = slope_x;
                 s_pos[b][threadIdx.x] = pos_x;
             }
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(64 * NW, grad_kv_waves(DP)) void attn_grad_kv_kerne
                 if (some) add_infinities(s, r0 + first);
                 unit = cap_scores<T, EXTRAS>(p, s, &ds);
             }
-            if constexpr (EXTRAS == kBias) {
+            if constexpr (EXTRAS >= kBias) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int at = first + block_row(r, h);
@@ -609,8 +609,11 @@ hipError_t launch_typed(const AttnParams& p, hipStream_t stream) {
     return by_channels(p.D, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
         constexpr bool KV = WHICH == kKeyGrad;
-        if (p.slopes) launch_owners<T, DP, WHICH, kBias>(p, stream);
-        else if (p.softcap > 0.f) launch_owners<T, DP, WHICH, kCap>(p, stream);
+        const Extras extras = extras_of<T>(p);
+        if (extras == kFarCap) {
+            if constexpr (sizeof(T) == 2) launch_owners<T, DP, WHICH, kFarCap>(p, stream);
+        } else if (extras == kBias) launch_owners<T, DP, WHICH, kBias>(p, stream);
+        else if (extras == kCap) launch_owners<T, DP, WHICH, kCap>(p, stream);
         else launch_owners<T, DP, WHICH, kPlain>(p, stream);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.splits == 1) return e;

@@ -29,7 +29,7 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, row_waves(DP, NW, sizeof(T))) void attn_fwd_kernel(AttnParams p) {
     using O = Op<T>;
-    using Keys = KeyTiles<T, DP, NW, EXTRAS == kBias, kValues>;
+    using Keys = KeyTiles<T, DP, NW, EXTRAS >= kBias, kValues>;
     using Tile = typename Keys::Tile;
     __shared__ __attribute__((aligned(16))) typename Keys::Shared sh;
     __shared__ uint32_t odd_words[32 * NW * Odd<DP>::kWords];
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW, sizeof(T))) void attn_fw
     const int lane = threadIdx.x & 63, wave = wave_index(), h = lane >> 5;
     Keys keys(sh, p, w, lane);
     if (!w.note_split(p, keys.any())) return;
-    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS == kBias);
+    const Row32 own = Row32::of<NW>(p, w, wave, lane, EXTRAS >= kBias);
     typename O::Frag q[DP / O::K];
     const T* qr = static_cast<const T*>(p.q) + w.n * p.qs[0] + own.i * p.qs[1] + own.head * p.qs[2];
 #pragma unroll
@@ -58,7 +58,7 @@ __global__ __launch_bounds__(64 * NW, row_waves(DP, NW, sizeof(T))) void attn_fw
         for (int kb = 0; kb < Tile::kBlocks; ++kb) {
             s[kb] = row_product<T, DP>(sh.k[b] + (sub + kb * 32) * Tile::kStride, Tile::kStride, q, lane, p.D, acc_t{});
             if constexpr (EXTRAS >= kCap) unit = cap_scores<T, EXTRAS>(p, s[kb], nullptr);
-            if constexpr (EXTRAS == kBias) {
+            if constexpr (EXTRAS >= kBias) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float2 kp = sh.pos[b][sub + kb * 32 + block_row(r, h)];
@@ -257,8 +257,11 @@ template <typename T>
 hipError_t launch_typed(const AttnParams& p, int waves, hipStream_t stream) {
     return by_channels(p.D, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        if (p.slopes) launch_rows<T, DP, kBias>(p, waves, stream);
-        else if (p.softcap > 0.f) launch_rows<T, DP, kCap>(p, waves, stream);
+        const Extras extras = extras_of<T>(p);
+        if (extras == kFarCap) {
+            if constexpr (sizeof(T) == 2) launch_rows<T, DP, kFarCap>(p, waves, stream);
+        } else if (extras == kBias) launch_rows<T, DP, kBias>(p, waves, stream);
+        else if (extras == kCap) launch_rows<T, DP, kCap>(p, waves, stream);
         else launch_rows<T, DP, kPlain>(p, waves, stream);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.splits == 1) return e;

@@ -307,3 +307,38 @@ def test_attention_grad_v_of_small_probabilities_in_fp16():
     out, lse = msda.attention_forward(q, k, v, scale=1.0)
     gv = msda.attention_backward(q, k, v, out, lse, go, scale=1.0)[2]
     assert_within("grad_v", gv, *ref["grad_v"])
+
+
+@pytest.mark.parametrize("softcap", [1e4, 1e6, 1e8])
+@pytest.mark.parametrize("dtype,D", [("f32", 32), ("f16", 64), ("bf16", 32), ("bf16", 128)])
+def test_attention_with_a_large_cap(dtype, D, softcap):
+    # cap tanh(s / cap) is s to (s / cap)^2 / 3 of it, 1e-6 or less here (scores up to 20): as without a cap
+    say(f"attention with a cap of {softcap}, {dtype} D={D}")
+    q, k, v, go = make(2, 150, 170, 4, 2, D, dtype, seed=9)
+    for bias in (False, True):
+        how = masks_of(2, 150, 170, 4, docs="mixed", prefix=9, bias=bias)
+        ref = layer_ref.attention(q, k, v, grad_out=go, **how)
+        how["softcap"] = softcap
+        out, lse = msda.attention_forward(q, k, v, **how)
+        got = (out, lse) + tuple(msda.attention_backward(q, k, v, out, lse, go, **how))
+        for name, t in zip(("out", "lse", "grad_q", "grad_k", "grad_v"), got):
+            assert_within(name, t, *ref[name])
+
+
+def test_attention_capped_scores_at_a_quarter_of_the_cap():
+    # where the two forms of tanh meet in fp32: lse of one key is its score, to the roundings of it
+    import torch
+
+    say("attention's capped scores around a quarter of the cap, fp32")
+    D = 8
+    q = torch.zeros(1, 4096, 1, D, device="cuda")
+    q[0, :, 0, 0] = torch.linspace(0.15, 0.3, 4096)
+    k = torch.zeros(1, 1, 1, D, device="cuda")
+    k[..., 0] = 1
+    lse = msda.attention_forward(q, k, k, scale=1.0, softcap=1.0)[1]
+    z = torch.tanh(q[0, :, 0, 0].double().cpu())
+    # within the series (first half and more): the polynomial's four operations, s * a, the log 2 units and back; 10 u of z
+    inside = q[0, :, 0, 0].cpu() < 0.25
+    off = (lse[0, 0].double().cpu() - z).abs() / z
+    assert float(off[inside].max()) <= 10 * layer_ref.U, float(off[inside].max()) / layer_ref.U
+    assert float(off[~inside].max()) <= 6 * layer_ref.U / 0.24 + 4 * layer_ref.U
