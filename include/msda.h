@@ -379,7 +379,9 @@ typedef struct {
     int causal;                   /* nonzero: the order rule above; needs Lk >= Lq                    */
     int unaligned;                /* nonzero: q, k and v may start off 16-byte boundaries; see below  */
     float scale;                  /* finite, > 0                                                      */
-    float softcap;                /* finite, >= 0; 0: scores are not capped                           */
+    float softcap;                /* finite, >= 0; 0: scores are not capped. Both, and scale /        */
+                                  /* softcap, are below 1e38 (INVALID_VALUE where 2 log2(e) times one */
+                                  /* of them overflows)                                               */
     int64_t q_stride[3];          /* strides of q [N, Lq, M, D] in elements: batch item, token, head; */
     int64_t k_stride[3];          /* the channels are contiguous. Likewise k [N, Lk, Mkv, D]          */
     int64_t v_stride[3];          /* and v [N, Lk, Mkv, D]; >= 0, and 0 repeats an entry              */

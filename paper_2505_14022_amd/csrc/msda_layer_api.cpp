@@ -249,6 +249,13 @@ msda_status_t check_attention(const msda_attention_t* a) {
         return fail(MSDA_ERROR_INVALID_VALUE, "scale=%g must be finite and > 0", (double)a->scale);
     if (!(a->softcap >= 0.f) || isinf(a->softcap))
         return fail(MSDA_ERROR_INVALID_VALUE, "softcap=%g must be finite and >= 0", (double)a->softcap);
+    // the kernels' factors, in units of log 2
+    const float log2e = 1.4426950408889634f;
+    if (isinf(a->scale * log2e))
+        return fail(MSDA_ERROR_INVALID_VALUE, "scale=%g times log2(e) must be finite", (double)a->scale);
+    if (isinf(a->softcap * log2e) || (a->softcap > 0.f && isinf(2.f * log2e * (a->scale / a->softcap))))
+        return fail(MSDA_ERROR_INVALID_VALUE, "softcap=%g and scale=%g: their products with 2 log2(e), and that of scale / softcap, "
+                    "must be finite", (double)a->softcap, (double)a->scale);
     if (a->causal && a->Lk < a->Lq)
         return fail(MSDA_ERROR_INVALID_VALUE, "causal needs Lk=%lld >= Lq=%lld", (long long)a->Lk, (long long)a->Lq);
     if (a->M > 32768)  // the rows of a tile lie within 2^31 bytes

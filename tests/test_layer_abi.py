@@ -232,3 +232,19 @@ def test_attention_refuses_grids_that_the_runtime_does_not_take(L, no_gpu, most,
 def test_rotary_refuses_grids_that_the_runtime_does_not_take(L, no_gpu, entry, kw):
     assert rotary(L, entry=entry, N=1, T=2 ** 24, A=1, items=1, **kw) == UNSUPPORTED and "launch" in msda.last_error()
     assert rotary(L, entry=entry, N=1, T=2 ** 24 - 1, A=1, items=1, **kw) == msda.MSDA_ERROR_LAUNCH_FAILED  # there is no GPU
+
+
+@pytest.mark.parametrize("kw,needle", [
+    (dict(scale=3e38), "scale"), (dict(softcap=3e38), "softcap"), (dict(scale=1.0, softcap=1e-39), "softcap"),
+    (dict(scale=100.0, softcap=4e-37), "softcap"), (dict(scale=1e-3, softcap=1e-45), "softcap"),
+])
+def test_attention_refuses_factors_that_overflow(L, no_gpu, kw, needle):
+    # zero scores times such a factor would be NaN
+    assert attention_size(L, 0, **kw) == INVALID and needle in msda.last_error()
+    assert forward(L, description(**kw)) == INVALID and needle in msda.last_error()
+    assert backward(L, description(**kw)) == INVALID and needle in msda.last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(scale=1e38), dict(softcap=1e38), dict(scale=1e-3, softcap=1e-38), dict(scale=1e-45)])
+def test_attention_takes_factors_up_to_there(L, no_gpu, kw):
+    assert attention_size(L, 1, **kw) == OK
