@@ -299,9 +299,13 @@ AttnPlan attn_plan(const AttnParams& p, int dtype, AttnKernel kernel) {
     int64_t splits = waves > 0 ? ((4 * waves < room ? 1 : 2) * room + waves - 1) / waves : 1;
     const bool full = waves >= room;
     // Masks leave some workgroups many tiles and others few. Where a SIMD holds one wave, nothing else runs beside the
-    // longest ones: shorter runs (16 heads of 128 channels over 2 x 4096 packed causal tokens: 441 us -> 323 and 10 more
-    // to add the splits up). The others lose more by the partial results (the encoder's step above 433 us -> 536).
-    if (per_simd == 1) splits *= p.q_doc ? 8 : p.causal ? 2 : 1;
+    // longest ones, and shorter runs even them out if the runs are long and the workgroups few. The backward, bf16, 4096 tokens
+    // of 16 heads of 128 channels on 4 key heads (256 tiles), without and with them: packed causal N = 2 640 us and 517, N = 1 457
+    // and 330; packed 942 and 739; causal 1176 and 1040, 736 and 736; padded, where there is nothing to even out, 1500
+    // and 1682. On 8 heads of their own (64 tiles) the partial results cost more: packed causal 319 and 452, packed 530 and 753,
+    // causal 528 and 664; and with twice the workgroups (9000 packed tokens) 1162 and 1203. The kernels of
+    // more waves lose as well (the encoder's step above 433 us -> 536).
+    if (per_simd == 1 && tiles >= 128 && waves < 2 * room) splits *= p.q_doc ? 8 : p.causal ? 4 : 1;
     // runs shorter than this do not pay for the workgroup's start and its partial results
     const int64_t least = full ? 16 : 4;
     // and the partial results of all splits have to fit into half a GB
