@@ -25,9 +25,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 
 // The power of two by which probabilities (at most 1) are scaled as an operand: fp16 would round those below 6e-5, which
-// a row over many thousand keys is full of, to fewer bits.
+// a row over many thousand keys is full of, to fewer bits. A probability is over 1 by what its score and maximum are rounded to:
+// 2^5 are left to fp16's largest number for scores of 10^7, whose rounding in fp32 is 1.
 template <typename T>
-constexpr int kProbShift = std::is_same_v<T, _Float16> ? 15 : 0;
+constexpr int kProbShift = std::is_same_v<T, _Float16> ? 11 : 0;
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 

@@ -123,7 +123,7 @@ def attention(q, k, v, scale=None, softcap=0.0, slopes=None, q_pos=None, k_pos=N
     is left out of every sum, whatever it holds. few_keys: every row has so few that its delta is not that of the
     rounded out, but mended by sum_j P (dP - delta). carried: fp16 gradients of scores are rounded with a power of two that
     holds the largest of a row (for grad_q) or key (grad_k) at 2^10 or more, so that half of fp16's smallest number, 2^-25, is
-    2^-35 of that, and its probabilities (of a row's largest in the forward) with one of 2^15."""
+    2^-35 of that, and its probabilities (of a row's largest in the forward) with one of 2^11."""
     dt = q.dtype
     h, tiny = half_step(dt), TINY[dt]
     hp = 0.0 if dt == torch.float32 else h           # probabilities and dS go through the element type
@@ -164,7 +164,7 @@ def attention(q, k, v, scale=None, softcap=0.0, slopes=None, q_pos=None, k_pos=N
     out = P @ V
     A = P @ V.abs()
     spread = seen.double().expand(N, M, Lq, Lk) @ V.abs()
-    d_out = (2 * rho + hp + (2 * Lk + 8) * U) * A + (tp * 2.0 ** -15 if carried else tp) * spread
+    d_out = (2 * rho + hp + (2 * Lk + 8) * U) * A + (tp * 2.0 ** -11 if carried else tp) * spread
     d_lse = rho + (Lk + 4) * U + 6 * U * lse.abs()
     flat = lambda x: x.transpose(1, 2)  # noqa: E731
     res = {"out": (flat(out), flat(d_out * 1.02 + h * out.abs() * 1.01 + tiny)),
@@ -197,6 +197,6 @@ def attention(q, k, v, scale=None, softcap=0.0, slopes=None, q_pos=None, k_pos=N
     b_k = groups((d_dS + (R + 4) * U * dS.abs()).transpose(2, 3) @ Q.abs() * scale)
     res["grad_k"] = (gk, b_k + h * gk.abs() * 1.02 + tiny)
     gv = groups(P.transpose(2, 3) @ G)
-    d_P = torch.where(seen, P * (rho2 + hp + (R + 4) * U) * 1.02 + tp * 2.0 ** (-15 if carried else -8), zero)  # fp16: scaled by 2^8 at least
+    d_P = torch.where(seen, P * (rho2 + hp + (R + 4) * U) * 1.02 + tp * 2.0 ** (-11 if carried else -8), zero)  # fp16: scaled by 2^8 at least
     res["grad_v"] = (gv, groups(d_P.transpose(2, 3) @ G.abs()) + h * gv.abs() * 1.02 + tiny)
     return res

@@ -342,3 +342,25 @@ def test_attention_capped_scores_at_a_quarter_of_the_cap():
     off = (lse[0, 0].double().cpu() - z).abs() / z
     assert float(off[inside].max()) <= 10 * layer_ref.U, float(off[inside].max()) / layer_ref.U
     assert float(off[~inside].max()) <= 6 * layer_ref.U / 0.24 + 4 * layer_ref.U
+
+
+@pytest.mark.parametrize("Lq", [1, 90])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_attention_of_scores_of_ten_millions(dtype, Lq):
+    # one key takes all: out is its value, to the rounding of a probability and of the result, and grad_v of the others is 0
+    import torch
+
+    say(f"attention with scores of ten millions, {dtype}")
+    q, k, v, go = make(1, Lq, 400, 2, 2, 64, dtype, seed=Lq)
+    q, k = q * 2500, k * 2500
+    z = (q.cpu().double().transpose(1, 2) @ k.cpu().double().permute(0, 2, 3, 1)) / 8
+    top2 = z.topk(2, -1)
+    clear = top2.values[..., 0] - top2.values[..., 1] > 2000  # [N, M, Lq]; far beyond the rounding of a score
+    assert float(top2.values.max()) > 1.2e7 and clear.float().mean() > 0.9
+    out, lse = msda.attention_forward(q, k, v)
+    want = torch.gather(v.cpu().double().transpose(1, 2), 2, top2.indices[..., :1].expand(-1, -1, -1, 64))
+    off = (out.cpu().double().transpose(1, 2) - want).abs()[clear]
+    assert bool(torch.isfinite(out).all()) and bool((off <= 3 * layer_ref.half_step(out.dtype) * want[clear].abs()).all())
+    assert float(((lse.cpu().double() - top2.values[..., 0]).abs() / top2.values[..., 0]).max()) <= 70 * layer_ref.U * 64
+    grads = msda.attention_backward(q, k, v, out, lse, go)
+    assert all(bool(torch.isfinite(g).all()) for g in grads)
