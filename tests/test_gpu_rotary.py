@@ -119,3 +119,26 @@ def test_rotary_empty():
     say("rotary of no tokens")
     x = torch.empty(2, 0, 3, 16, device="cuda")
     assert msda.rotary_forward(x, torch.empty(2, 0, 1, device="cuda"), freqs_of(1, 8)).shape == x.shape
+
+
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "pairs"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,M,D,R", [(37, 4, 32, 16), (5, 64, 128, 64), (9, 3, 96, 32), (3, 7, 1024, 512)])
+def test_rotary_in_place_of_whole_pieces(T, M, D, R, dtype, interleaved):
+    # heads of whole 16-byte pieces, each read by two threads, several turns of a workgroup to a token among them
+    import torch
+
+    g = torch.Generator().manual_seed(T)
+    qkv = torch.randn(2, T, 3, M, D, generator=g).to(DT[dtype]).cuda()
+    pos = (torch.rand(2, T, 2, generator=g) * 50).cuda()
+    f = freqs_of(2, R)
+    before = qkv.clone()
+    say(f"rotary in place of {T} x {M} x {D}, {R} pairs, {dtype} interleaved={interleaved}")
+    view = qkv[:, :, 1]
+    msda.rotary_forward(view, pos, f, interleaved, out=view)
+    assert_within("out", view, *layer_ref.rotary(before[:, :, 1], pos, f, interleaved))
+    assert torch.equal(view, msda.rotary_forward(before[:, :, 1], pos, f, interleaved))
+    msda.rotary_backward(view, pos, f, interleaved, grad_x=view)
+    again = msda.rotary_backward(msda.rotary_forward(before[:, :, 1], pos, f, interleaved), pos, f, interleaved)
+    assert torch.equal(view, again)
+    assert torch.equal(qkv[:, :, 0], before[:, :, 0]) and torch.equal(qkv[:, :, 2], before[:, :, 2])
