@@ -8,9 +8,11 @@
 // atomics would move rows x channels x key blocks fp32 values instead.
 // Where the owners are few the other axis is split over workgroups, and a last kernel adds the splits.
 // Measured, with the products of the pairs that are seen, grad_q and grad_kv: bf16, 2 x 4947 rows x 8 heads x 32, padded:
-// 127 and 177 us, 416 and 398 TFLOP/s, bound by the vector work of a pair as the forward; 2 x 4096 packed causal rows x
-// 16 heads x 128 on 4 key heads, capped: 144 and 298 us, 302 and 194 TFLOP/s (the second has room for one wave per SIMD:
-// k, v and two sums of 128 channels); fp32, 3 x 1023 rows over 2999 x 5 x 48: 182 and 268 us, 53 and 48 TFLOP/s.
+// 121 and 179 us, 437 and 394 TFLOP/s, bound by the vector work of a pair as the forward; 2 x 4096 packed causal rows x
+// 16 heads x 128 on 4 key heads, capped: 145 and 307 us, 300 and 188 TFLOP/s (the second has room for one wave per SIMD:
+// k, v and two sums of 128 channels); fp32, 3 x 1023 rows over 2999 x 5 x 48: 181 and 272 us, 53 and 47 TFLOP/s, the matrix unit
+// busy in 60 % of the cycles in which a CU has waves, which are 70 % of the kernels' (1080 workgroups for 512 places).
+// Where 16-bit rows may have few keys, a third kernel forms delta before them.
 #include "msda_attn.hpp"
 
 namespace msda {
@@ -20,7 +22,7 @@ namespace {
 // P (dP - delta) is about grad_out / keys, so rows of 16 thousand keys and a grad_out of 1e-3 would be rounded to 3 % of
 // grad_q, and large ones would overflow. It is set by the largest so far, like a softmax's running maximum: that is kept
 // within 2^10 .. 2^15, and the sums follow where it has to come down. What is lost is then at most 2^-35 of the largest. bf16
-// has the exponents of fp32 and needs none.
+// has the exponents of fp32 and needs none. The maximum makes fp16 steps 2 to 5 % longer than bf16's.
 template <typename T, int DP>
 struct Carried {
     static constexpr bool kAny = std::is_same_v<T, _Float16>;
@@ -163,6 +165,8 @@ __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_gra
 // to be had of longer ones. A workgroup walks over the tiles that its rows see, wherever they are, and leaves those that only
 // rows with more keys see: long rows cost it a tile or two, or none where the tables of documents say that they are. A
 // row is mended once all of its keys have been visited: one that is left out may have a value that outweighs its probability.
+// 6 us in the first shape above and 35 in the second, whose out and grad_out take 12 at a copy's rate (two waves per SIMD wait
+// for them, and a few workgroups for their tiles); grad_q reads delta in place of out then.
 template <typename T, int DP, int NW, int EXTRAS>
 __global__ __launch_bounds__(64 * NW, grad_q_waves(DP, sizeof(T))) void attn_delta_kernel(AttnParams p) {
     using O = Op<T>;

@@ -6,11 +6,11 @@
 // are rounded to the operands' type for the product with the values, unnormalized (at most 1, times kProbShift's power), while
 // their sum is taken before the rounding: the result's error is then the rounding's, averaged over the keys.
 // With few rows the keys are split over workgroups, whose partial results a second kernel joins.
-// Measured, with the products of the pairs that are seen: bf16, 2 x 4947 rows x 8 heads x 32, padded: 125 us, 280 TFLOP/s,
+// Measured, with the products of the pairs that are seen: bf16, 2 x 4947 rows x 8 heads x 32, padded: 127 us, 276 TFLOP/s,
 // bound by the vector work between the products (maximum, exponent, sum and conversion of each pair, which 32
-// channels do not outweigh); 2 x 4096 packed causal rows x 16 heads x 128 on 4 key heads, capped: 128 us, 225 TFLOP/s,
-// a third of the pairs of its tiles masked; fp32, 3 x 1023 rows over 2999 x 5 x 48: 122 us, 53 TFLOP/s. One row a head,
-// 8 x 32 on 8 key heads over 16411 keys x 128: 126 us and 8 to join, 4.3 TB/s (a large copy reaches 5.5).
+// channels do not outweigh); 2 x 4096 packed causal rows x 16 heads x 128 on 4 key heads, capped: 129 us, 224 TFLOP/s,
+// a third of the pairs of its tiles masked; fp32, 3 x 1023 rows over 2999 x 5 x 48: 120 us, 54 TFLOP/s. One row a head,
+// 8 x 32 on 8 key heads over 16411 keys x 128: 126 us and 7 to join, 4.3 TB/s (a large copy reaches 5.5).
 #include "msda_attn.hpp"
 
 namespace msda {
