@@ -22,7 +22,7 @@ namespace {
 // P (dP - delta) is about grad_out / keys, so rows of 16 thousand keys and a grad_out of 1e-3 would be rounded to 3 % of
 // grad_q, and large ones would overflow. It is set by the largest so far, like a softmax's running maximum: that is kept
 // within 2^10 .. 2^15, and the sums follow where it has to come down. What is lost is then at most 2^-35 of the largest. bf16
-// has the exponents of fp32 and needs none. The maximum makes fp16 steps 2 to 5 % longer than bf16's.
+// has the exponents of fp32 and needs none. The maximum made fp16 steps 2 to 5 % longer.
 template <typename T, int DP>
 struct Carried {
     static constexpr bool kAny = std::is_same_v<T, _Float16>;

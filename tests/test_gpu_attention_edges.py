@@ -364,3 +364,39 @@ def test_attention_of_scores_of_ten_millions(dtype, Lq):
     assert float(((lse.cpu().double() - top2.values[..., 0]).abs() / top2.values[..., 0]).max()) <= 70 * layer_ref.U * 64
     grads = msda.attention_backward(q, k, v, out, lse, go)
     assert all(bool(torch.isfinite(g).all()) for g in grads)
+
+
+@pytest.mark.parametrize("dtype,D", [("f16", 64), ("bf16", 32), ("bf16", 128)])
+def test_attention_of_16_bits_captured_and_replayed(dtype, D):
+    # short and long documents (tables, delta, runs of tiles and their sums in the graph), new inputs for each replay
+    import torch
+
+    say(f"attention captured into a graph, {dtype} D={D}")
+    L = 900
+    doc = torch.cat([torch.arange(200) // 3, torch.full((650,), 100), torch.full((50,), -2)]).int()[None].cuda()
+    how = {"q_doc": doc, "k_doc": doc.clone(), "causal": True, "softcap": 20.0}
+    t = make(1, L, L, 4, 2, D, dtype, seed=0)
+
+    def step(q, k, v, go):
+        out, lse = msda.attention_forward(q, k, v, **how)
+        return (out, lse) + tuple(msda.attention_backward(q, k, v, out, lse, go, **how))
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(*t)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(*t)
+    for seed in (1, 2, 3):
+        new = make(1, L, L, 4, 2, D, dtype, seed=seed)
+        for a, b in zip(t, new):
+            a.copy_(b)
+        doc.copy_(torch.roll(doc, 7 * seed, 1))
+        how["k_doc"].copy_(doc)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = step(*new)  # between the replays, on the same allocator
+        torch.cuda.synchronize()
+        for name, a, b in zip(("out", "lse", "grad_q", "grad_k", "grad_v"), captured, eager):
+            assert torch.equal(a, b), (seed, name)
