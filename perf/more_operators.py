@@ -10,7 +10,7 @@ ones among them; inputs are drawn on the GPU from the seed alone, lengths follow
   op            what a pass calls
   rms_quantize  msda.rmsnorm_quantize (inference)
   rms_step      msda.rmsnorm_forward and msda.rmsnorm_backward (training)
-  mm            msda.quantize_rows on the activations, where they are not in 8 bits yet, and msda.int8_matmul
+  mm            msda.quantize_rows on the activations, where they are not in 8 bits yet, and msda.quantized_matmul
   append        msda.cache_append
   attn          msda.cache_attention
 
@@ -345,7 +345,7 @@ def _own(s):
         return (out, rstd) + tuple(msda.rmsnorm_backward(s["x"], s["gout"], rstd, s["weight"], residual=s["residual"]))
     if op == "mm":
         codes, scale = (s["x"], s["x_scale"]) if case["codes"] else msda.quantize_rows(s["x"])
-        return msda.int8_matmul(codes, s["w"], scale, s["w_scale"], bias=s["bias"], dtype=DTYPES[case["dtype"]])
+        return msda.quantized_matmul(codes, s["w"], scale, s["w_scale"], bias=s["bias"], dtype=DTYPES[case["dtype"]])
     cache = [s[x] for x in ("k_cache", "v_cache", "k_scale", "v_scale", "table", "length")]
     if op == "append":
         msda.cache_append(s["k"], s["v"], *cache, start=s["start"], pos=s["pos"], freqs=s["freqs"],
