@@ -425,6 +425,130 @@ msda_status_t msda_attention_backward(const msda_attention_t* a, const void* q, 
                                       void* grad_k, void* grad_v, void* workspace, size_t workspace_bytes,
                                       void* stream);
 
+/*
+ * Serving operators: what a decoder layer runs at inference with weights, activations and the keys and values of
+ * earlier tokens held in 8 bits. Codes are signed bytes from -127 to 127; a code times its scale is the value it
+ * stands for. A code is x * (1 / scale) rounded to the nearest, ties to even, with scale = most * (1 / 127) of the
+ * largest magnitude that shares it, each operation in fp32; where that is below 2^-100, scale and codes are 0. A row
+ * (or a block of the cache) that holds an infinity or a NaN gets scale NaN and codes 0, so that its values are NaN.
+ */
+
+/*
+ * Root-mean-square normalization of rows of C channels, with an optional residual addition before it:
+ *   s = x + residual                       (fp32; residual may be NULL: s = x)
+ *   rstd = (sum_c s^2 / C + eps)^(-1/2),  out = s * rstd * weight      (weight NULL: 1)
+ *   x, residual, out [rows, C] dtype;  weight [C] fp32
+ *   sum              [rows, C] dtype or NULL: s rounded to dtype (out is formed from the unrounded s)
+ *   rstd             [rows] fp32 or NULL: kept for the backward pass
+ * Sizes, alignment, eps and limits as in msda_layernorm_forward (C <= MSDA_LAYERNORM_MAX_C). out or sum may be x or
+ * residual itself (a row is read before it is written), but not both the same one.
+ */
+msda_status_t msda_rmsnorm_forward(const void* x, const void* residual, const float* weight, void* out, void* sum,
+                                   float* rstd, int64_t rows, int64_t C, float eps, int dtype, void* stream);
+
+/*
+ * The same with the result in 8 bits: codes [rows, C] of s * weight, each row with a scale of its own, and
+ * scale [rows] fp32 times rstd (a row's rstd is a factor of its values and scale alike), so that codes * scale is out.
+ * 8-byte aligned codes are written in pieces of 4 or 8.
+ */
+msda_status_t msda_rmsnorm_quantize(const void* x, const void* residual, const float* weight, int8_t* codes,
+                                    float* scale, void* sum, int64_t rows, int64_t C, float eps, int dtype, void* stream);
+
+/* Workspace bytes of msda_rmsnorm_backward where a weight gradient is wanted (host-only). */
+msda_status_t msda_rmsnorm_backward_workspace_size(int64_t rows, int64_t C, int dtype, size_t* bytes);
+
+/*
+ * Backward pass of msda_rmsnorm_forward, from its inputs x and residual and its rstd:
+ *   xh = s * rstd,  g = grad_out * weight
+ *   grad_x = rstd * (g - xh * mean_c(g * xh)) + grad_sum,  grad_weight = sum_rows grad_out * xh
+ * Arguments, workspace and rows == 0 as in msda_layernorm_backward; grad_weight may be NULL (not computed).
+ */
+msda_status_t msda_rmsnorm_backward(const void* x, const void* residual, const float* weight, const void* grad_out,
+                                    const void* grad_sum, const float* rstd, void* grad_x, float* grad_weight,
+                                    void* workspace, size_t workspace_bytes, int64_t rows, int64_t C, int dtype,
+                                    void* stream);
+
+/* Rows of C channels in 8 bits: codes [rows, C] and scale [rows] of x [rows, C] dtype. Sizes as in msda_rmsnorm_quantize. */
+msda_status_t msda_quantize_rows(const void* x, int8_t* codes, float* scale, int64_t rows, int64_t C, int dtype,
+                                 void* stream);
+
+/*
+ * Matrix product of 8-bit integers with a scale for each row of both:
+ *   out[t, o] = (sum_k a[t, k] * b[o, k]) * (a_scale[t] * b_scale[o]) + bias[o]
+ *   a [T, K], b [O, K] int8 (any codes, -128 among them);  a_scale [T], b_scale [O], bias [O] fp32 (bias NULL: 0)
+ *   out [T, O] dtype
+ * The sums are exact (32-bit integers, K <= MSDA_QUANTIZED_MAX_K) and scaled in fp32. Any K, O and alignment is taken;
+ * 16-byte aligned a and b with K a multiple of 16 are the fast ones. T * O == 0 is a no-op; K == 0 is
+ * MSDA_ERROR_INVALID_VALUE. T or O from 2^31 - 1024 on, or more workgroups than one launch takes (2^23; the smallest has 16
+ * tokens and 16 channels), is MSDA_ERROR_NOT_SUPPORTED.
+ */
+#define MSDA_QUANTIZED_MAX_K 131071
+msda_status_t msda_quantized_matmul(const int8_t* a, const int8_t* b, const float* a_scale, const float* b_scale,
+                                    const float* bias, void* out, int64_t T, int64_t K, int64_t O, int dtype,
+                                    void* stream);
+
+/*
+ * A paged cache of keys and values in 8 bits, with a scale for each page and head, and the tokens of N sequences
+ * that a call brings. Sequence n holds length[n] tokens, the new ones included, which are its last:
+ * tokens start[n] .. start[n+1] - 1 of the call's T packed tokens. Its j-th token is slot j % page_size of page
+ * table[n, j / page_size]. What the device's tables say is checked there: start is taken within [0, T] (tokens of no
+ * sequence are neither read nor written), a length below the count of new tokens leaves the first of these outside,
+ * tokens beyond width * page_size and tokens of a page that is not in [0, pages) do not exist (they are not stored, and
+ * nobody sees them).
+ */
+typedef struct {
+    int64_t N;          /* sequences, below 2^24                                                          */
+    int64_t pages;      /* of the pool, below 2^31                                                        */
+    int64_t page_size;  /* tokens of a page: 16, 32, 64, 128 or 256                                       */
+    int64_t Mkv, D;     /* heads, and channels of each: a multiple of 16, at most MSDA_CACHE_MAX_D        */
+    int64_t width;      /* pages of a sequence that the table holds; width * page_size below 2^31 - 1024  */
+    int64_t table_stride;   /* elements from one sequence's row of the table to the next, >= width unless N < 2 */
+    int8_t* k;              /* DEVICE [pages, Mkv, page_size, D] codes, 16-byte aligned; likewise v       */
+    int8_t* v;
+    float* k_scale;         /* DEVICE [pages, Mkv] fp32; likewise v_scale                                 */
+    float* v_scale;
+    const int32_t* table;   /* DEVICE [N, width], rows of table_stride                                    */
+    const int32_t* length;  /* DEVICE [N]                                                                 */
+    const int32_t* start;   /* DEVICE [N + 1], not decreasing; or NULL: token n is sequence n's, T == N   */
+} msda_cache_t;
+#define MSDA_CACHE_MAX_D 128
+
+/*
+ * Appends the call's keys and values [T, Mkv, D] dtype, the keys turned by their positions on the way (as
+ * msda_rotary_forward does, in fp32, and rounded once, to the code):
+ *   k_stride, v_stride  HOST arrays of two strides in elements (token, head), >= 0, the channels contiguous
+ *   pos    [T, A] fp32, or NULL: a token's place in its sequence (A == 1);  freqs [A, R] fp32; R == 0: not turned
+ * A page and head has one scale. It is that of the tokens that stand in the page before the new ones, or larger where
+ * these need it: then the codes that stand there are rounded anew to the larger scale. A page whose first slot is
+ * new starts afresh. Slots past the last new token keep what they hold. A page that new tokens reach belongs to one
+ * sequence (it may be shared once it is full); a page that two of them append to in one call holds one's, the other's
+ * or a mixture. T == 0 or N == 0 is a no-op.
+ */
+msda_status_t msda_cache_append(const msda_cache_t* cache, const void* k, const int64_t* k_stride, const void* v,
+                                const int64_t* v_stride, const float* pos, const float* freqs, int64_t T, int64_t A,
+                                int64_t R, int interleaved, int dtype, void* stream);
+
+/*
+ * Attention of the call's queries q [T, M, D] over the cache, which holds their own keys already. Query head m reads
+ * head m / (M / Mkv); scores are capped as in msda_attention_forward.
+ *   z = cap(scale * q . k),  lse = log sum exp(z),  out = sum exp(z - lse) v
+ * causal: the query of place p sees the tokens up to place p of its sequence; otherwise all length[n] of them. A query
+ * that sees no token gets out = 0 and lse = -inf. A page with a scale that is negative or not finite makes NaN of the rows that see any of it;
+ * what is not seen (codes and scales alike) has no effect but on how probabilities are rounded, which are held in
+ * units of the largest value scale at hand.
+ *   q_stride  HOST array of two strides in elements (token, head), >= 0, the channels contiguous
+ *   out [T, M, D] dtype contiguous, 16-byte aligned;  lse [T, M] fp32 or NULL. Rows of tokens of no sequence are left as
+ *   they were.
+ * Long sequences of few queries are split over their tokens and joined. workspace: DEVICE scratch of at least
+ * msda_cache_attention_workspace_size bytes (from the sizes, M, T, dtype and whether start is given), 16-byte aligned, used
+ * by nothing else until the enqueued work completes. T == 0 or N == 0 is a no-op.
+ */
+msda_status_t msda_cache_attention_workspace_size(const msda_cache_t* cache, int64_t T, int64_t M, int dtype,
+                                                  size_t* bytes);
+msda_status_t msda_cache_attention(const msda_cache_t* cache, const void* q, const int64_t* q_stride, void* out,
+                                   float* lse, int64_t T, int64_t M, float scale, float softcap, int causal, int dtype,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static name of a status code ("MSDA_SUCCESS", ...); any int is accepted, and a value that is no
  * msda_status_t gives "MSDA_UNKNOWN_STATUS". */
 const char* msda_status_string(int status);

@@ -17,7 +17,8 @@ LIB_DIR = os.path.join(PKG, "_lib")
 LIB_PATH = os.path.join(LIB_DIR, "libmsda.so")
 SOURCES = ["msda_api.cpp", "msda_arrange.cpp", "msda_fwd.hip", "msda_bwd.hip", "msda_bwd_value.hip",
            "msda_prologue.hip", "msda_noalloc.hip", "msda_layer_api.cpp", "msda_norm.hip", "msda_rotary.hip",
-           "msda_attn_fwd.hip", "msda_attn_bwd.hip"]
+           "msda_attn_fwd.hip", "msda_attn_bwd.hip", "msda_serve_api.cpp", "msda_rms.hip", "msda_product.hip",
+           "msda_append.hip", "msda_cache_attn.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

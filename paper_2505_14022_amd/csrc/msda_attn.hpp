@@ -331,7 +331,7 @@ struct TileWalk {
 // Work of workgroup b: consecutive items go to one XCD (workgroup b runs on XCD b % 8), so that the rows of
 // a slab read its keys through one L2.
 __device__ __forceinline__ int xcd_item(int b, int grid) { return (b & 7) * (grid >> 3) + (b >> 3); }
-int xcd_grid(int64_t items) { return (int)((items + 7) / 8 * 8); }
+[[maybe_unused]] int xcd_grid(int64_t items) { return (int)((items + 7) / 8 * 8); }
 
 // What a workgroup works on: a block of owners and a run of the other axis' tiles.
 struct Work {

@@ -1,0 +1,532 @@
+// Attention over a paged cache of 8-bit keys and values with a scale for each page and head.
+//   z = cap(scale k_scale q . k_code),  lse = log sum exp z,  out = sum exp(z - lse) v_scale v_code
+// For single tokens it is bound by reading the cache once, for chunks of a prompt by the matrix unit and the vector work
+// between its products. One pass over the keys with a running maximum and sum, everything in registers: a wave has 16 rows
+// (queries of the heads that share a key head) or a multiple, as columns of 16 x 16 x 32 instructions, and takes 32 keys at a time.
+//   scores: keys are the instruction's rows. A lane (column n, quarter g) reads consecutive bytes of key n of 16, in an order
+//     of channels that the queries follow, and gets the scores of keys 4 g .. 4 g + 3 of both halves of the 32;
+//   values: a sum over keys may take them in any order, so the lane's eight probabilities are its operand as they are, and it
+//     reads DP / 16 bytes of each of its eight keys, which are the rows n DP / 16 .. of the other operand.
+// So nothing is exchanged between lanes but a maximum, and the cache goes from memory to registers. A code c becomes
+// fp16 without a conversion: byte c ^ 0x80 below the exponent of 1024 is 1152 + c, less 1152 is c.
+// A page's key scale is a factor of its scores. Its value scale goes into the exponent, relative to the largest of the
+// pages at hand, so that it costs nothing for each key.
+// Roundings: queries are scaled by a power of two to their row's largest and held in fp16 (in fp32 as the sum of two), exact for
+// fp16 and for all of bf16 within 2^28 of the largest; probabilities are rounded to fp16 for the product (in fp32 the sum of
+// two), times 2^14, so that those of long rows keep their bits; their sum is taken before that. Statistics and sums are fp32.
+#include "msda_attn.hpp"
+#include "msda_cache.hpp"
+
+namespace msda {
+namespace {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+constexpr int kCacheWaves = 4;
+constexpr float kShift = 14.f;  // probabilities times 2^14 as an operand
+
+// Bytes A and B (0 .. 3) of the words x and y of codes, as two fp16 numbers.
+template <int A, int B>
+__device__ __forceinline__ uint32_t two_codes(uint32_t x, uint32_t y) {
+    // selector: 0 .. 3 bytes of y (second operand), 4 .. 7 of x, 12 zero
+    const uint32_t u = __builtin_amdgcn_perm(x, y, 0x0c000c00u | (4 + A) | (uint32_t)B << 16) ^ 0x64806480u;
+    const half2v h = __builtin_bit_cast(half2v, u) - half2v{(_Float16)1152.f, (_Float16)1152.f};
+    return __builtin_bit_cast(uint32_t, h);
+}
+
+__device__ __forceinline__ half8 eight_codes(uint32_t lo, uint32_t hi) {
+    const uint4 w = make_uint4(two_codes<0, 1>(lo, lo), two_codes<2, 3>(lo, lo), two_codes<0, 1>(hi, hi), two_codes<2, 3>(hi, hi));
+    return __builtin_bit_cast(half8, w);
+}
+
+// The largest of the four lanes of a column.
+__device__ __forceinline__ float column_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16, 64));
+    return fmaxf(x, __shfl_xor(x, 32, 64));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    x += __shfl_xor(x, 16, 64);
+    return x + __shfl_xor(x, 32, 64);
+}
+
+// A workgroup's block of rows and run of tokens.
+struct CacheWork {
+    int n, item, kv, head0, heads, split;  // item: of (block, key head, heads), in the order of the partial results
+    int token0, tokens;  // the block's first token of the call, and how many
+    int place0;          // its place in the sequence
+    int end;             // tokens of the sequence that exist
+    // Work item `at`: runs of a block's rows are neighbours, then the blocks of a key head, the last first: with an order
+    // they have the most keys.
+    __device__ __forceinline__ bool find(const CacheAttnParams& p, int at, int lane) {
+        split = at % p.splits;
+        const int rest = at / p.splits;
+        return find_block(p, p.blocks - 1 - rest % p.blocks, rest / p.blocks, lane);
+    }
+    // Block `block` of tokens, part `part` of the heads.
+    __device__ __forceinline__ bool find_block(const CacheAttnParams& p, int block, int part, int lane) {
+        const int per_block = p.c.Mkv * p.groups;
+        if (part >= per_block) return false;
+        item = block * per_block + part;
+        kv = part / p.groups;
+        head0 = (part - kv * p.groups) * p.group;
+        heads = min(p.group, p.G - head0);
+        head0 += kv * p.G;
+        const Place at = p.c.start ? find_place(p.c, block, p.tokens, 1, lane) : Place{block, 0};
+        if (at.n < 0) return false;
+        n = at.n;
+        const Tokens t(p.c, n);
+        const int skip = at.block * p.tokens;
+        tokens = min(p.tokens, t.count - skip);
+        if (tokens <= 0) return false;
+        token0 = t.start + skip;
+        place0 = t.first + skip;
+        end = (int)min((int64_t)t.length, (int64_t)p.c.width << p.c.page_shift);
+        return true;
+    }
+    // Keys that token i of the block sees.
+    __device__ __forceinline__ int limit(const CacheAttnParams& p, int i) const {
+        return p.causal ? min(max(place0 + i + 1, 0), end) : end;
+    }
+    // Runs in which the block's rows see any key.
+    __device__ __forceinline__ int runs(const CacheAttnParams& p) const {
+        const int most = limit(p, tokens - 1);
+        return most <= 0 ? 0 : min((most - 1) / p.run + 1, p.splits);
+    }
+};
+
+// The pages of 64 columns of the sequence's table, one to a lane.
+struct Pages {
+    int first = -1;             // column of lane 0
+    int page;                   // -1: no tokens
+    float k_scale, bias, less;  // bias: log2 of the value scale relative to `base`, and kShift; less: 2^-bias
+    float base = 0.f;           // the largest value scale so far; sums are in units of it
+    // Loads columns `column` ..; returns the factor from the old unit to the new one.
+    __device__ __forceinline__ float load(const CacheAttnParams& p, const CacheWork& w, int column, int end, int lane) {
+        first = column;
+        page = -1;
+        k_scale = 0.f;
+        float v_scale = 0.f;
+        if (((int64_t)(column + lane) << p.c.page_shift) < end) page = page_at(p.c, w.n, column + lane);
+        if (page >= 0) {
+            const int64_t at = (int64_t)page * p.c.Mkv + w.kv;
+            k_scale = p.c.k_scale[at];
+            v_scale = p.c.v_scale[at];
+        }
+        if (!(k_scale >= 0.f && k_scale < kInf)) k_scale = __builtin_nanf("");
+        const bool odd = !(v_scale >= 0.f && v_scale < kInf);
+        float top = group_max<64>(odd ? 0.f : v_scale);
+        top = fmaxf(top, base);
+        const float unit = top > 0.f ? top : 1.f;
+        const float turn = base > 0.f ? base / unit : 1.f;
+        base = top;
+        // a scale below 2^-74 of the largest, or of 0, counts as that much: its values are lost beside others in fp32
+        bias = fmaxf((v_scale > 0.f ? __builtin_amdgcn_logf(v_scale) : -kInf) - __builtin_amdgcn_logf(unit), -74.f) + kShift;
+        less = exp2_of(-bias);
+        if (odd) {
+            bias = __builtin_nanf("");
+            less = 0.f;
+        }
+        return turn;
+    }
+};
+__device__ __forceinline__ float lane_value(float x, int lane) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
+// lse of a row's maximum (in units of log 2) and sum.
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2; }
+
+// Where the maxima and sums of partial results lie: behind their channels.
+template <int DP>
+__device__ __forceinline__ float2* stats_of(const CacheAttnParams& p, int rows) {
+    return reinterpret_cast<float2*>(p.part + (int64_t)p.blocks * p.c.Mkv * p.groups * rows * p.splits * DP);
+}
+
+// Four channels of a row, joined from partial results.
+struct Joined {
+    float m = -kInf, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+    __device__ __forceinline__ void take(float2 ml, float4 y) {
+        const float top = fmaxf(m, ml.x), base = top == -kInf ? 0.f : top;
+        const float u = exp2_of(m - base), v = exp2_of(ml.x - base);
+        m = top;
+        l = l * u + ml.y * v;
+        x[0] = x[0] * u + y.x * v;
+        x[1] = x[1] * u + y.y * v;
+        x[2] = x[2] * u + y.z * v;
+        x[3] = x[3] * u + y.w * v;
+    }
+    // at: the row's place in [T, M]
+    template <typename T>
+    __device__ __forceinline__ void store(const CacheAttnParams& p, int64_t at, int d) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] *= inv;
+        store_four(static_cast<T*>(p.out) + at * p.c.D, d, p.c.D, x);
+        if (p.lse && d == 0) p.lse[at] = lse_of(m, l);
+    }
+};
+
+// OWN: every wave has rows of its own and walks over all keys; otherwise the waves share the rows and take the 32 keys in
+// turn, and their results are joined in LDS.
+template <typename T, int DP, int NQ, bool OWN, bool CAP>
+__global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAttnParams p) {
+    constexpr bool kTwo = std::is_same_v<T, float>;
+    constexpr int kSteps = DP / 32, kBytes = DP / 16, kWords = (kBytes + 3) / 4;
+    constexpr int kRows = 16 * NQ * (OWN ? kCacheWaves : 1);
+    constexpr int kStride = DP + 4;  // of a row in LDS
+    __shared__ __attribute__((aligned(16))) float joined[OWN ? 1 : kCacheWaves * kRows * kStride];
+    __shared__ float2 stats[OWN ? 1 : kCacheWaves * kRows];
+    const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, g = lane >> 4;
+    CacheWork w;
+    if (!w.find(p, xcd_item(blockIdx.x, gridDim.x), lane)) return;
+    if (w.split >= max(w.runs(p), 1)) return;
+    const Cache& c = p.c;
+
+    // the lane's rows, and their queries
+    int limit[NQ];
+    float unit[NQ];  // of a raw score
+    half8 q[NQ][kSteps], q_low[kTwo ? NQ : 1][kSteps];
+    int lowest = 0x7fffffff, highest = 0;
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        const int row = (OWN ? wave * 16 * NQ : 0) + j * 16 + col, i = row / p.group, h = row - i * p.group;
+        const bool mine = i < w.tokens && h < w.heads;
+        limit[j] = mine ? w.limit(p, i) : 0;
+        highest = max(highest, limit[j]);
+        if (mine) lowest = min(lowest, limit[j]);
+        float x[kSteps][8];
+        float top = 0.f;
+        const T* from = static_cast<const T*>(p.q) + (int64_t)(w.token0 + (mine ? i : 0)) * p.qs[0] + (int64_t)(w.head0 + (mine ? h : 0)) * p.qs[1];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int d = DP == 32 ? g * 8 : (s / 2) * 64 + g * 16 + (s % 2) * 8;
+            const bool in = mine && d < c.D;
+            constexpr int kPer = 16 / sizeof(T);
+            if (p.vec) {
+#pragma unroll
+                for (int e = 0; e < 8; e += kPer) {
+                    Piece<T, kPer> y = {};
+                    if (in) y = *reinterpret_cast<const Piece<T, kPer>*>(from + d + e);
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) x[s][e + k] = (float)y.v[k];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[s][e] = in ? (float)from[d + e] : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[s][e]));
+        }
+        top = column_max(top);
+        int shift = top > 0.f && top < kInf ? 14 - ((int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127) : 0;
+        shift = min(shift, 126);
+        const float up = __builtin_bit_cast(float, (uint32_t)(shift + 127) << 23);
+        unit[j] = fminf(p.scale * (CAP ? 1.f : kLog2e) * __builtin_bit_cast(float, (uint32_t)(127 - shift) << 23), 3.4e38f);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = x[s][e] * up;
+                q[j][s][e] = (_Float16)y;
+                if constexpr (kTwo) q_low[j][s][e] = (_Float16)(y - (float)q[j][s][e]);
+            }
+    }
+#pragma unroll
+    for (int m = 1; m < 16; m *= 2) {
+        lowest = min(lowest, __shfl_xor(lowest, m, 64));
+        highest = max(highest, __shfl_xor(highest, m, 64));
+    }
+    lowest = __builtin_amdgcn_readfirstlane(lowest);
+    highest = __builtin_amdgcn_readfirstlane(highest);
+
+    float4v o[NQ][kBytes];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        m[j] = -kInf;
+        l[j] = 0.f;
+#pragma unroll
+        for (int u = 0; u < kBytes; ++u) o[j][u] = float4v{0.f, 0.f, 0.f, 0.f};
+    }
+    Pages pages;
+    // byte offsets of the lane within 16 keys; channels from D on are read as others: they meet zeros, or rows of no result
+    uint32_t k_at[DP == 32 ? 1 : DP / 64];
+#pragma unroll
+    for (int u = 0; u < (DP == 32 ? 1 : DP / 64); ++u) {
+        const int d = DP == 32 ? g * 8 : u * 64 + g * 16;
+        k_at[u] = col * c.D + (d < c.D ? d : 0);
+    }
+    const uint32_t v_at = 4 * g * c.D + (col * kBytes < c.D ? col * kBytes : 0);
+
+    const int run0 = w.split * p.run, run1 = (int)min((int64_t)highest, (int64_t)run0 + p.run);
+    for (int key0 = run0 + (OWN ? 0 : 32 * wave); key0 < run1; key0 += OWN ? 32 : 32 * kCacheWaves) {
+        const int columns[2] = {key0 >> c.page_shift, (key0 + 16) >> c.page_shift};
+        if (pages.first < 0 || columns[1] >= pages.first + 64) {
+            const float turn = pages.load(p, w, columns[0], highest, lane);
+#pragma unroll
+            for (int j = 0; j < NQ; ++j)
+#pragma unroll
+                for (int u = 0; u < kBytes; ++u) o[j][u] *= turn;
+        }
+        uint4 kx[2][DP == 32 ? 1 : DP / 64];
+        uint32_t vx[8][kWords];
+        float k_scale[2], bias[2], less[2];
+        int stop[2];  // 0 where there is no page
+        bool whole = key0 + 32 <= lowest;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int at = columns[t] - pages.first, slot = (key0 + 16 * t) & (c.page - 1);
+            const int page = __builtin_amdgcn_readlane(pages.page, at);
+            whole = whole && page >= 0;
+            stop[t] = page >= 0 ? 0x7fffffff : 0;
+            k_scale[t] = lane_value(pages.k_scale, at);
+            bias[t] = lane_value(pages.bias, at);
+            less[t] = lane_value(pages.less, at);
+            const int64_t base = (((int64_t)max(page, 0) * c.Mkv + w.kv) << c.page_shift) * c.D + (int64_t)slot * c.D;
+#pragma unroll
+            for (int u = 0; u < (DP == 32 ? 1 : DP / 64); ++u) {
+                if constexpr (DP == 32) {
+                    const uint2 y = *reinterpret_cast<const uint2*>(c.k + base + k_at[u]);
+                    kx[t][u] = make_uint4(y.x, y.y, 0, 0);
+                } else {
+                    kx[t][u] = *reinterpret_cast<const uint4*>(c.k + base + k_at[u]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int8_t* from = c.v + base + (int64_t)i * c.D + v_at;
+                if constexpr (kBytes == 8) {
+                    const uint2 y = *reinterpret_cast<const uint2*>(from);
+                    vx[4 * t + i][0] = y.x;
+                    vx[4 * t + i][1] = y.y;
+                } else if constexpr (kBytes == 4) {
+                    vx[4 * t + i][0] = *reinterpret_cast<const uint32_t*>(from);
+                } else {
+                    vx[4 * t + i][0] = *reinterpret_cast<const uint16_t*>(from);
+                }
+            }
+        }
+        float4v s[NQ][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) s[j][t] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                const uint4 x = kx[t][k / 2];
+                const half8 f = k % 2 ? eight_codes(x.z, x.w) : eight_codes(x.x, x.y);
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) {
+                    s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[j][k], s[j][t], 0, 0, 0);
+                    if constexpr (kTwo) s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q_low[j][k], s[j][t], 0, 0, 0);
+                }
+            }
+        }
+        half8 prob[NQ], prob_low[kTwo ? NQ : 1];
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            float top = -kInf;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const float by = unit[j] * k_scale[t];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float z = s[j][t][r] * by;
+                    if constexpr (CAP) z = p.softcap * kLog2e * tanh_of<true>(z, 1.f / p.softcap, 2.f * kLog2e / p.softcap);
+                    if (!whole) z = key0 + 16 * t + 4 * g + r < min(limit[j], stop[t]) ? z : -kInf;
+                    s[j][t][r] = z;
+                    top = fmaxf(top, z);
+                }
+            }
+            if (__any(top > m[j])) {
+                const float now = fmaxf(m[j], column_max(top));
+                const float fade = exp2_of(m[j] - (now == -kInf ? 0.f : now));
+                m[j] = now;
+                l[j] *= fade;
+#pragma unroll
+                for (int u = 0; u < kBytes; ++u) o[j][u] *= fade;
+            }
+            const float base = m[j] == -kInf ? 0.f : m[j];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float x = exp2_of(s[j][t][r] - (base - bias[t]));
+                    if (!whole) x = s[j][t][r] == -kInf ? 0.f : x;
+                    sum += x;
+                    prob[j][4 * t + r] = (_Float16)x;
+                    if constexpr (kTwo) prob_low[j][4 * t + r] = (_Float16)(x - (float)prob[j][4 * t + r]);
+                }
+                l[j] += sum * less[t];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kBytes; ++u) {
+            uint32_t f[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t a = vx[2 * i][u / 4], b = vx[2 * i + 1][u / 4];
+                f[i] = u % 4 == 0 ? two_codes<0, 0>(a, b) : u % 4 == 1 ? two_codes<1, 1>(a, b) : u % 4 == 2 ? two_codes<2, 2>(a, b) : two_codes<3, 3>(a, b);
+            }
+            const half8 v = __builtin_bit_cast(half8, make_uint4(f[0], f[1], f[2], f[3]));
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) {
+                o[j][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, prob[j], o[j][u], 0, 0, 0);
+                if constexpr (kTwo) o[j][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, prob_low[j], o[j][u], 0, 0, 0);
+            }
+        }
+    }
+
+    const float by = pages.base * exp2_of(-kShift);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        l[j] = column_sum(l[j]);
+#pragma unroll
+        for (int u = 0; u < kBytes; ++u) o[j][u] *= by;
+    }
+    if constexpr (OWN) {
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            const int row = wave * 16 * NQ + j * 16 + col, i = row / p.group, h = row - i * p.group;
+            if (i >= w.tokens || h >= w.heads) continue;
+            if (p.splits > 1) {
+                const int64_t at = ((int64_t)w.item * kRows + row) * p.splits + w.split;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int u = 0; u < kBytes; u += 2)
+                        *reinterpret_cast<float2*>(p.part + at * DP + (4 * g + r) * kBytes + u) = make_float2(o[j][u][r], o[j][u + 1][r]);
+                if (g == 0) stats_of<DP>(p, kRows)[at] = make_float2(m[j], l[j]);
+                continue;
+            }
+            const float inv = l[j] == 0.f ? 0.f : 1.f / l[j];
+            const int64_t at = (int64_t)(w.token0 + i) * p.M + w.head0 + h;
+            T* out = static_cast<T*>(p.out) + at * c.D;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = (4 * g + r) * kBytes;
+                if (d >= c.D) continue;
+                Piece<T, kBytes> y;
+#pragma unroll
+                for (int u = 0; u < kBytes; ++u) y.v[u] = (T)(o[j][u][r] * inv);
+                if constexpr (sizeof(y) <= 16) {
+                    *reinterpret_cast<Piece<T, kBytes>*>(out + d) = y;
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kBytes; u += 4) *reinterpret_cast<float4*>(out + d + u) = make_float4(y.v[u], y.v[u + 1], y.v[u + 2], y.v[u + 3]);
+                }
+            }
+            if (p.lse && g == 0) p.lse[at] = lse_of(m[j], l[j]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            float* mine = joined + (wave * kRows + j * 16 + col) * kStride;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int u = 0; u < kBytes; u += 2)
+                    *reinterpret_cast<float2*>(mine + (4 * g + r) * kBytes + u) = make_float2(o[j][u][r], o[j][u + 1][r]);
+            if (g == 0) stats[wave * kRows + j * 16 + col] = make_float2(m[j], l[j]);
+        }
+        __syncthreads();
+        for (int k = threadIdx.x; k < kRows * (DP / 4); k += 64 * kCacheWaves) {
+            const int row = k / (DP / 4), d = k % (DP / 4) * 4, i = row / p.group, h = row - i * p.group;
+            if (i >= w.tokens || h >= w.heads) continue;
+            Joined x;
+#pragma unroll
+            for (int v = 0; v < kCacheWaves; ++v)
+                x.take(stats[v * kRows + row], *reinterpret_cast<const float4*>(joined + (v * kRows + row) * kStride + d));
+            if (p.splits > 1) {
+                const int64_t at = ((int64_t)w.item * kRows + row) * p.splits + w.split;
+                *reinterpret_cast<float4*>(p.part + at * DP + d) = make_float4(x.x[0], x.x[1], x.x[2], x.x[3]);
+                if (d == 0) stats_of<DP>(p, kRows)[at] = make_float2(x.m, x.l);
+            } else {
+                x.template store<T>(p, (int64_t)(w.token0 + i) * p.M + w.head0 + h, d);
+            }
+        }
+    }
+}
+
+// Joins the runs of a block's rows: DP / 4 lanes to a row, a workgroup for each block.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p, int rows) {
+    const int lane = threadIdx.x & 63, per_block = p.c.Mkv * p.groups;
+    CacheWork w;
+    if (!w.find_block(p, blockIdx.x / per_block, blockIdx.x % per_block, lane)) return;
+    const int runs = max(w.runs(p), 1);
+    for (int k = threadIdx.x; k < w.tokens * p.group * (DP / 4); k += 256) {
+        const int row = k / (DP / 4), d = k % (DP / 4) * 4, i = row / p.group, h = row - i * p.group;
+        if (h >= w.heads) continue;
+        const int64_t at = ((int64_t)w.item * rows + row) * p.splits;
+        Joined x;
+#pragma unroll 4
+        for (int s = 0; s < runs; ++s)
+            x.take(stats_of<DP>(p, rows)[at + s], *reinterpret_cast<const float4*>(p.part + (at + s) * DP + d));
+        x.template store<T>(p, (int64_t)(w.token0 + i) * p.M + w.head0 + h, d);
+    }
+}
+
+template <typename T, int DP, bool CAP>
+hipError_t launch_rows(const CacheAttnParams& p, const CacheAttnPlan& plan, hipStream_t stream) {
+    const dim3 grid((unsigned)plan.workgroups), block(64 * kCacheWaves);
+    if (plan.rows == 16) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 1, false, CAP>), grid, block, 0, stream, p);
+    else if (plan.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 2, false, CAP>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((cache_attn_kernel<T, DP, 2, true, CAP>), grid, block, 0, stream, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    hipLaunchKernelGGL((cache_join_kernel<T, DP>), dim3((unsigned)((int64_t)p.blocks * p.c.Mkv * p.groups)), dim3(256), 0, stream, p,
+                       plan.rows);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_typed(const CacheAttnParams& p, const CacheAttnPlan& plan, hipStream_t stream) {
+    return by_channels(p.c.D, [&](auto dp) {
+        constexpr int DP = decltype(dp)::value;
+        return p.softcap > 0.f ? launch_rows<T, DP, true>(p, plan, stream) : launch_rows<T, DP, false>(p, plan, stream);
+    });
+}
+
+}  // namespace
+
+// Rows of a workgroup by what a sequence has on average, and runs so that the card is full.
+CacheAttnPlan cache_attn_plan(const CacheAttnParams& p, int dtype) {
+    (void)dtype;
+    CacheAttnPlan a;
+    const Cache& c = p.c;
+    const int64_t mean = c.start && c.N > 0 ? (c.T + c.N - 1) / c.N : 1, G = p.G;
+    a.rows = mean * G <= 16 ? 16 : mean * G <= 64 ? 32 : 128;
+    a.group = (int)(G < a.rows ? G : a.rows);
+    a.groups = (int)((G + a.group - 1) / a.group);
+    a.tokens = a.rows / a.group;
+    a.blocks = place_count(c, a.tokens, 1);
+    const int64_t items = a.blocks * c.Mkv * a.groups, longest = (int64_t)c.width * c.page;
+    const int64_t least = a.rows == 128 ? 512 : 256;  // tokens of a run
+    int64_t splits = items > 0 ? 2048 / items : 1;
+    if (a.rows == 128 && items >= 512) splits = 1;
+    if (splits > longest / least) splits = longest / least;
+    // the partial results have to fit into half a GB
+    const int64_t row_bytes = (attn_channels(c.D) + 2) * 4, most = ((int64_t)512 << 20) / (items * a.rows * row_bytes + 1);
+    if (splits > most) splits = most;
+    if (splits < 1) splits = 1;
+    int64_t run = (longest + splits - 1) / splits;
+    run = (run + 32 * kCacheWaves - 1) / (32 * kCacheWaves) * (32 * kCacheWaves);
+    a.run = (int)(run < 1 ? 32 * kCacheWaves : run);
+    a.splits = (int)((longest + a.run - 1) / a.run);
+    if (a.splits < 1) a.splits = 1;
+    a.workgroups = (items * a.splits + 7) / 8 * 8;  // see xcd_item
+    a.bytes = a.splits > 1 ? (size_t)(items * a.rows * a.splits) * row_bytes : 0;
+    return a;
+}
+
+hipError_t launch_cache_attn(const CacheAttnParams& p, const CacheAttnPlan& plan, int dtype, hipStream_t stream) {
+    if (dtype == MSDA_F32) return launch_typed<float>(p, plan, stream);
+    if (dtype == MSDA_F16) return launch_typed<_Float16>(p, plan, stream);
+    return launch_typed<bf16_t>(p, plan, stream);
+}
+
+}  // namespace msda

@@ -37,6 +37,9 @@ struct NormParams {
 int norm_backward_blocks(int64_t rows, int64_t C, int dtype);
 hipError_t launch_layernorm_forward(const NormParams& p, int dtype, hipStream_t stream);
 hipError_t launch_layernorm_backward(const NormParams& p, int dtype, hipStream_t stream);
+// Sums over `blocks` rows of `partial` [2][blocks][C] (or [blocks][C] without `second`), and zeros; either result may be null.
+hipError_t launch_column_sums(const float* partial, float* first, float* second, int C, int blocks, hipStream_t stream);
+hipError_t launch_column_zeros(float* first, float* second, int C, hipStream_t stream);
 
 // ---------------------------------------------------------------- rotary positions
 

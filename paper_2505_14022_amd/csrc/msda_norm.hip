@@ -12,59 +12,10 @@
 // Measured: 87296 rows x 1024 in fp16 take 80 us forward, 92 backward and 6 for the sums, 4.1 TB/s in all (a large copy
 // reaches 5.5); 39894 rows x 256 in bf16 with a residual 11, 16 and 5; 300 rows x 256 3.0, of a call of 13.4.
 #include "msda_layer.h"
-#include "msda_layer.hpp"
+#include "msda_rows.hpp"
 
 namespace msda {
 namespace {
-
-// Sums of NX values over the G lanes of a row; every lane of the row gets them. With G = NT the row is
-// the workgroup's: `red` holds the waves' sums, and all threads take part.
-template <int NT, int G, int NX>
-__device__ __forceinline__ void row_sums(float (&x)[NX], float* red) {
-#pragma unroll
-    for (int k = 0; k < NX; ++k) x[k] = group_sum<(G < 64 ? G : 64)>(x[k]);
-    if constexpr (G > 64) {
-        constexpr int W = NT / 64;
-        __syncthreads();  // the last sums have been read
-        if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-            for (int k = 0; k < NX; ++k) red[k * W + (threadIdx.x >> 6)] = x[k];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < NX; ++k) {
-            float t = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) t += red[k * W + w];
-            x[k] = t;
-        }
-    }
-}
-
-// The lane's columns of weight or bias (`none` without one), in 16-byte pieces if `pieces`.
-template <int VEC, int G, int NV>
-__device__ __forceinline__ void load_columns(float (&w)[NV][VEC], const float* from, float none, int g, int C, bool pieces) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int c = (j * G + g) * VEC;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) w[j][i] = none;
-        if (!from || c >= C) continue;
-        if (VEC % 4 == 0 && pieces) {
-#pragma unroll
-            for (int i = 0; i + 3 < VEC; i += 4) {
-                const float4 x = *reinterpret_cast<const float4*>(from + c + i);
-                w[j][i] = x.x;
-                w[j][i + 1] = x.y;
-                w[j][i + 2] = x.z;
-                w[j][i + 3] = x.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) w[j][i] = from[c + i];
-        }
-    }
-}
 
 template <typename T, int VEC, int NT, int G, int NV>
 __global__ __launch_bounds__(NT) void norm_fwd_kernel(NormParams p) {
@@ -266,38 +217,6 @@ __global__ __launch_bounds__(256) void norm_zero_kernel(float* grad_weight, floa
     if (grad_bias) grad_bias[c] = 0.f;
 }
 
-// Lanes per row and the row's pieces per lane: a lane keeps at most 16 elements, since the backward holds
-// five values of each. Called with a functor taking (threads, lanes, pieces) as integral constants.
-template <int N>
-using Int = std::integral_constant<int, N>;
-
-template <int VEC, typename F>
-hipError_t by_row(int C, F f) {
-    const int n = (C + VEC - 1) / VEC;
-    if (n <= 8) return f(Int<256>(), Int<8>(), Int<1>());
-    if (n <= 16) return f(Int<256>(), Int<16>(), Int<1>());
-    if (n <= 32) return f(Int<256>(), Int<32>(), Int<1>());
-    if (n <= 64) return f(Int<256>(), Int<64>(), Int<1>());
-    if (n <= 128) return f(Int<256>(), Int<64>(), Int<2>());
-    if (n <= 256) return f(Int<256>(), Int<256>(), Int<1>());
-    if (n <= 512) return f(Int<256>(), Int<256>(), Int<2>());
-    if (n <= 1024) return f(Int<1024>(), Int<1024>(), Int<1>());
-    if constexpr (VEC < 16) {
-        if (n <= 2048) return f(Int<1024>(), Int<1024>(), Int<2>());
-    }
-    if constexpr (VEC <= 4) {
-        if (n <= 4096) return f(Int<1024>(), Int<1024>(), Int<4>());
-    }
-    if constexpr (VEC == 1) return f(Int<1024>(), Int<1024>(), Int<16>());
-    return hipErrorInvalidValue;
-}
-
-// Rows of a workgroup of the backward (as by_row, for the host).
-int rows_per_block(int64_t C, int vec) {
-    const int64_t n = (C + vec - 1) / vec;
-    return n <= 8 ? 32 : n <= 16 ? 16 : n <= 32 ? 8 : n <= 128 ? 4 : 1;
-}
-
 template <typename T, int VEC, bool BWD>
 hipError_t launch_rows_of(const NormParams& p, hipStream_t stream) {
     return by_row<VEC>(p.C, [&](auto nt, auto g, auto nv) {
@@ -345,14 +264,21 @@ hipError_t launch_layernorm_forward(const NormParams& p, int dtype, hipStream_t 
 hipError_t launch_layernorm_backward(const NormParams& p, int dtype, hipStream_t stream) {
     if (p.rows == 0) {
         if (!p.grad_weight && !p.grad_bias) return hipSuccess;
-        hipLaunchKernelGGL(norm_zero_kernel, dim3((p.C + 255) / 256), dim3(256), 0, stream, p.grad_weight, p.grad_bias,
-                           p.C);
-        return hipGetLastError();
+        return launch_column_zeros(p.grad_weight, p.grad_bias, p.C, stream);
     }
     hipError_t e = launch_norm<true>(p, dtype, stream);
     if (e != hipSuccess || !p.partial) return e;
-    hipLaunchKernelGGL(norm_sum_kernel, dim3((p.C + 31) / 32, 2), dim3(1024), 0, stream, p.partial, p.grad_weight,
-                       p.grad_bias, p.C, p.blocks);
+    return launch_column_sums(p.partial, p.grad_weight, p.grad_bias, p.C, p.blocks, stream);
+}
+
+hipError_t launch_column_sums(const float* partial, float* first, float* second, int C, int blocks, hipStream_t stream) {
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((C + 31) / 32, second ? 2 : 1), dim3(1024), 0, stream, partial, first, second, C,
+                       blocks);
+    return hipGetLastError();
+}
+
+hipError_t launch_column_zeros(float* first, float* second, int C, hipStream_t stream) {
+    hipLaunchKernelGGL(norm_zero_kernel, dim3((C + 255) / 256), dim3(256), 0, stream, first, second, C);
     return hipGetLastError();
 }
 

@@ -1,0 +1,239 @@
+// Matrix product of 8-bit integers with a scale for each row of both:
+//   out[t, o] = (sum_k a[t, k] b[o, k]) (a_scale[t] b_scale[o]) + bias[o]
+// Sums are 32-bit integers from the matrix instructions, exact up to 131071 products of two codes. The rows of b (a
+// layer's weights) are the instructions' rows and the tokens their columns, so that a lane holds consecutive channels of
+// one token and stores them together.
+// Few tokens: bound by reading b once. A workgroup owns 16 channels and its waves share the sum: each reads rows of b
+// straight into its registers, and the waves' sums are added in LDS. Many tokens: bound by the matrix unit. Tiles of both go to LDS past the
+// registers while the previous ones are multiplied; 16-byte pieces of a row of 128 are permuted by the row's number, so that
+// reads of one column of pieces spread over the banks.
+#include "msda_layer.hpp"
+#include "msda_serve.h"
+
+namespace msda {
+namespace {
+
+typedef int int4_t __attribute__((ext_vector_type(4)));
+typedef int int16_t_ __attribute__((ext_vector_type(16)));
+
+// Pieces k .. k + 15 of a row, zeros from K on.
+template <bool PIECES>
+__device__ __forceinline__ int4_t load_codes(const int8_t* row, int k, int K) {
+    int4_t x = {0, 0, 0, 0};
+    if (PIECES) {
+        if (k < K) x = *reinterpret_cast<const int4_t*>(row + k);
+    } else if (k + 16 <= K) {
+        __builtin_memcpy(&x, row + k, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (k + i < K) x[i / 4] |= (int)(uint8_t)row[k + i] << (8 * (i % 4));
+    }
+    return x;
+}
+
+// Four consecutive channels of a token, from their sums.
+template <typename T>
+__device__ __forceinline__ void store_sums(const ProductParams& p, int64_t t, int o, const int (&sum)[4], float a_scale) {
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int c = o + e < p.O ? o + e : p.O - 1;
+        y[e] = (float)sum[e] * (a_scale * p.b_scale[c]);
+        if (p.bias) y[e] += p.bias[c];
+    }
+    T* to = static_cast<T*>(p.out) + t * p.O + o;
+    if (p.wide && o + 4 <= p.O) {
+        Piece<T, 4> x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.v[e] = (T)y[e];
+        *reinterpret_cast<Piece<T, 4>*>(to) = x;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (o + e < p.O) to[e] = (T)y[e];
+    }
+}
+
+constexpr int kRowWaves = 8, kRowSteps = 4;  // waves of a workgroup, and 64-byte steps of a wave that are loaded together
+
+template <typename T, int NT, bool PIECES>
+__global__ __launch_bounds__(64 * kRowWaves) void product_rows_kernel(ProductParams p, int across) {
+    __shared__ int4_t part[kRowWaves][NT][64];
+    const int lane = threadIdx.x & 63, wave = wave_index(), r = lane & 15, g = lane >> 4;
+    const int t0 = (blockIdx.x / across) * 16 * NT, o0 = (blockIdx.x % across) * 16;
+    const int8_t* b = p.b + (int64_t)min(o0 + r, p.O - 1) * p.K;
+    const int8_t* a[NT];
+    int4_t acc[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        a[n] = p.a + (int64_t)min(t0 + n * 16 + r, p.T - 1) * p.K;
+        acc[n] = int4_t{0, 0, 0, 0};
+    }
+    for (int k0 = wave * kRowSteps * 64; k0 < p.K; k0 += kRowWaves * kRowSteps * 64) {
+        int4_t x[kRowSteps], y[NT][kRowSteps];
+#pragma unroll
+        for (int s = 0; s < kRowSteps; ++s) {
+            x[s] = load_codes<PIECES>(b, k0 + s * 64 + g * 16, p.K);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) y[n][s] = load_codes<PIECES>(a[n], k0 + s * 64 + g * 16, p.K);
+        }
+#pragma unroll
+        for (int s = 0; s < kRowSteps; ++s)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[s], y[n][s], acc[n], 0, 0, 0);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) part[wave][n][lane] = acc[n];
+    __syncthreads();
+    if (wave >= NT) return;
+    int4_t sum = part[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < kRowWaves; ++w) sum += part[w][wave][lane];
+    const int t = t0 + wave * 16 + r, o = o0 + 4 * g;
+    if (t >= p.T || o >= p.O) return;
+    const int four[4] = {sum[0], sum[1], sum[2], sum[3]};
+    store_sums<T>(p, t, o, four, p.a_scale[t]);
+}
+
+// ---------------------------------------------------------------- tiles
+
+__device__ const int4_t kZeroPiece[1] = {{0, 0, 0, 0}};
+
+// Tiles of BM tokens and BN channels, WM x WN waves, 128 bytes of every row at a time.
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void product_tiles_kernel(ProductParams p, int across) {
+    constexpr int kWaves = WM * WN, kTM = BM / WM / 32, kTN = BN / WN / 32;  // 32 x 32 blocks of a wave
+    constexpr int kRows = BM + BN, kLoads = kRows / 8 / kWaves;              // 8 rows a load of a wave
+    __shared__ __attribute__((aligned(16))) int8_t tile[2][kRows * 128];
+    const int lane = threadIdx.x & 63, wave = wave_index(), wm = wave / WN, wn = wave % WN;
+    const int t0 = (blockIdx.x / across) * BM, o0 = (blockIdx.x % across) * BN;
+    const int8_t* from[kLoads];
+    const int piece = (lane & 7) ^ (lane >> 3);  // of the row that the lane's place in LDS holds
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int row = (wave * kLoads + i) * 8 + (lane >> 3);
+        from[i] = row < BM ? p.a + (int64_t)min(t0 + row, p.T - 1) * p.K : p.b + (int64_t)min(o0 + row - BM, p.O - 1) * p.K;
+        from[i] += piece * 16;
+    }
+    auto load = [&](int k0, int s) {
+        auto put = [&](int i, const void* src) {
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                             (__attribute__((address_space(3))) void*)(tile[s] + (wave * kLoads + i) * 1024), 16,
+                                             0, 0);
+        };
+        if (k0 + 128 <= p.K) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) put(i, from[i] + k0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) put(i, k0 + piece * 16 < p.K ? (const void*)(from[i] + k0) : (const void*)kZeroPiece);
+        }
+    };
+    int16_t_ acc[kTN][kTM];
+#pragma unroll
+    for (int n = 0; n < kTN; ++n)
+#pragma unroll
+        for (int m = 0; m < kTM; ++m) acc[n][m] = int16_t_{};
+    const int lr = lane & 31, lh = lane >> 5;
+    auto fragment = [&](int s, int row, int step) {
+        return *reinterpret_cast<const int4_t*>(tile[s] + row * 128 + (((step * 2 + lh) ^ (row & 7)) << 4));
+    };
+    load(0, 0);
+    int s = 0;
+    for (int k0 = 0; k0 < p.K; k0 += 128, s ^= 1) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the wave's pieces are in LDS
+        __syncthreads();                     // everybody's are, and the other buffer has been read
+        if (k0 + 128 < p.K) load(k0 + 128, s ^ 1);
+#pragma unroll
+        for (int step = 0; step < 4; ++step) {
+            int4_t x[kTN], y[kTM];
+#pragma unroll
+            for (int n = 0; n < kTN; ++n) x[n] = fragment(s, BM + (wn * kTN + n) * 32 + lr, step);
+#pragma unroll
+            for (int m = 0; m < kTM; ++m) y[m] = fragment(s, (wm * kTM + m) * 32 + lr, step);
+#pragma unroll
+            for (int n = 0; n < kTN; ++n)
+#pragma unroll
+                for (int m = 0; m < kTM; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[n], y[m], acc[n][m], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < kTM; ++m) {
+        const int t = t0 + (wm * kTM + m) * 32 + lr;
+        if (t >= p.T) continue;
+        const float a_scale = p.a_scale[t];
+#pragma unroll
+        for (int n = 0; n < kTN; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int o = o0 + (wn * kTN + n) * 32 + 8 * q + 4 * lh;
+                const int four[4] = {acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
+                if (o < p.O) store_sums<T>(p, t, o, four, a_scale);
+            }
+    }
+}
+
+template <typename T, int NT>
+void launch_rows(const ProductParams& p, int64_t workgroups, hipStream_t stream) {
+    const dim3 grid((unsigned)workgroups), block(64 * kRowWaves);
+    const int across = (p.O + 15) / 16;
+    if (p.pieces) hipLaunchKernelGGL((product_rows_kernel<T, NT, true>), grid, block, 0, stream, p, across);
+    else hipLaunchKernelGGL((product_rows_kernel<T, NT, false>), grid, block, 0, stream, p, across);
+}
+
+template <typename T, int BM, int BN, int WM, int WN>
+void launch_tiles(const ProductParams& p, int64_t workgroups, hipStream_t stream) {
+    hipLaunchKernelGGL((product_tiles_kernel<T, BM, BN, WM, WN>), dim3((unsigned)workgroups), dim3(64 * WM * WN), 0, stream, p,
+                       (p.O + BN - 1) / BN);
+}
+
+template <typename T>
+hipError_t launch_typed(const ProductParams& p, hipStream_t stream) {
+    const ProductPlan plan = product_plan(p);
+    if (plan.channels == 16) {
+        if (plan.tokens == 16) launch_rows<T, 1>(p, plan.workgroups, stream);
+        else if (plan.tokens == 32) launch_rows<T, 2>(p, plan.workgroups, stream);
+        else launch_rows<T, 4>(p, plan.workgroups, stream);
+    } else if (plan.tokens == 256) {
+        launch_tiles<T, 256, 256, 2, 4>(p, plan.workgroups, stream);
+    } else if (plan.tokens == 128) {
+        launch_tiles<T, 128, 128, 2, 2>(p, plan.workgroups, stream);
+    } else {
+        launch_tiles<T, 64, 64, 2, 2>(p, plan.workgroups, stream);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+ProductPlan product_plan(const ProductParams& p) {
+    ProductPlan a;
+    auto tiles = [&](int tokens, int channels) {
+        return ((int64_t)p.T + tokens - 1) / tokens * (((int64_t)p.O + channels - 1) / channels);
+    };
+    auto take = [&](int tokens, int channels, int waves) {
+        a.tokens = tokens;
+        a.channels = channels;
+        a.waves = waves;
+        a.workgroups = tiles(tokens, channels);
+    };
+    if (!p.pieces || p.T <= 64) {
+        take(p.T <= 16 ? 16 : p.T <= 32 ? 32 : 64, 16, kRowWaves);
+    } else if (tiles(256, 256) >= 256) {
+        take(256, 256, 8);
+    } else if (tiles(128, 128) >= 256) {
+        take(128, 128, 4);
+    } else {
+        take(64, 64, 4);
+    }
+    return a;
+}
+
+hipError_t launch_product(const ProductParams& p, int dtype, hipStream_t stream) {
+    if (dtype == MSDA_F32) return launch_typed<float>(p, stream);
+    if (dtype == MSDA_F16) return launch_typed<_Float16>(p, stream);
+    return launch_typed<bf16_t>(p, stream);
+}
+
+}  // namespace msda

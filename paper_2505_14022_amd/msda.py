@@ -28,6 +28,8 @@ MSDA_MAX_LEVELS = 16
 MSDA_LAYERNORM_MAX_C = 16384
 MSDA_ROTARY_MAX_D = 1024
 MSDA_ATTENTION_MAX_D = 128
+MSDA_QUANTIZED_MAX_K = 131071
+MSDA_CACHE_MAX_D = 128
 MSDA_WORKSPACE_PREFERRED = 0
 MSDA_WORKSPACE_OWNER = 1
 MSDA_WORKSPACE_DETERMINISTIC = 2
@@ -38,7 +40,10 @@ EXPORTED = ["msda_check_args", "msda_forward", "msda_backward", "msda_backward_a
             "msda_status_string", "msda_last_error", "msda_version", "msda_release", "msda_backward_noalloc",
             "msda_layernorm_forward", "msda_layernorm_backward", "msda_layernorm_backward_workspace_size",
             "msda_rotary_forward", "msda_rotary_backward",
-            "msda_attention_forward", "msda_attention_backward", "msda_attention_workspace_size"]
+            "msda_attention_forward", "msda_attention_backward", "msda_attention_workspace_size",
+            "msda_rmsnorm_forward", "msda_rmsnorm_quantize", "msda_rmsnorm_backward", "msda_rmsnorm_backward_workspace_size",
+            "msda_quantize_rows", "msda_quantized_matmul", "msda_cache_append", "msda_cache_attention",
+            "msda_cache_attention_workspace_size"]
 MSDA_NOALLOC_SCRATCH_BYTES = 128 << 20
 
 
@@ -54,6 +59,12 @@ class AttentionDescription(ctypes.Structure):
         [("dtype", ctypes.c_int), ("causal", ctypes.c_int), ("unaligned", ctypes.c_int), ("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + \
         [(name, ctypes.c_int64 * 3) for name in ("q_stride", "k_stride", "v_stride")] + \
         [(name, ctypes.c_void_p) for name in ("slopes", "q_pos", "k_pos", "q_doc", "k_doc", "prefix")]
+
+
+class CacheDescription(ctypes.Structure):
+    """msda_cache_t."""
+    _fields_ = [(name, ctypes.c_int64) for name in ("N", "pages", "page_size", "Mkv", "D", "width", "table_stride")] + \
+        [(name, ctypes.c_void_p) for name in ("k", "v", "k_scale", "v_scale", "table", "length", "start")]
 
 
 _lib = None
@@ -116,6 +127,18 @@ def lib():
         L.msda_attention_forward.restype = ctypes.c_int
         L.msda_attention_backward.argtypes = [desc] + [vp] * 10 + [size, vp]
         L.msda_attention_backward.restype = ctypes.c_int
+        L.msda_rmsnorm_forward.argtypes = [vp] * 6 + [i64, i64, f32, ctypes.c_int, vp]
+        L.msda_rmsnorm_quantize.argtypes = [vp] * 6 + [i64, i64, f32, ctypes.c_int, vp]
+        L.msda_rmsnorm_backward_workspace_size.argtypes = [i64, i64, ctypes.c_int, sizep]
+        L.msda_rmsnorm_backward.argtypes = [vp] * 9 + [size, i64, i64, ctypes.c_int, vp]
+        L.msda_quantize_rows.argtypes = [vp] * 3 + [i64, i64, ctypes.c_int, vp]
+        L.msda_quantized_matmul.argtypes = [vp] * 6 + [i64, i64, i64, ctypes.c_int, vp]
+        cache = ctypes.POINTER(CacheDescription)
+        L.msda_cache_append.argtypes = [cache, vp, ip, vp, ip, vp, vp, i64, i64, i64, ctypes.c_int, ctypes.c_int, vp]
+        L.msda_cache_attention_workspace_size.argtypes = [cache, i64, i64, ctypes.c_int, sizep]
+        L.msda_cache_attention.argtypes = [cache, vp, ip, vp, vp, i64, i64, f32, f32, ctypes.c_int, ctypes.c_int, vp, size, vp]
+        for name in EXPORTED[-9:]:
+            getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -728,3 +751,237 @@ def attention_backward(q, k, v, out, lse, grad_out, scale=None, softcap: float =
                                           _address(grad_v), _address(ws), _bytes(ws), s)
     _raise(r, "msda_attention_backward")
     return grad_q, grad_k, grad_v
+
+
+# ---------------------------------------------------------------- serving operators
+
+
+def rmsnorm_workspace_size(rows, C, dtype) -> int:
+    """msda_rmsnorm_backward_workspace_size: bytes of device workspace for the sums over rows."""
+    out = ctypes.c_size_t(0)
+    _raise(lib().msda_rmsnorm_backward_workspace_size(rows, C, int(dtype), ctypes.byref(out)),
+           "msda_rmsnorm_backward_workspace_size")
+    return int(out.value)
+
+
+def rmsnorm_forward(x, weight=None, residual=None, eps=1e-6, want_sum: bool = False, out=None, rstd=None, sum=None,
+                    stream=None):
+    """(out, rstd) from msda_rmsnorm_forward: root-mean-square norm of x + residual over the last dimension; with
+    want_sum (or a `sum` tensor) also x + residual itself, as a third result. weight is fp32."""
+    import torch
+
+    rows, C = _rows(x)
+    code = _layer_dtype(x)
+    _expect("x", x, x.shape, x.dtype, x)
+    for name, t in (("residual", residual), ("out", out), ("sum", sum)):
+        _expect(name, t, x.shape, x.dtype, x)
+    _expect("weight", weight, (C,), torch.float32, x)
+    _expect("rstd", rstd, x.shape[:-1], torch.float32, x)
+    context, s = _launching(x, stream)
+    with context:
+        out = torch.empty_like(x) if out is None else out
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
+        sum = torch.empty_like(x) if sum is None and want_sum else sum
+        r = lib().msda_rmsnorm_forward(_address(x), _address(residual), _address(weight), _address(out), _address(sum),
+                                       _address(rstd), rows, C, float(eps), code, s)
+    _raise(r, "msda_rmsnorm_forward")
+    return (out, rstd) if sum is None else (out, rstd, sum)
+
+
+def rmsnorm_quantize(x, weight=None, residual=None, eps=1e-6, want_sum: bool = False, codes=None, scale=None, sum=None,
+                     stream=None):
+    """(codes, scale) from msda_rmsnorm_quantize: rmsnorm_forward's result in 8 bits, codes (int8, x's shape) times scale
+    (fp32, one for each row); with want_sum (or a `sum` tensor) also x + residual, as a third result."""
+    import torch
+
+    rows, C = _rows(x)
+    code = _layer_dtype(x)
+    _expect("x", x, x.shape, x.dtype, x)
+    for name, t in (("residual", residual), ("sum", sum)):
+        _expect(name, t, x.shape, x.dtype, x)
+    _expect("weight", weight, (C,), torch.float32, x)
+    _expect("codes", codes, x.shape, torch.int8, x)
+    _expect("scale", scale, x.shape[:-1], torch.float32, x)
+    context, s = _launching(x, stream)
+    with context:
+        codes = torch.empty(x.shape, dtype=torch.int8, device=x.device) if codes is None else codes
+        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scale is None else scale
+        sum = torch.empty_like(x) if sum is None and want_sum else sum
+        r = lib().msda_rmsnorm_quantize(_address(x), _address(residual), _address(weight), _address(codes), _address(scale),
+                                        _address(sum), rows, C, float(eps), code, s)
+    _raise(r, "msda_rmsnorm_quantize")
+    return (codes, scale) if sum is None else (codes, scale, sum)
+
+
+def rmsnorm_backward(x, grad_out, rstd, weight=None, residual=None, grad_sum=None, want_weight_grad: bool = True, grad_x=None,
+                     grad_weight=None, workspace="auto", stream=None):
+    """(grad_x, grad_weight) from msda_rmsnorm_backward; grad_x is the gradient of x and of residual. Without
+    want_weight_grad the last is None (or the tensor given). grad_sum: the gradient of the forward's `sum`."""
+    import torch
+
+    rows, C = _rows(x)
+    code = _layer_dtype(x)
+    _expect("x", x, x.shape, x.dtype, x)
+    for name, t in (("residual", residual), ("grad_out", grad_out), ("grad_sum", grad_sum), ("grad_x", grad_x)):
+        _expect(name, t, x.shape, x.dtype, x)
+    for name, t in (("weight", weight), ("grad_weight", grad_weight)):
+        _expect(name, t, (C,), torch.float32, x)
+    _expect("rstd", rstd, x.shape[:-1], torch.float32, x)
+    context, s = _launching(x, stream)
+    with context:
+        grad_x = torch.empty_like(x) if grad_x is None else grad_x
+        if want_weight_grad and grad_weight is None:
+            grad_weight = torch.empty(C, dtype=torch.float32, device=x.device)
+        ws = _workspace(workspace, 0 if grad_weight is None else rmsnorm_workspace_size(rows, C, code), x)
+        r = lib().msda_rmsnorm_backward(_address(x), _address(residual), _address(weight), _address(grad_out),
+                                        _address(grad_sum), _address(rstd), _address(grad_x), _address(grad_weight),
+                                        _address(ws), _bytes(ws), rows, C, code, s)
+    _raise(r, "msda_rmsnorm_backward")
+    return grad_x, grad_weight
+
+
+def quantize_rows(x, codes=None, scale=None, stream=None):
+    """(codes, scale) from msda_quantize_rows: x in 8 bits, codes (int8, x's shape) times scale (fp32, one for each row of the
+    last dimension)."""
+    import torch
+
+    rows, C = _rows(x)
+    code = _layer_dtype(x)
+    _expect("x", x, x.shape, x.dtype, x)
+    _expect("codes", codes, x.shape, torch.int8, x)
+    _expect("scale", scale, x.shape[:-1], torch.float32, x)
+    context, s = _launching(x, stream)
+    with context:
+        codes = torch.empty(x.shape, dtype=torch.int8, device=x.device) if codes is None else codes
+        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scale is None else scale
+        r = lib().msda_quantize_rows(_address(x), _address(codes), _address(scale), rows, C, code, s)
+    _raise(r, "msda_quantize_rows")
+    return codes, scale
+
+
+def quantized_matmul(a, b, a_scale, b_scale, bias=None, dtype=None, out=None, stream=None):
+    """out [..., O] from msda_quantized_matmul: codes a [..., K] (int8) times codes b [O, K] (int8), with scales a_scale [...]
+    and b_scale [O] and a bias [O] (fp32). dtype of the result: float32, float16 or bfloat16 (`out`'s, or bfloat16)."""
+    import torch
+
+    rows, K = _rows(a)
+    if b.dim() != 2:
+        raise ValueError(f"b must be [O, K], not {tuple(b.shape)}")
+    O = b.shape[0]
+    dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
+    shape = a.shape[:-1] + (O,)
+    _expect("a", a, a.shape, torch.int8, a)
+    _expect("b", b, (O, K), torch.int8, a)
+    _expect("a_scale", a_scale, a.shape[:-1], torch.float32, a)
+    for name, t in (("b_scale", b_scale), ("bias", bias)):
+        _expect(name, t, (O,), torch.float32, a)
+    _expect("out", out, shape, dtype, a)
+    context, s = _launching(a, stream)
+    with context:
+        out = torch.empty(shape, dtype=dtype, device=a.device) if out is None else out
+        r = lib().msda_quantized_matmul(_address(a), _address(b), _address(a_scale), _address(b_scale), _address(bias),
+                                        _address(out), rows, K, O, _layer_dtype(out), s)
+    _raise(r, "msda_quantized_matmul")
+    return out
+
+
+def _two_strides(t):
+    return (ctypes.c_int64 * 2)(*t.stride()[:2])
+
+
+def _cache(T, k_cache, v_cache, k_scale, v_scale, table, length, start):
+    """The call's msda_cache_t, after the checks of its tensors."""
+    import torch
+
+    if k_cache.dim() != 4 or table.dim() != 2:
+        raise ValueError(f"k_cache must be [pages, Mkv, page_size, D] and table [N, width], not {tuple(k_cache.shape)} and "
+                         f"{tuple(table.shape)}")
+    pages, Mkv, page_size, D = k_cache.shape
+    N, width = table.shape
+    _expect("k_cache", k_cache, k_cache.shape, torch.int8, k_cache)
+    _expect("v_cache", v_cache, k_cache.shape, torch.int8, k_cache)
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        _expect(name, t, (pages, Mkv), torch.float32, k_cache)
+    _expect("table", table, (N, width), torch.int32, k_cache, strided=True)
+    _expect("length", length, (N,), torch.int32, k_cache)
+    _expect("start", start, (N + 1,), torch.int32, k_cache)
+    return CacheDescription(N, pages, page_size, Mkv, D, width, table.stride(0),
+                            *(_address(t) for t in (k_cache, v_cache, k_scale, v_scale, table, length, start)))
+
+
+def cache_append(k, v, k_cache, v_cache, k_scale, v_scale, table, length, start=None, pos=None, freqs=None,
+                 interleaved: bool = False, stream=None):
+    """Appends k and v [T, Mkv, D] to a paged cache in place, from msda_cache_append.
+
+    k_cache and v_cache [pages, Mkv, page_size, D] (int8) with k_scale and v_scale [pages, Mkv] (fp32); table [N, width]
+    (int32): the pages of each sequence, a view of a wider table's first columns is taken; length [N] (int32): tokens of each
+    sequence, the new ones included; start [N + 1] (int32): the first of each sequence's new tokens among the T, or None: one
+    each. freqs [A, R] (fp32): k is turned by pos [T, A] (fp32; None: a token's place in its sequence, A == 1) on the way,
+    as by rotary_forward. k and v may be views whose channels are contiguous.
+    """
+    import torch
+
+    if k.dim() != 3 or (freqs is not None and freqs.dim() != 2):
+        raise ValueError(f"k must be [T, Mkv, D] and freqs [A, R], not {tuple(k.shape)} and "
+                         f"{None if freqs is None else tuple(freqs.shape)}")
+    if freqs is None and pos is not None:
+        raise ValueError("pos needs freqs")
+    T = k.shape[0]
+    A, R = (1, 0) if freqs is None else freqs.shape
+    code = _layer_dtype(k)
+    c = _cache(T, k_cache, v_cache, k_scale, v_scale, table, length, start)
+    _expect("k", k, (T, c.Mkv, c.D), k.dtype, k_cache, strided=True)
+    _expect("v", v, (T, c.Mkv, c.D), k.dtype, k_cache, strided=True)
+    _expect("pos", pos, (T, A), torch.float32, k_cache)
+    _expect("freqs", freqs, (A, R), torch.float32, k_cache)
+    context, s = _launching(k_cache, stream)
+    with context:
+        r = lib().msda_cache_append(ctypes.byref(c), _address(k), _two_strides(k), _address(v), _two_strides(v), _address(pos),
+                                    _address(freqs), T, A, R, int(bool(interleaved)), code, s)
+    _raise(r, "msda_cache_append")
+
+
+def _cache_attention_workspace(c, T, M, code) -> int:
+    out = ctypes.c_size_t(0)
+    _raise(lib().msda_cache_attention_workspace_size(ctypes.byref(c), T, M, code, ctypes.byref(out)),
+           "msda_cache_attention_workspace_size")
+    return int(out.value)
+
+
+def cache_attention_workspace_size(q, k_cache, v_cache, k_scale, v_scale, table, length, start=None) -> int:
+    """msda_cache_attention_workspace_size of the call with these arguments."""
+    c = _cache(q.shape[0], k_cache, v_cache, k_scale, v_scale, table, length, start)
+    return _cache_attention_workspace(c, q.shape[0], q.shape[1], _layer_dtype(q))
+
+
+def cache_attention(q, k_cache, v_cache, k_scale, v_scale, table, length, start=None, scale=None, softcap: float = 0.0,
+                    causal: bool = True, want_lse: bool = True, out=None, lse=None, workspace="auto", stream=None):
+    """(out [T, M, D], lse [T, M] or None) of the new tokens' queries q [T, M, D] over a paged cache, from
+    msda_cache_attention.
+
+    The cache's arguments as in cache_append, which has stored the new tokens' keys and values already; M is a multiple of Mkv;
+    q may be a view whose channels are contiguous. scale: D ** -0.5 when None. softcap: cap of the scores (0: none). causal:
+    a token sees those up to itself, otherwise all of its sequence. workspace: "auto" allocates it, or a caller-owned uint8
+    tensor of cache_attention_workspace_size bytes.
+    """
+    import torch
+
+    if q.dim() != 3:
+        raise ValueError(f"q must be [T, M, D], not {tuple(q.shape)}")
+    T, M, D = q.shape
+    code = _layer_dtype(q)
+    c = _cache(T, k_cache, v_cache, k_scale, v_scale, table, length, start)
+    _expect("q", q, (T, M, c.D), q.dtype, k_cache, strided=True)
+    _expect("out", out, q.shape, q.dtype, k_cache)
+    _expect("lse", lse, (T, M), torch.float32, k_cache)
+    context, s = _launching(k_cache, stream)
+    with context:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        if lse is None and want_lse:
+            lse = torch.empty((T, M), dtype=torch.float32, device=q.device)
+        ws = _workspace(workspace, _cache_attention_workspace(c, T, M, code), k_cache)
+        r = lib().msda_cache_attention(ctypes.byref(c), _address(q), _two_strides(q), _address(out), _address(lse), T, M,
+                                       D ** -0.5 if scale is None else float(scale), float(softcap), int(bool(causal)), code,
+                                       _address(ws), _bytes(ws), s)
+    _raise(r, "msda_cache_attention")
+    return out, lse
