@@ -36,8 +36,15 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t x, uint32_t y) {
     return __builtin_bit_cast(uint32_t, h);
 }
 
+// The bytes of two words, the same way: c ^ 0x80 for four at once, and the exponent's byte from a constant.
 __device__ __forceinline__ half8 eight_codes(uint32_t lo, uint32_t hi) {
-    const uint4 w = make_uint4(two_codes<0, 1>(lo, lo), two_codes<2, 3>(lo, lo), two_codes<0, 1>(hi, hi), two_codes<2, 3>(hi, hi));
+    const half2v off = {(_Float16)1152.f, (_Float16)1152.f};
+    auto two = [&](uint32_t x, uint32_t selector) {
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2v, __builtin_amdgcn_perm(x, 0x64646464u, selector)) - off);
+    };
+    lo ^= 0x80808080u;
+    hi ^= 0x80808080u;
+    const uint4 w = make_uint4(two(lo, 0x00050004u), two(lo, 0x00070006u), two(hi, 0x00050004u), two(hi, 0x00070006u));
     return __builtin_bit_cast(half8, w);
 }
 
@@ -114,9 +121,13 @@ struct Pages {
             k_scale = p.c.k_scale[at];
             v_scale = p.c.v_scale[at];
         }
-        if (!(k_scale >= 0.f && k_scale < kInf)) k_scale = __builtin_nanf("");
-        const bool odd = !(v_scale >= 0.f && v_scale < kInf);
-        float top = group_max<64>(odd ? 0.f : v_scale);
+        // the scores of a page that makes NaN are NaN, which a row that does not see it replaces
+        const bool odd = !(k_scale >= 0.f && k_scale < kInf && v_scale >= 0.f && v_scale < kInf);
+        if (odd) {
+            k_scale = __builtin_nanf("");
+            v_scale = 0.f;
+        }
+        float top = group_max<64>(v_scale);
         top = fmaxf(top, base);
         const float unit = top > 0.f ? top : 1.f;
         const float turn = base > 0.f ? base / unit : 1.f;
@@ -124,10 +135,6 @@ struct Pages {
         // a scale below 2^-74 of the largest, or of 0, counts as that much: its values are lost beside others in fp32
         bias = fmaxf((v_scale > 0.f ? __builtin_amdgcn_logf(v_scale) : -kInf) - __builtin_amdgcn_logf(unit), -74.f) + kShift;
         less = exp2_of(-bias);
-        if (odd) {
-            bias = __builtin_nanf("");
-            less = 0.f;
-        }
         return turn;
     }
 };
@@ -168,41 +175,29 @@ struct Joined {
     }
 };
 
-// OWN: every wave has rows of its own and walks over all keys; otherwise the waves share the rows and take the 32 keys in
-// turn, and their results are joined in LDS.
-template <typename T, int DP, int NQ, bool OWN, bool CAP>
-__global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAttnParams p) {
-    constexpr bool kTwo = std::is_same_v<T, float>;
-    constexpr int kSteps = DP / 32, kBytes = DP / 16, kWords = (kBytes + 3) / 4;
-    constexpr int kRows = 16 * NQ * (OWN ? kCacheWaves : 1);
-    constexpr int kStride = DP + 4;  // of a row in LDS
-    __shared__ __attribute__((aligned(16))) float joined[OWN ? 1 : kCacheWaves * kRows * kStride];
-    __shared__ float2 stats[OWN ? 1 : kCacheWaves * kRows];
-    const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, g = lane >> 4;
-    CacheWork w;
-    if (!w.find(p, xcd_item(blockIdx.x, gridDim.x), lane)) return;
-    if (w.split >= max(w.runs(p), 1)) return;
-    const Cache& c = p.c;
-
-    // the lane's rows, and their queries
-    int limit[NQ];
-    float unit[NQ];  // of a raw score
-    half8 q[NQ][kSteps], q_low[kTwo ? NQ : 1][kSteps];
-    int lowest = 0x7fffffff, highest = 0;
+// The queries of rows row0 + 16 j + col of the block, 8 channels from d_of(s) on for each step, as fp16 operands (in fp32
+// the sum of q and low); how many keys a row sees (and the least and the most of the wave's rows); and the factor that
+// makes a raw score one in units of log 2, or with CAP in natural ones.
+template <typename T, int NQ, int STEPS, bool CAP, int NL, typename F>
+__device__ __forceinline__ void load_queries(const CacheAttnParams& p, const CacheWork& w, int row0, int col, F d_of,
+                                             half8 (&q)[NQ][STEPS], half8 (&low)[NL][STEPS], int (&limit)[NQ], float (&unit)[NQ],
+                                             int& lowest, int& highest) {
+    lowest = 0x7fffffff;
+    highest = 0;
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
-        const int row = (OWN ? wave * 16 * NQ : 0) + j * 16 + col, i = row / p.group, h = row - i * p.group;
+        const int row = row0 + j * 16 + col, i = row / p.group, h = row - i * p.group;
         const bool mine = i < w.tokens && h < w.heads;
         limit[j] = mine ? w.limit(p, i) : 0;
         highest = max(highest, limit[j]);
         if (mine) lowest = min(lowest, limit[j]);
-        float x[kSteps][8];
+        float x[STEPS][8];
         float top = 0.f;
         const T* from = static_cast<const T*>(p.q) + (int64_t)(w.token0 + (mine ? i : 0)) * p.qs[0] + (int64_t)(w.head0 + (mine ? h : 0)) * p.qs[1];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int d = DP == 32 ? g * 8 : (s / 2) * 64 + g * 16 + (s % 2) * 8;
-            const bool in = mine && d < c.D;
+        for (int s = 0; s < STEPS; ++s) {
+            const int d = d_of(s);
+            const bool in = mine && d < p.c.D;
             constexpr int kPer = 16 / sizeof(T);
             if (p.vec) {
 #pragma unroll
@@ -225,21 +220,98 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
         const float up = __builtin_bit_cast(float, (uint32_t)(shift + 127) << 23);
         unit[j] = fminf(p.scale * (CAP ? 1.f : kLog2e) * __builtin_bit_cast(float, (uint32_t)(127 - shift) << 23), 3.4e38f);
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
+        for (int s = 0; s < STEPS; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float y = x[s][e] * up;
                 q[j][s][e] = (_Float16)y;
-                if constexpr (kTwo) q_low[j][s][e] = (_Float16)(y - (float)q[j][s][e]);
+                if constexpr (std::is_same_v<T, float>) low[j][s][e] = (_Float16)(y - (float)q[j][s][e]);
             }
     }
 #pragma unroll
-    for (int m = 1; m < 16; m *= 2) {
-        lowest = min(lowest, __shfl_xor(lowest, m, 64));
-        highest = max(highest, __shfl_xor(highest, m, 64));
+    for (int k = 1; k < 16; k *= 2) {
+        lowest = min(lowest, __shfl_xor(lowest, k, 64));
+        highest = max(highest, __shfl_xor(highest, k, 64));
     }
     lowest = __builtin_amdgcn_readfirstlane(lowest);
     highest = __builtin_amdgcn_readfirstlane(highest);
+}
+
+// Raw scores of a lane's row with NG groups of four keys, key + 16 t .. key + 16 t + 3, made probabilities (times 2^kShift and the
+// value scale in units of the largest), in fp16 (with TWO the sum of prob and low). whole: the row sees all of them; otherwise
+// those below `limit`, of groups that have a page. The running maximum and sum follow.
+struct GroupScales {
+    float k_scale, bias, less;
+    bool there;
+};
+template <bool CAP, int NG>
+__device__ __forceinline__ float finish_scores(const CacheAttnParams& p, float4v (&s)[NG], float (&by)[NG], float unit,
+                                               const GroupScales (&of)[NG], bool whole, int key, int limit) {
+    float top = -kInf;
+#pragma unroll
+    for (int t = 0; t < NG; ++t) {
+        by[t] = unit * of[t].k_scale;
+        if (CAP || !whole) {
+            const int stop = whole || of[t].there ? limit : 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float z = s[t][r] * by[t];
+                if constexpr (CAP) z = p.softcap * kLog2e * tanh_of<true>(z, 1.f / p.softcap, 2.f * kLog2e / p.softcap);
+                s[t][r] = whole || key + 16 * t + r < stop ? z : -kInf;
+            }
+            by[t] = 1.f;
+        }
+        top = fmaxf(top, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])) * by[t]);
+    }
+    return top;
+}
+// The running maximum after a lane's `top`, and the factor of what was summed before.
+__device__ __forceinline__ float raise(float& m, float top) {
+    const float now = fmaxf(m, column_max(top));
+    const float fade = exp2_of(m - (now == -kInf ? 0.f : now));
+    m = now;
+    return fade;
+}
+template <bool TWO, int NG>
+__device__ __forceinline__ void weigh(const float4v (&s)[NG], const float (&by)[NG], const GroupScales (&of)[NG], float m, float& l,
+                                      half8 (&prob)[NG / 2], half8* low) {
+    const float base = m == -kInf ? 0.f : m;
+#pragma unroll
+    for (int t = 0; t < NG; ++t) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float x = exp2_of(__builtin_fmaf(s[t][r], by[t], of[t].bias - base));
+            sum += x;
+            prob[t / 2][4 * (t % 2) + r] = (_Float16)x;
+            if constexpr (TWO) low[t / 2][4 * (t % 2) + r] = (_Float16)(x - (float)prob[t / 2][4 * (t % 2) + r]);
+        }
+        l += sum * of[t].less;
+    }
+}
+
+// OWN: every wave has rows of its own and walks over all keys; otherwise the waves share the rows and take the 32 keys in
+// turn, and their results are joined in LDS.
+template <typename T, int DP, int NQ, bool OWN, bool CAP>
+__global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAttnParams p) {
+    constexpr bool kTwo = std::is_same_v<T, float>;
+    constexpr int kSteps = DP / 32, kBytes = DP / 16, kWords = (kBytes + 3) / 4;
+    constexpr int kRows = 16 * NQ * (OWN ? kCacheWaves : 1);
+    constexpr int kStride = DP + 4;  // of a row in LDS
+    __shared__ __attribute__((aligned(16))) float joined[OWN ? 1 : kCacheWaves * kRows * kStride];
+    __shared__ float2 stats[OWN ? 1 : kCacheWaves * kRows];
+    const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, g = lane >> 4;
+    CacheWork w;
+    if (!w.find(p, xcd_item(blockIdx.x, gridDim.x), lane)) return;
+    if (w.split >= max(w.runs(p), 1)) return;
+    const Cache& c = p.c;
+
+    int limit[NQ], lowest, highest;
+    float unit[NQ];
+    half8 q[NQ][kSteps], q_low[kTwo ? NQ : 1][kSteps];
+    load_queries<T, NQ, kSteps, CAP>(p, w, OWN ? wave * 16 * NQ : 0, col,
+                                     [&](int s) { return DP == 32 ? g * 8 : (s / 2) * 64 + g * 16 + (s % 2) * 8; }, q, q_low, limit,
+                                     unit, lowest, highest);
 
     float4v o[NQ][kBytes];
     float m[NQ], l[NQ];
@@ -272,18 +344,14 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
         }
         uint4 kx[2][DP == 32 ? 1 : DP / 64];
         uint32_t vx[8][kWords];
-        float k_scale[2], bias[2], less[2];
-        int stop[2];  // 0 where there is no page
+        GroupScales of[2];
         bool whole = key0 + 32 <= lowest;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int at = columns[t] - pages.first, slot = (key0 + 16 * t) & (c.page - 1);
             const int page = __builtin_amdgcn_readlane(pages.page, at);
             whole = whole && page >= 0;
-            stop[t] = page >= 0 ? 0x7fffffff : 0;
-            k_scale[t] = lane_value(pages.k_scale, at);
-            bias[t] = lane_value(pages.bias, at);
-            less[t] = lane_value(pages.less, at);
+            of[t] = {lane_value(pages.k_scale, at), lane_value(pages.bias, at), lane_value(pages.less, at), page >= 0};
             const int64_t base = (((int64_t)max(page, 0) * c.Mkv + w.kv) << c.page_shift) * c.D + (int64_t)slot * c.D;
 #pragma unroll
             for (int u = 0; u < (DP == 32 ? 1 : DP / 64); ++u) {
@@ -324,44 +392,18 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
                 }
             }
         }
-        half8 prob[NQ], prob_low[kTwo ? NQ : 1];
+        half8 prob[NQ][1], prob_low[kTwo ? NQ : 1][1];
 #pragma unroll
         for (int j = 0; j < NQ; ++j) {
-            float top = -kInf;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const float by = unit[j] * k_scale[t];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float z = s[j][t][r] * by;
-                    if constexpr (CAP) z = p.softcap * kLog2e * tanh_of<true>(z, 1.f / p.softcap, 2.f * kLog2e / p.softcap);
-                    if (!whole) z = key0 + 16 * t + 4 * g + r < min(limit[j], stop[t]) ? z : -kInf;
-                    s[j][t][r] = z;
-                    top = fmaxf(top, z);
-                }
-            }
+            float by[2];
+            const float top = finish_scores<CAP>(p, s[j], by, unit[j], of, whole, key0 + 4 * g, limit[j]);
             if (__any(top > m[j])) {
-                const float now = fmaxf(m[j], column_max(top));
-                const float fade = exp2_of(m[j] - (now == -kInf ? 0.f : now));
-                m[j] = now;
+                const float fade = raise(m[j], top);
                 l[j] *= fade;
 #pragma unroll
                 for (int u = 0; u < kBytes; ++u) o[j][u] *= fade;
             }
-            const float base = m[j] == -kInf ? 0.f : m[j];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                float sum = 0.f;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float x = exp2_of(s[j][t][r] - (base - bias[t]));
-                    if (!whole) x = s[j][t][r] == -kInf ? 0.f : x;
-                    sum += x;
-                    prob[j][4 * t + r] = (_Float16)x;
-                    if constexpr (kTwo) prob_low[j][4 * t + r] = (_Float16)(x - (float)prob[j][4 * t + r]);
-                }
-                l[j] += sum * less[t];
-            }
+            weigh<kTwo>(s[j], by, of, m[j], l[j], prob[j], prob_low[kTwo ? j : 0]);
         }
 #pragma unroll
         for (int u = 0; u < kBytes; ++u) {
@@ -374,8 +416,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
             const half8 v = __builtin_bit_cast(half8, make_uint4(f[0], f[1], f[2], f[3]));
 #pragma unroll
             for (int j = 0; j < NQ; ++j) {
-                o[j][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, prob[j], o[j][u], 0, 0, 0);
-                if constexpr (kTwo) o[j][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, prob_low[j], o[j][u], 0, 0, 0);
+                o[j][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, prob[j][0], o[j][u], 0, 0, 0);
+                if constexpr (kTwo) o[j][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, prob_low[j][0], o[j][u], 0, 0, 0);
             }
         }
     }
@@ -451,6 +493,199 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
     }
 }
 
+// ---------------------------------------------------------------- many rows
+
+// Many rows of a sequence: every wave has 32 rows of its own, and the workgroup's waves share the work of turning codes into
+// fp16. Tiles of 8192 codes of keys and of values are loaded one ahead into registers and put into LDS as operands: keys
+// as rows of channels, values as rows of keys (a thread has 4 channels of 8 keys, and a code's place in two_codes
+// turns them around for free), the keys of 32 in the order in which a lane's probabilities have them. Both are read in 16-byte pieces,
+// permuted by the row's number so that the lanes of a read, and of a write, spread over the banks.
+template <int DP>
+struct CacheTile {
+    static constexpr int kKeys = 8192 / DP;
+    static constexpr int kGroups = kKeys / 16;          // of 16 keys, each of one page
+    static constexpr int kKeyPieces = DP / 8;           // of a key's row
+    static constexpr int kValuePieces = kKeys / 8;      // of a channel's row
+    _Float16 k[kKeys * DP], v[kKeys * DP];
+    static __device__ __forceinline__ int key_at(int key, int piece) {
+        return key * DP + ((piece ^ (DP == 128 ? key & 15 : key >> 1 & 7)) << 3);
+    }
+    static __device__ __forceinline__ int value_at(int d, int piece) {
+        return d * kKeys + ((piece ^ (DP == 128 ? (d >> 1 & 7) ^ (d >> 4 & 1) : (d ^ d >> 4) & 15)) << 3);
+    }
+};
+
+template <typename T, int DP, bool CAP>
+__global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_tiles_kernel(CacheAttnParams p) {
+    using Tile = CacheTile<DP>;
+    constexpr int NQ = 2, kSteps = DP / 32, kBlocks = DP / 16, kRows = 16 * NQ * kCacheWaves;
+    constexpr int kKeyLoads = 2, kPerKey = DP / 16;  // 16-byte loads of keys by a thread, and of a key
+    __shared__ __attribute__((aligned(16))) Tile tile;
+    const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, g = lane >> 4;
+    CacheWork w;
+    if (!w.find(p, xcd_item(blockIdx.x, gridDim.x), lane)) return;
+    if (w.split >= max(w.runs(p), 1)) return;
+    const Cache& c = p.c;
+
+    int limit[NQ], lowest, highest;
+    float unit[NQ];
+    half8 q[NQ][kSteps];
+    load_queries<T, NQ, kSteps, CAP>(p, w, wave * 16 * NQ, col, [&](int s) { return s * 32 + g * 8; }, q, q, limit, unit, lowest, highest);
+    const int most = w.limit(p, w.tokens - 1);  // keys that the workgroup's rows see
+
+    float4v o[NQ][kBlocks];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        m[j] = -kInf;
+        l[j] = 0.f;
+#pragma unroll
+        for (int u = 0; u < kBlocks; ++u) o[j][u] = float4v{0.f, 0.f, 0.f, 0.f};
+    }
+    // What lane i knows of the tile's keys 16 i .. 16 i + 15: of the tile that is worked on, and of the next one.
+    struct Group {
+        int page;
+        float k_scale, bias, less;
+    } now, next;
+    Pages pages;
+    uint4 kx[kKeyLoads];
+    uint32_t vx[8];
+    // the thread's keys and channels: see `stage`
+    constexpr int kLanes = DP / 4;  // threads that have 8 keys' values
+    const int v_group = (int)threadIdx.x / kLanes, v_d = (int)threadIdx.x % kLanes * 4, vg = v_group & 3;
+    const int v_pair = __builtin_amdgcn_readfirstlane(v_group >> 2);  // 32 keys
+    const uint32_t v_at = 4 * vg * c.D + (v_d < c.D ? v_d : 0);
+    const int k_part = lane % kPerKey;
+    const uint32_t k_at = lane / kPerKey * c.D + (k_part * 16 < c.D ? k_part * 16 : 0);
+    auto slab = [&](int page, int key) {
+        return (((int64_t)max(page, 0) * c.Mkv + w.kv) << c.page_shift) * c.D + (int64_t)(key & (c.page - 1)) * c.D;
+    };
+    auto fetch = [&](int key0) {
+        const int first = key0 >> c.page_shift, last = (key0 + Tile::kKeys - 16) >> c.page_shift;
+        if (pages.first < 0 || last >= pages.first + 64) {
+            const float turn = pages.load(p, w, first, most, lane);
+#pragma unroll
+            for (int j = 0; j < NQ; ++j)
+#pragma unroll
+                for (int u = 0; u < kBlocks; ++u) o[j][u] *= turn;
+            now.bias += __builtin_amdgcn_logf(turn);
+            now.less *= 1.f / turn;
+        }
+        const int from = min(((key0 + 16 * lane) >> c.page_shift) - pages.first, 63);
+        next.page = __shfl(pages.page, from, 64);
+        next.k_scale = __shfl(pages.k_scale, from, 64);
+        next.bias = __shfl(pages.bias, from, 64);
+        next.less = __shfl(pages.less, from, 64);
+#pragma unroll
+        for (int a = 0; a < kKeyLoads; ++a) {
+            const int key = (a * kCacheWaves + wave) * (64 / kPerKey), group = key >> 4;
+            const int64_t base = slab(__builtin_amdgcn_readlane(next.page, group), key0 + 16 * group) + (key & 15) * c.D;
+            kx[a] = *reinterpret_cast<const uint4*>(c.k + base + k_at);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int group = 2 * v_pair + t;
+            const int64_t base = slab(__builtin_amdgcn_readlane(next.page, group), key0 + 16 * group);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vx[4 * t + i] = *reinterpret_cast<const uint32_t*>(c.v + base + i * c.D + v_at);
+        }
+    };
+    auto stage = [&]() {
+#pragma unroll
+        for (int a = 0; a < kKeyLoads; ++a) {
+            const int key = (a * kCacheWaves + wave) * (64 / kPerKey) + lane / kPerKey;
+            *reinterpret_cast<half8*>(tile.k + Tile::key_at(key, 2 * k_part)) = eight_codes(kx[a].x, kx[a].y);
+            *reinterpret_cast<half8*>(tile.k + Tile::key_at(key, 2 * k_part + 1)) = eight_codes(kx[a].z, kx[a].w);
+        }
+        auto put = [&](int j, uint32_t x, uint32_t y, uint32_t z, uint32_t u) {
+            *reinterpret_cast<uint4*>(tile.v + Tile::value_at(v_d + j, v_group)) = make_uint4(x, y, z, u);
+        };
+        put(0, two_codes<0, 0>(vx[0], vx[1]), two_codes<0, 0>(vx[2], vx[3]), two_codes<0, 0>(vx[4], vx[5]), two_codes<0, 0>(vx[6], vx[7]));
+        put(1, two_codes<1, 1>(vx[0], vx[1]), two_codes<1, 1>(vx[2], vx[3]), two_codes<1, 1>(vx[4], vx[5]), two_codes<1, 1>(vx[6], vx[7]));
+        put(2, two_codes<2, 2>(vx[0], vx[1]), two_codes<2, 2>(vx[2], vx[3]), two_codes<2, 2>(vx[4], vx[5]), two_codes<2, 2>(vx[6], vx[7]));
+        put(3, two_codes<3, 3>(vx[0], vx[1]), two_codes<3, 3>(vx[2], vx[3]), two_codes<3, 3>(vx[4], vx[5]), two_codes<3, 3>(vx[6], vx[7]));
+    };
+
+    const int run0 = w.split * p.run, run1 = (int)min((int64_t)most, (int64_t)run0 + p.run);
+    now = next = {-1, 0.f, 0.f, 0.f};
+    if (run0 < run1) fetch(run0);
+    for (int key0 = run0; key0 < run1; key0 += Tile::kKeys) {
+        __syncthreads();  // everybody has read the tile before
+        stage();
+        now = next;
+        __syncthreads();  // the tile is there
+        if (key0 + Tile::kKeys < run1) fetch(key0 + Tile::kKeys);
+        const bool there = __all(lane >= Tile::kGroups || now.page >= 0);
+#pragma unroll 1
+        for (int sub = 0; sub < Tile::kKeys && key0 + sub < highest; sub += 32) {
+            constexpr int NG = 2;
+            const bool whole = there && key0 + sub + 32 <= lowest;
+            float4v s[NQ][NG];
+            GroupScales of[NG];
+#pragma unroll
+            for (int t = 0; t < NG; ++t) {
+                const int at = sub / 16 + t;
+                of[t] = {lane_value(now.k_scale, at), lane_value(now.bias, at), lane_value(now.less, at),
+                         __builtin_amdgcn_readlane(now.page, at) >= 0};
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) s[j][t] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k) {
+                    const half8 f = *reinterpret_cast<const half8*>(tile.k + Tile::key_at(sub + 16 * t + col, 4 * k + g));
+#pragma unroll
+                    for (int j = 0; j < NQ; ++j) s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[j][k], s[j][t], 0, 0, 0);
+                }
+            }
+            half8 vf[kBlocks];
+#pragma unroll
+            for (int u = 0; u < kBlocks; ++u) vf[u] = *reinterpret_cast<const half8*>(tile.v + Tile::value_at(16 * u + col, sub / 8 + g));
+            half8 prob[NQ][1];
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) {
+                float by[NG];
+                const float top = finish_scores<CAP>(p, s[j], by, unit[j], of, whole, key0 + sub + 4 * g, limit[j]);
+                if (__any(top > m[j])) {
+                    const float fade = raise(m[j], top);
+                    l[j] *= fade;
+#pragma unroll
+                    for (int u = 0; u < kBlocks; ++u) o[j][u] *= fade;
+                }
+                weigh<false>(s[j], by, of, m[j], l[j], prob[j], nullptr);
+            }
+#pragma unroll
+            for (int u = 0; u < kBlocks; ++u) {
+                const half8 v = vf[u];
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) o[j][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, prob[j][0], o[j][u], 0, 0, 0);
+            }
+        }
+    }
+
+    const float by = pages.base * exp2_of(-kShift);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        l[j] = column_sum(l[j]);
+        const int row = wave * 16 * NQ + j * 16 + col, i = row / p.group, h = row - i * p.group;
+        if (i >= w.tokens || h >= w.heads) continue;
+        if (p.splits > 1) {
+            const int64_t at = ((int64_t)w.item * kRows + row) * p.splits + w.split;
+#pragma unroll
+            for (int u = 0; u < kBlocks; ++u)
+                *reinterpret_cast<float4v*>(p.part + at * DP + 16 * u + 4 * g) = o[j][u] * by;
+            if (g == 0) stats_of<DP>(p, kRows)[at] = make_float2(m[j], l[j]);
+            continue;
+        }
+        const float inv = l[j] == 0.f ? 0.f : by / l[j];
+        const int64_t at = (int64_t)(w.token0 + i) * p.M + w.head0 + h;
+#pragma unroll
+        for (int u = 0; u < kBlocks; ++u) {
+            const float y[4] = {o[j][u][0] * inv, o[j][u][1] * inv, o[j][u][2] * inv, o[j][u][3] * inv};
+            store_four(static_cast<T*>(p.out) + at * c.D, 16 * u + 4 * g, c.D, y);
+        }
+        if (p.lse && g == 0) p.lse[at] = lse_of(m[j], l[j]);
+    }
+}
+
 // Joins the runs of a block's rows: DP / 4 lanes to a row, a workgroup for each block.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p, int rows) {
@@ -470,11 +705,16 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p, int 
     }
 }
 
+// Whether many rows go through tiles in LDS: 16-bit queries of more than 32 channels.
+template <typename T, int DP>
+constexpr bool kTiled = sizeof(T) == 2 && DP > 32;
+
 template <typename T, int DP, bool CAP>
 hipError_t launch_rows(const CacheAttnParams& p, const CacheAttnPlan& plan, hipStream_t stream) {
     const dim3 grid((unsigned)plan.workgroups), block(64 * kCacheWaves);
     if (plan.rows == 16) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 1, false, CAP>), grid, block, 0, stream, p);
     else if (plan.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 2, false, CAP>), grid, block, 0, stream, p);
+    else if constexpr (kTiled<T, DP>) hipLaunchKernelGGL((cache_tiles_kernel<T, DP, CAP>), grid, block, 0, stream, p);
     else hipLaunchKernelGGL((cache_attn_kernel<T, DP, 2, true, CAP>), grid, block, 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;

@@ -39,8 +39,7 @@ __device__ __forceinline__ void store_sums(const ProductParams& p, int64_t t, in
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int c = o + e < p.O ? o + e : p.O - 1;
-        y[e] = (float)sum[e] * (a_scale * p.b_scale[c]);
-        if (p.bias) y[e] += p.bias[c];
+        y[e] = __builtin_fmaf((float)sum[e], a_scale * p.b_scale[c], p.bias ? p.bias[c] : 0.f);
     }
     T* to = static_cast<T*>(p.out) + t * p.O + o;
     if (p.wide && o + 4 <= p.O) {
@@ -100,34 +99,60 @@ __global__ __launch_bounds__(64 * kRowWaves) void product_rows_kernel(ProductPar
 
 __device__ const int4_t kZeroPiece[1] = {{0, 0, 0, 0}};
 
-// Tiles of BM tokens and BN channels, WM x WN waves, 128 bytes of every row at a time.
-template <typename T, int BM, int BN, int WM, int WN>
+constexpr int kBand = 8;  // tiles of tokens that are worked on together
+
+// 16 bytes from every lane's address to LDS, lane after lane from `to` on (the same in all lanes). By the instruction's name, and
+// not by its builtin, after which the compiler has every read of LDS wait for all of these loads: the kernel waits for
+// those that it needs with wait_loads.
+__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to;
+    uint32_t keep;  // m0 is the compiler's; what is written to it needs one instruction's time before such a load
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep)
+                 : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(from)
+                 : "memory");
+}
+
+// Waits until at most N of the wave's loads are under way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+}
+
+// Tiles of BM tokens and BN channels, WM x WN waves, 128 bytes of every row at a time, of which NS are in LDS.
+template <typename T, int BM, int BN, int WM, int WN, int NS>
 __global__ __launch_bounds__(64 * WM * WN) void product_tiles_kernel(ProductParams p, int across) {
     constexpr int kWaves = WM * WN, kTM = BM / WM / 32, kTN = BN / WN / 32;  // 32 x 32 blocks of a wave
     constexpr int kRows = BM + BN, kLoads = kRows / 8 / kWaves;              // 8 rows a load of a wave
-    __shared__ __attribute__((aligned(16))) int8_t tile[2][kRows * 128];
+    __shared__ __attribute__((aligned(16))) int8_t tile[NS][kRows * 128];
+    __shared__ float a_scale[BM];
     const int lane = threadIdx.x & 63, wave = wave_index(), wm = wave / WN, wn = wave % WN;
-    const int t0 = (blockIdx.x / across) * BM, o0 = (blockIdx.x % across) * BN;
+    // An XCD takes consecutive tiles (workgroup b runs on XCD b % 8), down a band of kBand and then across, so that those
+    // that it has at work read few rows of either operand.
+    const int item = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), down = (p.T + BM - 1) / BM;
+    const int band = item / (kBand * across), in = item - band * (kBand * across), high = min(kBand, down - band * kBand);
+    if (high <= 0) return;
+    const int t0 = (band * kBand + in % high) * BM, o0 = in / high * BN;
+    if (o0 >= p.O) return;
     const int8_t* from[kLoads];
-    const int piece = (lane & 7) ^ (lane >> 3);  // of the row that the lane's place in LDS holds
+    int piece[kLoads];  // of the row, which the lane's place in LDS holds
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
         const int row = (wave * kLoads + i) * 8 + (lane >> 3);
+        piece[i] = (lane & 7) ^ (row >> 1 & 7);
         from[i] = row < BM ? p.a + (int64_t)min(t0 + row, p.T - 1) * p.K : p.b + (int64_t)min(o0 + row - BM, p.O - 1) * p.K;
-        from[i] += piece * 16;
+        from[i] += piece[i] * 16;
     }
     auto load = [&](int k0, int s) {
         auto put = [&](int i, const void* src) {
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                             (__attribute__((address_space(3))) void*)(tile[s] + (wave * kLoads + i) * 1024), 16,
-                                             0, 0);
+            load_to_lds(src, tile[s] + (wave * kLoads + i) * 1024);
         };
         if (k0 + 128 <= p.K) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) put(i, from[i] + k0);
         } else {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) put(i, k0 + piece * 16 < p.K ? (const void*)(from[i] + k0) : (const void*)kZeroPiece);
+            for (int i = 0; i < kLoads; ++i) put(i, k0 + piece[i] * 16 < p.K ? (const void*)(from[i] + k0) : (const void*)kZeroPiece);
         }
     };
     int16_t_ acc[kTN][kTM];
@@ -137,14 +162,23 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiles_kernel(ProductPara
         for (int m = 0; m < kTM; ++m) acc[n][m] = int16_t_{};
     const int lr = lane & 31, lh = lane >> 5;
     auto fragment = [&](int s, int row, int step) {
-        return *reinterpret_cast<const int4_t*>(tile[s] + row * 128 + (((step * 2 + lh) ^ (row & 7)) << 4));
+        return *reinterpret_cast<const int4_t*>(tile[s] + row * 128 + (((step * 2 + lh) ^ (row >> 1 & 7)) << 4));
     };
-    load(0, 0);
-    int s = 0;
-    for (int k0 = 0; k0 < p.K; k0 += 128, s ^= 1) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the wave's pieces are in LDS
-        __syncthreads();                     // everybody's are, and the other buffer has been read
-        if (k0 + 128 < p.K) load(k0 + 128, s ^ 1);
+    for (int i = threadIdx.x; i < BM; i += 64 * kWaves) a_scale[i] = p.a_scale[min(t0 + i, p.T - 1)];
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i)
+        if (i * 128 < p.K) load(i * 128, i);
+    int s = 0, last = NS - 1;
+    for (int k0 = 0; k0 < p.K; k0 += 128) {
+        // the wave's pieces of this buffer are in LDS, those of the next ones may be on their way
+        if (NS > 3 && k0 + 256 < p.K) wait_loads<(NS > 3 ? 2 : 0) * kLoads>();
+        else if (NS > 2 && k0 + 128 < p.K) wait_loads<(NS > 2 ? 1 : 0) * kLoads>();
+        else wait_loads<0>();
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();        // everybody's are, and the buffer before it has been read
+        asm volatile("" ::: "memory");
+        if (k0 + (NS - 1) * 128 < p.K) load(k0 + (NS - 1) * 128, last);
 #pragma unroll
         for (int step = 0; step < 4; ++step) {
             int4_t x[kTN], y[kTM];
@@ -157,20 +191,56 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiles_kernel(ProductPara
 #pragma unroll
                 for (int m = 0; m < kTM; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[n], y[m], acc[n][m], 0, 0, 0);
         }
+        last = s;
+        s = s + 1 == NS ? 0 : s + 1;
+    }
+    // Sums change lanes through LDS, so that a lane has kPer consecutive channels (the same ones all along: their scales
+    // stay in registers) and a wave stores whole pieces of rows.
+    constexpr int kPer = 16 / sizeof(T), kAcross = 32 * kTN / kPer, kDown = 64 / kAcross, kWide = 32 * kTN + 4;
+    static_assert(kWaves * 32 * kWide * 4 <= sizeof(tile), "the waves' sums fit into the tiles");
+    __syncthreads();  // the tiles have been read
+    int* mine = reinterpret_cast<int*>(&tile[0][0]) + wave * 32 * kWide;
+    const int o = o0 + wn * 32 * kTN + lane % kAcross * kPer;
+    float b_scale[kPer], bias[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int c = min(o + e, p.O - 1);
+        b_scale[e] = p.b_scale[c];
+        bias[e] = p.bias ? p.bias[c] : 0.f;
     }
 #pragma unroll
     for (int m = 0; m < kTM; ++m) {
-        const int t = t0 + (wm * kTM + m) * 32 + lr;
-        if (t >= p.T) continue;
-        const float a_scale = p.a_scale[t];
 #pragma unroll
         for (int n = 0; n < kTN; ++n)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int o = o0 + (wn * kTN + n) * 32 + 8 * q + 4 * lh;
-                const int four[4] = {acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
-                if (o < p.O) store_sums<T>(p, t, o, four, a_scale);
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<int4_t*>(mine + lr * kWide + n * 32 + 8 * q + 4 * lh) =
+                    int4_t{acc[n][m][4 * q], acc[n][m][4 * q + 1], acc[n][m][4 * q + 2], acc[n][m][4 * q + 3]};
+        wave_lds_sync();
+#pragma unroll
+        for (int i = 0; i < 32 / kDown; ++i) {
+            const int row = i * kDown + lane / kAcross, t = t0 + (wm * kTM + m) * 32 + row;
+            const int* from = mine + row * kWide + lane % kAcross * kPer;
+            const float by = a_scale[(wm * kTM + m) * 32 + row];
+            Piece<T, kPer> y;
+#pragma unroll
+            for (int e = 0; e < kPer; e += 4) {
+                const int4_t x = *reinterpret_cast<const int4_t*>(from + e);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y.v[e + k] = (T)__builtin_fmaf((float)x[k], by * b_scale[e + k], bias[e + k]);
             }
+            T* to = static_cast<T*>(p.out) + (int64_t)t * p.O + o;
+            if (t < p.T && o < p.O) {
+                if (p.wide) {
+                    stream_store(reinterpret_cast<uint4*>(to), __builtin_bit_cast(uint4, y));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e)
+                        if (o + e < p.O) to[e] = y.v[e];
+                }
+            }
+        }
+        wave_lds_sync();
     }
 }
 
@@ -182,10 +252,10 @@ void launch_rows(const ProductParams& p, int64_t workgroups, hipStream_t stream)
     else hipLaunchKernelGGL((product_rows_kernel<T, NT, false>), grid, block, 0, stream, p, across);
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, int NS>
 void launch_tiles(const ProductParams& p, int64_t workgroups, hipStream_t stream) {
-    hipLaunchKernelGGL((product_tiles_kernel<T, BM, BN, WM, WN>), dim3((unsigned)workgroups), dim3(64 * WM * WN), 0, stream, p,
-                       (p.O + BN - 1) / BN);
+    hipLaunchKernelGGL((product_tiles_kernel<T, BM, BN, WM, WN, NS>), dim3((unsigned)((workgroups + 7) / 8 * 8)), dim3(64 * WM * WN),
+                       0, stream, p, (p.O + BN - 1) / BN);
 }
 
 template <typename T>
@@ -196,11 +266,11 @@ hipError_t launch_typed(const ProductParams& p, hipStream_t stream) {
         else if (plan.tokens == 32) launch_rows<T, 2>(p, plan.workgroups, stream);
         else launch_rows<T, 4>(p, plan.workgroups, stream);
     } else if (plan.tokens == 256) {
-        launch_tiles<T, 256, 256, 2, 4>(p, plan.workgroups, stream);
+        launch_tiles<T, 256, 256, 2, 4, 2>(p, plan.workgroups, stream);
     } else if (plan.tokens == 128) {
-        launch_tiles<T, 128, 128, 2, 2>(p, plan.workgroups, stream);
+        launch_tiles<T, 128, 128, 2, 2, 2>(p, plan.workgroups, stream);
     } else {
-        launch_tiles<T, 64, 64, 2, 2>(p, plan.workgroups, stream);
+        launch_tiles<T, 64, 64, 2, 2, 3>(p, plan.workgroups, stream);
     }
     return hipGetLastError();
 }

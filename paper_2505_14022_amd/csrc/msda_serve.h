@@ -36,7 +36,7 @@ struct ProductParams {
     void* out;                  // [T, O] dtype
     int T, K, O;
     bool pieces;                // rows of a and b are whole 16-byte pieces on 16-byte boundaries
-    bool wide;                  // four results of a row can be stored at once
+    bool wide;                  // rows of out are whole 16-byte pieces on 16-byte boundaries
 };
 // How a product is cut up: rows of a and of b to a workgroup.
 struct ProductPlan {

@@ -165,7 +165,7 @@ msda_status_t msda_quantized_matmul(const int8_t* a, const int8_t* b, const floa
     p.K = (int)K;
     p.O = (int)O;
     p.pieces = K % 16 == 0 && is_aligned(a, 16) && is_aligned(b, 16);
-    p.wide = O % 4 == 0 && is_aligned(out, 4 * dtype_size(dtype));
+    p.wide = (O * dtype_size(dtype)) % 16 == 0 && is_aligned(out, 16);
     const msda::ProductPlan plan = msda::product_plan(p);
     if (plan.workgroups > kMaxWorkItems / (64 * plan.waves))
         return fail(MSDA_ERROR_NOT_SUPPORTED, "T=%lld rows of O=%lld channels are too many for one launch", (long long)T,
@@ -237,7 +237,7 @@ msda::Cache cache_of(const msda_cache_t& c, int64_t T) {
     while ((1 << x.page_shift) < x.page) ++x.page_shift;
     x.Mkv = (int)c.Mkv;
     x.D = (int)c.D;
-    x.width = (int)c.width;
+    x.width = c.pages > 0 ? (int)c.width : 0;  // without a page no token exists
     return x;
 }
 
