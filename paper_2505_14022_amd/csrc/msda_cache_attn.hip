@@ -746,7 +746,7 @@ CacheAttnPlan cache_attn_plan(const CacheAttnParams& p, int dtype) {
     a.blocks = place_count(c, a.tokens, 1);
     const int64_t items = a.blocks * c.Mkv * a.groups, longest = (int64_t)c.width * c.page;
     const int64_t least = a.rows == 128 ? 512 : 256;  // tokens of a run
-    int64_t splits = items > 0 ? 2048 / items : 1;
+    int64_t splits = items > 0 ? 1024 / items : 1;
     if (a.rows == 128 && items >= 512) splits = 1;
     if (splits > longest / least) splits = longest / least;
     // the partial results have to fit into half a GB

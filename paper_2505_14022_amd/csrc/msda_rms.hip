@@ -5,15 +5,14 @@
 // Bound by memory, as layer norm is, and built like it: a row stays in the registers of the lanes that own it. A row's
 // rstd divides its values and their largest alike, so the codes do not depend on it: they need the largest |t| and the
 // sum of squares, which are found in one reduction, and the codes come from fp32 operations that do not depend on the
-// order of any sum. The largest is taken over the bits of |t| as integers, among which infinities and NaN come last:
-// they are told without a test of their own.
+// order of any sum. A NaN stays the largest, and is told with
+// the infinities by the largest's bits.
+#include "msda_codes.hpp"
 #include "msda_rows.hpp"
 #include "msda_serve.h"
 
 namespace msda {
 namespace {
-
-constexpr uint32_t kNotFinite = 0x7f800000u, kLeast = 0x0d800000u;  // bits of infinity, and of 2^-100
 
 // The largest of G lanes' values and the sum of others, as row_sums.
 template <int NT, int G>
@@ -41,15 +40,6 @@ __device__ __forceinline__ void row_sum_and_max(float& sum, uint32_t& most, floa
             most = red_most[w] > most ? red_most[w] : most;
         }
     }
-}
-
-// Stores VEC codes of values in steps of 1 / inverse.
-template <int VEC>
-__device__ __forceinline__ void store_codes(int8_t* to, const float (&t)[VEC], float inverse) {
-    Piece<int8_t, VEC> x;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x.v[i] = (int8_t)(int)fminf(fmaxf(rintf(t[i] * inverse), -127.f), 127.f);
-    *reinterpret_cast<Piece<int8_t, VEC>*>(to) = x;
 }
 
 template <typename T, int VEC, int NT, int G, int NV, RmsResult RESULT>
@@ -82,8 +72,7 @@ __global__ __launch_bounds__(NT) void rms_fwd_kernel(RmsParams p) {
     for (; row < p.rows; row += step) {
         const int64_t at = row * C;
         float s[NV][VEC];
-        float sum = 0.f;
-        uint32_t most = 0;
+        float sum = 0.f, top = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * G + g) * VEC;
@@ -93,15 +82,16 @@ __global__ __launch_bounds__(NT) void rms_fwd_kernel(RmsParams p) {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     if constexpr (RESULT != kCodes) sum += s[j][i] * s[j][i];
-                    if constexpr (RESULT != kNormed) {
-                        const float t = RESULT == kCodes ? s[j][i] : s[j][i] * w[j][i];
-                        const uint32_t bits = __builtin_bit_cast(uint32_t, t) & 0x7fffffffu;
-                        most = bits > most ? bits : most;
-                    }
+                }
+                if constexpr (RESULT != kNormed) {
+                    auto t = [&](int i) { return RESULT == kCodes ? s[j][i] : s[j][i] * w[j][i]; };
+#pragma unroll
+                    for (int i = 0; i < VEC; i += 2) top = larger(top, t(i), i + 1 < VEC ? t(i + 1) : 0.f);
                 }
             }
         }
         fetch(row + step);
+        uint32_t most = magnitude_bits(top);
         if constexpr (RESULT == kNormed) {
             float one[1] = {sum};
             row_sums<NT, G>(one, red);
@@ -115,9 +105,8 @@ __global__ __launch_bounds__(NT) void rms_fwd_kernel(RmsParams p) {
         }
         float inverse = 0.f;
         if constexpr (RESULT != kNormed) {
-            float u = most < kLeast ? 0.f : __builtin_bit_cast(float, most) * (1.f / 127.f);
-            if (most >= kNotFinite) u = __builtin_nanf("");
-            else if (u > 0.f) inverse = 1.f / u;
+            const float u = scale_of(most);
+            if (u > 0.f) inverse = 1.f / u;
             if (g == 0) p.scale[row] = u * rstd;
         }
 #pragma unroll
@@ -135,7 +124,7 @@ __global__ __launch_bounds__(NT) void rms_fwd_kernel(RmsParams p) {
                         if constexpr (RESULT == kNormedCodes) s[j][i] *= w[j][i];
                         if (most >= kNotFinite) s[j][i] = 0.f;
                     }
-                    store_codes(p.codes + at + c, s[j], inverse);
+                    *reinterpret_cast<Piece<int8_t, VEC>*>(p.codes + at + c) = codes_of<VEC>(s[j], inverse);
                 }
             }
         }
