@@ -26,6 +26,7 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 
 constexpr int kCacheWaves = 4;
 constexpr float kShift = 14.f;  // probabilities times 2^14 as an operand
+constexpr float kFar = 74.f;    // value scales that differ by 2^74 and more count as if by that
 
 // Bytes A and B (0 .. 3) of the words x and y of codes, as two fp16 numbers.
 template <int A, int B>
@@ -123,17 +124,15 @@ struct Pages {
         }
         // the scores of a page that makes NaN are NaN, which a row that does not see it replaces
         const bool odd = !(k_scale >= 0.f && k_scale < kInf && v_scale >= 0.f && v_scale < kInf);
-        if (odd) {
-            k_scale = __builtin_nanf("");
-            v_scale = 0.f;
-        }
+        if (odd) k_scale = __builtin_nanf("");
+        if (odd || v_scale < 1.17549435e-38f) v_scale = 0.f;  // logarithms are those of normal numbers
         float top = group_max<64>(v_scale);
         top = fmaxf(top, base);
         const float unit = top > 0.f ? top : 1.f;
         const float turn = base > 0.f ? base / unit : 1.f;
         base = top;
-        // a scale below 2^-74 of the largest, or of 0, counts as that much: its values are lost beside others in fp32
-        bias = fmaxf((v_scale > 0.f ? __builtin_amdgcn_logf(v_scale) : -kInf) - __builtin_amdgcn_logf(unit), -74.f) + kShift;
+        // a scale below 2^-kFar of the largest, or of 0, counts as that much: its values are lost beside others in fp32
+        bias = fmaxf((v_scale > 0.f ? __builtin_amdgcn_logf(v_scale) : -kInf) - __builtin_amdgcn_logf(unit), -kFar) + kShift;
         less = exp2_of(-bias);
         return turn;
     }
@@ -568,8 +567,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_tiles_kernel(CacheA
             for (int j = 0; j < NQ; ++j)
 #pragma unroll
                 for (int u = 0; u < kBlocks; ++u) o[j][u] *= turn;
-            now.bias += __builtin_amdgcn_logf(turn);
-            now.less *= 1.f / turn;
+            now.bias = fmaxf(now.bias + __builtin_amdgcn_logf(turn), kShift - kFar);
+            now.less = exp2_of(-now.bias);
         }
         const int from = min(((key0 + 16 * lane) >> c.page_shift) - pages.first, 63);
         next.page = __shfl(pages.page, from, 64);

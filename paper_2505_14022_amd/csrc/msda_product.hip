@@ -131,9 +131,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiles_kernel(ProductPara
     // that it has at work read few rows of either operand.
     const int item = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), down = (p.T + BM - 1) / BM;
     const int band = item / (kBand * across), in = item - band * (kBand * across), high = min(kBand, down - band * kBand);
-    if (high <= 0) return;
+    if (high <= 0 || in >= high * across) return;  // past the last band's tiles: the grid is a multiple of 8
     const int t0 = (band * kBand + in % high) * BM, o0 = in / high * BN;
-    if (o0 >= p.O) return;
     const int8_t* from[kLoads];
     int piece[kLoads];  // of the row, which the lane's place in LDS holds
 #pragma unroll

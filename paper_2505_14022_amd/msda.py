@@ -780,7 +780,7 @@ def rmsnorm_forward(x, weight=None, residual=None, eps=1e-6, want_sum: bool = Fa
     context, s = _launching(x, stream)
     with context:
         out = torch.empty_like(x) if out is None else out
-        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if rstd is None else rstd
+        rstd = x.new_empty(x.shape[:-1], dtype=torch.float32) if rstd is None else rstd
         sum = torch.empty_like(x) if sum is None and want_sum else sum
         r = lib().msda_rmsnorm_forward(_address(x), _address(residual), _address(weight), _address(out), _address(sum),
                                        _address(rstd), rows, C, float(eps), code, s)
@@ -804,8 +804,8 @@ def rmsnorm_quantize(x, weight=None, residual=None, eps=1e-6, want_sum: bool = F
     _expect("scale", scale, x.shape[:-1], torch.float32, x)
     context, s = _launching(x, stream)
     with context:
-        codes = torch.empty(x.shape, dtype=torch.int8, device=x.device) if codes is None else codes
-        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scale is None else scale
+        codes = torch.empty_like(x, dtype=torch.int8) if codes is None else codes
+        scale = x.new_empty(x.shape[:-1], dtype=torch.float32) if scale is None else scale
         sum = torch.empty_like(x) if sum is None and want_sum else sum
         r = lib().msda_rmsnorm_quantize(_address(x), _address(residual), _address(weight), _address(codes), _address(scale),
                                         _address(sum), rows, C, float(eps), code, s)
@@ -831,7 +831,7 @@ def rmsnorm_backward(x, grad_out, rstd, weight=None, residual=None, grad_sum=Non
     with context:
         grad_x = torch.empty_like(x) if grad_x is None else grad_x
         if want_weight_grad and grad_weight is None:
-            grad_weight = torch.empty(C, dtype=torch.float32, device=x.device)
+            grad_weight = x.new_empty(C, dtype=torch.float32)
         ws = _workspace(workspace, 0 if grad_weight is None else rmsnorm_workspace_size(rows, C, code), x)
         r = lib().msda_rmsnorm_backward(_address(x), _address(residual), _address(weight), _address(grad_out),
                                         _address(grad_sum), _address(rstd), _address(grad_x), _address(grad_weight),
@@ -852,8 +852,8 @@ def quantize_rows(x, codes=None, scale=None, stream=None):
     _expect("scale", scale, x.shape[:-1], torch.float32, x)
     context, s = _launching(x, stream)
     with context:
-        codes = torch.empty(x.shape, dtype=torch.int8, device=x.device) if codes is None else codes
-        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) if scale is None else scale
+        codes = torch.empty_like(x, dtype=torch.int8) if codes is None else codes
+        scale = x.new_empty(x.shape[:-1], dtype=torch.float32) if scale is None else scale
         r = lib().msda_quantize_rows(_address(x), _address(codes), _address(scale), rows, C, code, s)
     _raise(r, "msda_quantize_rows")
     return codes, scale
@@ -878,15 +878,18 @@ def quantized_matmul(a, b, a_scale, b_scale, bias=None, dtype=None, out=None, st
     _expect("out", out, shape, dtype, a)
     context, s = _launching(a, stream)
     with context:
-        out = torch.empty(shape, dtype=dtype, device=a.device) if out is None else out
+        out = a.new_empty(shape, dtype=dtype) if out is None else out
         r = lib().msda_quantized_matmul(_address(a), _address(b), _address(a_scale), _address(b_scale), _address(bias),
                                         _address(out), rows, K, O, _layer_dtype(out), s)
     _raise(r, "msda_quantized_matmul")
     return out
 
 
+_TwoStrides = ctypes.c_int64 * 2
+
+
 def _two_strides(t):
-    return (ctypes.c_int64 * 2)(*t.stride()[:2])
+    return _TwoStrides(*t.stride()[:2])
 
 
 def _cache(T, k_cache, v_cache, k_scale, v_scale, table, length, start):
@@ -976,9 +979,9 @@ def cache_attention(q, k_cache, v_cache, k_scale, v_scale, table, length, start=
     _expect("lse", lse, (T, M), torch.float32, k_cache)
     context, s = _launching(k_cache, stream)
     with context:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        out = q.new_empty(q.shape) if out is None else out
         if lse is None and want_lse:
-            lse = torch.empty((T, M), dtype=torch.float32, device=q.device)
+            lse = q.new_empty((T, M), dtype=torch.float32)
         ws = _workspace(workspace, _cache_attention_workspace(c, T, M, code), k_cache)
         r = lib().msda_cache_attention(ctypes.byref(c), _address(q), _two_strides(q), _address(out), _address(lse), T, M,
                                        D ** -0.5 if scale is None else float(scale), float(softcap), int(bool(causal)), code,

@@ -177,6 +177,7 @@ def attention(q, k_cache, v_cache, k_scale, v_scale, table, length, start=None, 
     table, lengths = table.cpu(), [int(x) for x in length]
     starts = None if start is None else [int(x) for x in start]
     kc, vc, ks, vs, qs = k_cache.cpu(), v_cache.cpu(), k_scale.cpu(), v_scale.cpu(), up(q)
+    vs = torch.where(vs < 2.0 ** -126, torch.zeros_like(vs), vs)  # counted as 0, by definition
     for n, (at, count, first) in enumerate(places(T, lengths, starts, table.shape[1], P)):
         end = min(max(lengths[n], 0), table.shape[1] * P)
         place = torch.arange(end)

@@ -384,6 +384,29 @@ def test_attention_with_scales_of_all_sizes():
     assert float(out.abs().max()) == 0
 
 
+@pytest.mark.parametrize("new", [1, 90])
+@pytest.mark.parametrize("least", [2.0 ** -140, 2.0 ** -100])
+def test_value_scales_at_the_ends_of_fp32(new, least):
+    """Small scales first and large ones past the 64 pages that are looked up at once, small ones throughout, and zeros."""
+    import torch
+
+    say(f"attention over value scales of {least} and of 2^100, {new} tokens each")
+    c = Case([1500, 1100], [new, new], G=2, D=64, P=16, dtype="bf16", seed=36)
+    row = c.table.long()
+    c.v_scale[row[0, :66]] = least
+    c.v_scale[row[0, 66:]] = 2.0 ** 100
+    c.v_scale[row[1]] = 0
+    out, lse = c.check_attention()
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    assert float(out[new:].abs().max()) == 0
+    c.v_scale[row[0]] = 2.0 ** 100
+    c.v_scale[row[0, 66:]] = least
+    c.check_attention()
+    c.v_scale[row[0]] = least
+    out, lse = c.check_attention()
+    assert bool(torch.isfinite(lse).all())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_queries_of_all_sizes(dtype):
     import torch
