@@ -68,15 +68,14 @@ __global__ __launch_bounds__(64 * kUnits, 4) void append_kernel(AppendParams p, 
     extern __shared__ float turns[];
     const Cache& c = p.c;
     const int lane = threadIdx.x & 63, wave = wave_index();
-    const Place at = c.start ? find_place(c, blockIdx.x, c.page, 2, lane) : Place{(int)blockIdx.x, 0};
-    if (at.n < 0) return;
-    const Tokens t(c, at.n);
+    const Place t = find_place(c, blockIdx.x, c.page, 2, lane);
+    if (t.n < 0) return;
     // the page's column in the table, and its new tokens: slots s0 .. s1 - 1
-    const int column = (max(t.first, 0) >> c.page_shift) + at.block;
+    const int column = (max(t.first, 0) >> c.page_shift) + t.block;
     const int64_t base = (int64_t)column << c.page_shift;
     const int s0 = (int)max((int64_t)t.first - base, (int64_t)0), s1 = (int)min((int64_t)t.length - base, (int64_t)c.page);
     if (s0 >= s1) return;
-    const int page = page_at(c, at.n, column);
+    const int page = page_at(c, t.n, column);
     if (page < 0) return;
     const int nt = s1 - s0;
     const int64_t token0 = t.start + (base + s0 - t.first);  // the call's token in slot s0

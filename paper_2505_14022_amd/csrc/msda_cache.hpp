@@ -12,37 +12,51 @@
 namespace msda {
 namespace {
 
-__device__ __forceinline__ int start_of(const Cache& c, int n) { return c.start ? min(max(c.start[n], 0), c.T) : n; }
-
-// A workgroup's sequence (-1: none), and which of the sequence's workgroups it is.
+// A workgroup's sequence, which of the sequence's workgroups it is, and the sequence's tokens: in all, the call's first one, how
+// many there are of the call's, and the first one's place. What the last look takes of every candidate is the sequence's
+// all: nothing more is read for it.
 struct Place {
-    int n, block;
+    int n, block;  // n < 0: none
+    int length, start, count, first;
 };
 __device__ __forceinline__ Place find_place(const Cache& c, int b, int size, int extra, int lane) {
-    auto first = [&](int n) { return start_of(c, n) / size + extra * n; };
+    auto at = [&](int n) { return min(max(c.start[n], 0), c.T); };
+    Place x = {-1, 0, 0, 0, 0, 0};
+    if (!c.start) {  // a token and a workgroup each
+        x.n = b;
+        x.length = max(c.length[b], 0);
+        x.start = b;
+        x.count = 1;
+        x.first = x.length - 1;
+        return x;
+    }
     int lo = 0, hi = c.N;  // the sequence is one of lo .. hi - 1, if any
     while (true) {
         const int step = (hi - lo + 63) / 64, n = lo + lane * step;
-        const uint64_t below = __ballot(n < hi && first(n) <= b);
-        if (below == 0) return {-1, 0};
-        lo += (63 - __builtin_clzll(below)) * step;
-        if (step == 1) break;
+        int start = 0, next = 0, length = 0;
+        if (n < hi) {
+            start = at(n);
+            if (step == 1) {
+                next = at(n + 1);
+                length = max(c.length[n], 0);
+            }
+        }
+        const uint64_t below = __ballot(n < hi && start / size + extra * n <= b);
+        if (below == 0) return x;
+        const int winner = 63 - __builtin_clzll(below);
+        lo += winner * step;
+        if (step == 1) {
+            x.n = __builtin_amdgcn_readfirstlane(lo);
+            x.start = __builtin_amdgcn_readlane(start, winner);
+            x.length = __builtin_amdgcn_readlane(length, winner);
+            x.count = max(__builtin_amdgcn_readlane(next, winner) - x.start, 0);
+            x.first = x.length - x.count;
+            x.block = b - (x.start / size + extra * x.n);
+            return x;
+        }
         hi = min(hi, lo + step);
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    return {lo, b - first(lo)};
 }
-
-// The tokens of a sequence: in all, the call's first one, how many there are of the call's, and the first one's place.
-struct Tokens {
-    int length, start, count, first;
-    __device__ __forceinline__ Tokens(const Cache& c, int n) {
-        length = max(c.length[n], 0);
-        start = start_of(c, n);
-        count = c.start ? max(start_of(c, n + 1) - start, 0) : 1;
-        first = length - count;
-    }
-};
 
 // The page of a sequence's tokens page * column .., or -1.
 __device__ __forceinline__ int page_at(const Cache& c, int n, int column) {

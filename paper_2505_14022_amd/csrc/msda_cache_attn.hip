@@ -81,11 +81,10 @@ struct CacheWork {
         head0 = (part - kv * p.groups) * p.group;
         heads = min(p.group, p.G - head0);
         head0 += kv * p.G;
-        const Place at = p.c.start ? find_place(p.c, block, p.tokens, 1, lane) : Place{block, 0};
-        if (at.n < 0) return false;
-        n = at.n;
-        const Tokens t(p.c, n);
-        const int skip = at.block * p.tokens;
+        const Place t = find_place(p.c, block, p.tokens, 1, lane);
+        if (t.n < 0) return false;
+        n = t.n;
+        const int skip = t.block * p.tokens;
         tokens = min(p.tokens, t.count - skip);
         if (tokens <= 0) return false;
         token0 = t.start + skip;
@@ -106,7 +105,7 @@ struct CacheWork {
 
 // The pages of 64 columns of the sequence's table, one to a lane.
 struct Pages {
-    int first = -1;             // column of lane 0
+    int first;                  // column of lane 0
     int page;                   // -1: no tokens
     float k_scale, bias, less;  // bias: log2 of the value scale relative to `base`, and kShift; less: 2^-bias
     float base = 0.f;           // the largest value scale so far; sums are in units of it
@@ -176,13 +175,15 @@ struct Joined {
 
 // The queries of rows row0 + 16 j + col of the block, 8 channels from d_of(s) on for each step, as fp16 operands (in fp32
 // the sum of q and low); how many keys a row sees (and the least and the most of the wave's rows); and the factor that
-// makes a raw score one in units of log 2, or with CAP in natural ones.
-template <typename T, int NQ, int STEPS, bool CAP, int NL, typename F>
+// makes a raw score one in units of log 2, or with CAP in natural ones. meanwhile() is called while the queries are on their
+// way.
+template <typename T, int NQ, int STEPS, int CAP, int NL, typename F, typename W>
 __device__ __forceinline__ void load_queries(const CacheAttnParams& p, const CacheWork& w, int row0, int col, F d_of,
                                              half8 (&q)[NQ][STEPS], half8 (&low)[NL][STEPS], int (&limit)[NQ], float (&unit)[NQ],
-                                             int& lowest, int& highest) {
+                                             int& lowest, int& highest, W meanwhile) {
     lowest = 0x7fffffff;
     highest = 0;
+    Piece<T, 8> x[NQ][STEPS];
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
         const int row = row0 + j * 16 + col, i = row / p.group, h = row - i * p.group;
@@ -190,39 +191,45 @@ __device__ __forceinline__ void load_queries(const CacheAttnParams& p, const Cac
         limit[j] = mine ? w.limit(p, i) : 0;
         highest = max(highest, limit[j]);
         if (mine) lowest = min(lowest, limit[j]);
-        float x[STEPS][8];
-        float top = 0.f;
         const T* from = static_cast<const T*>(p.q) + (int64_t)(w.token0 + (mine ? i : 0)) * p.qs[0] + (int64_t)(w.head0 + (mine ? h : 0)) * p.qs[1];
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             const int d = d_of(s);
             const bool in = mine && d < p.c.D;
             constexpr int kPer = 16 / sizeof(T);
+            x[j][s] = {};
             if (p.vec) {
 #pragma unroll
                 for (int e = 0; e < 8; e += kPer) {
                     Piece<T, kPer> y = {};
                     if (in) y = *reinterpret_cast<const Piece<T, kPer>*>(from + d + e);
 #pragma unroll
-                    for (int k = 0; k < kPer; ++k) x[s][e + k] = (float)y.v[k];
+                    for (int k = 0; k < kPer; ++k) x[j][s].v[e + k] = y.v[k];
                 }
-            } else {
+            } else if (in) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[s][e] = in ? (float)from[d + e] : 0.f;
+                for (int e = 0; e < 8; ++e) x[j][s].v[e] = from[d + e];
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[s][e]));
         }
+    }
+    meanwhile();
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        float top = 0.f;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)x[j][s].v[e]));
         top = column_max(top);
         int shift = top > 0.f && top < kInf ? 14 - ((int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127) : 0;
         shift = min(shift, 126);
         const float up = __builtin_bit_cast(float, (uint32_t)(shift + 127) << 23);
-        unit[j] = fminf(p.scale * (CAP ? 1.f : kLog2e) * __builtin_bit_cast(float, (uint32_t)(127 - shift) << 23), 3.4e38f);
+        unit[j] = fminf(p.scale * (CAP > 0 ? 1.f : kLog2e) * __builtin_bit_cast(float, (uint32_t)(127 - shift) << 23), 3.4e38f);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float y = x[s][e] * up;
+                const float y = (float)x[j][s].v[e] * up;
                 q[j][s][e] = (_Float16)y;
                 if constexpr (std::is_same_v<T, float>) low[j][s][e] = (_Float16)(y - (float)q[j][s][e]);
             }
@@ -243,21 +250,24 @@ struct GroupScales {
     float k_scale, bias, less;
     bool there;
 };
-template <bool CAP, int NG>
+// CAP: capped by tanh, in its short form for 16-bit results and caps up to kShortCap (a score is 2^-14 off then), else its series.
+template <int CAP, int NG>
 __device__ __forceinline__ float finish_scores(const CacheAttnParams& p, float4v (&s)[NG], float (&by)[NG], float unit,
                                                const GroupScales (&of)[NG], bool whole, int key, int limit) {
     float top = -kInf;
 #pragma unroll
     for (int t = 0; t < NG; ++t) {
         by[t] = unit * of[t].k_scale;
-        if (CAP || !whole) {
-            const int stop = whole || of[t].there ? limit : 0;
+        if constexpr (CAP > 0) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float z = s[t][r] * by[t];
-                if constexpr (CAP) z = p.softcap * kLog2e * tanh_of<true>(z, 1.f / p.softcap, 2.f * kLog2e / p.softcap);
-                s[t][r] = whole || key + 16 * t + r < stop ? z : -kInf;
-            }
+            for (int r = 0; r < 4; ++r)
+                s[t][r] = p.cap_unit * tanh_of<(CAP == 2)>(s[t][r] * by[t], p.cap_inverse, p.cap_exponent);
+            by[t] = 1.f;
+        }
+        if (!whole) {
+            const int stop = of[t].there ? limit : 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[t][r] = key + 16 * t + r < stop ? s[t][r] * by[t] : -kInf;
             by[t] = 1.f;
         }
         top = fmaxf(top, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])) * by[t]);
@@ -291,7 +301,7 @@ __device__ __forceinline__ void weigh(const float4v (&s)[NG], const float (&by)[
 
 // OWN: every wave has rows of its own and walks over all keys; otherwise the waves share the rows and take the 32 keys in
 // turn, and their results are joined in LDS.
-template <typename T, int DP, int NQ, bool OWN, bool CAP>
+template <typename T, int DP, int NQ, bool OWN, int CAP>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAttnParams p) {
     constexpr bool kTwo = std::is_same_v<T, float>;
     constexpr int kSteps = DP / 32, kBytes = DP / 16, kWords = (kBytes + 3) / 4;
@@ -308,9 +318,11 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
     int limit[NQ], lowest, highest;
     float unit[NQ];
     half8 q[NQ][kSteps], q_low[kTwo ? NQ : 1][kSteps];
+    const int run0 = w.split * p.run, first_key = run0 + (OWN ? 0 : 32 * wave), most = w.limit(p, w.tokens - 1);
+    Pages pages;
     load_queries<T, NQ, kSteps, CAP>(p, w, OWN ? wave * 16 * NQ : 0, col,
                                      [&](int s) { return DP == 32 ? g * 8 : (s / 2) * 64 + g * 16 + (s % 2) * 8; }, q, q_low, limit,
-                                     unit, lowest, highest);
+                                     unit, lowest, highest, [&]() { pages.load(p, w, first_key >> c.page_shift, most, lane); });
 
     float4v o[NQ][kBytes];
     float m[NQ], l[NQ];
@@ -321,7 +333,6 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
 #pragma unroll
         for (int u = 0; u < kBytes; ++u) o[j][u] = float4v{0.f, 0.f, 0.f, 0.f};
     }
-    Pages pages;
     // byte offsets of the lane within 16 keys; channels from D on are read as others: they meet zeros, or rows of no result
     uint32_t k_at[DP == 32 ? 1 : DP / 64];
 #pragma unroll
@@ -331,11 +342,11 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
     }
     const uint32_t v_at = 4 * g * c.D + (col * kBytes < c.D ? col * kBytes : 0);
 
-    const int run0 = w.split * p.run, run1 = (int)min((int64_t)highest, (int64_t)run0 + p.run);
-    for (int key0 = run0 + (OWN ? 0 : 32 * wave); key0 < run1; key0 += OWN ? 32 : 32 * kCacheWaves) {
+    const int run1 = (int)min((int64_t)highest, (int64_t)run0 + p.run);
+    for (int key0 = first_key; key0 < run1; key0 += OWN ? 32 : 32 * kCacheWaves) {
         const int columns[2] = {key0 >> c.page_shift, (key0 + 16) >> c.page_shift};
-        if (pages.first < 0 || columns[1] >= pages.first + 64) {
-            const float turn = pages.load(p, w, columns[0], highest, lane);
+        if (columns[1] >= pages.first + 64) {
+            const float turn = pages.load(p, w, columns[0], most, lane);
 #pragma unroll
             for (int j = 0; j < NQ; ++j)
 #pragma unroll
@@ -514,7 +525,7 @@ struct CacheTile {
     }
 };
 
-template <typename T, int DP, bool CAP>
+template <typename T, int DP, int CAP>
 __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_tiles_kernel(CacheAttnParams p) {
     using Tile = CacheTile<DP>;
     constexpr int NQ = 2, kSteps = DP / 32, kBlocks = DP / 16, kRows = 16 * NQ * kCacheWaves;
@@ -529,8 +540,10 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_tiles_kernel(CacheA
     int limit[NQ], lowest, highest;
     float unit[NQ];
     half8 q[NQ][kSteps];
-    load_queries<T, NQ, kSteps, CAP>(p, w, wave * 16 * NQ, col, [&](int s) { return s * 32 + g * 8; }, q, q, limit, unit, lowest, highest);
-    const int most = w.limit(p, w.tokens - 1);  // keys that the workgroup's rows see
+    const int run0 = w.split * p.run, most = w.limit(p, w.tokens - 1);  // keys that the workgroup's rows see
+    Pages pages;
+    load_queries<T, NQ, kSteps, CAP>(p, w, wave * 16 * NQ, col, [&](int s) { return s * 32 + g * 8; }, q, q, limit, unit, lowest, highest,
+                                     [&]() { pages.load(p, w, run0 >> c.page_shift, most, lane); });
 
     float4v o[NQ][kBlocks];
     float m[NQ], l[NQ];
@@ -546,7 +559,6 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_tiles_kernel(CacheA
         int page;
         float k_scale, bias, less;
     } now, next;
-    Pages pages;
     uint4 kx[kKeyLoads];
     uint32_t vx[8];
     // the thread's keys and channels: see `stage`
@@ -561,7 +573,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_tiles_kernel(CacheA
     };
     auto fetch = [&](int key0) {
         const int first = key0 >> c.page_shift, last = (key0 + Tile::kKeys - 16) >> c.page_shift;
-        if (pages.first < 0 || last >= pages.first + 64) {
+        if (last >= pages.first + 64) {
             const float turn = pages.load(p, w, first, most, lane);
 #pragma unroll
             for (int j = 0; j < NQ; ++j)
@@ -605,7 +617,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_tiles_kernel(CacheA
         put(3, two_codes<3, 3>(vx[0], vx[1]), two_codes<3, 3>(vx[2], vx[3]), two_codes<3, 3>(vx[4], vx[5]), two_codes<3, 3>(vx[6], vx[7]));
     };
 
-    const int run0 = w.split * p.run, run1 = (int)min((int64_t)most, (int64_t)run0 + p.run);
+    const int run1 = (int)min((int64_t)most, (int64_t)run0 + p.run);
     now = next = {-1, 0.f, 0.f, 0.f};
     if (run0 < run1) fetch(run0);
     for (int key0 = run0; key0 < run1; key0 += Tile::kKeys) {
@@ -708,7 +720,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p, int 
 template <typename T, int DP>
 constexpr bool kTiled = sizeof(T) == 2 && DP > 32;
 
-template <typename T, int DP, bool CAP>
+template <typename T, int DP, int CAP>
 hipError_t launch_rows(const CacheAttnParams& p, const CacheAttnPlan& plan, hipStream_t stream) {
     const dim3 grid((unsigned)plan.workgroups), block(64 * kCacheWaves);
     if (plan.rows == 16) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 1, false, CAP>), grid, block, 0, stream, p);
@@ -726,7 +738,11 @@ template <typename T>
 hipError_t launch_typed(const CacheAttnParams& p, const CacheAttnPlan& plan, hipStream_t stream) {
     return by_channels(p.c.D, [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        return p.softcap > 0.f ? launch_rows<T, DP, true>(p, plan, stream) : launch_rows<T, DP, false>(p, plan, stream);
+        if (p.softcap == 0.f) return launch_rows<T, DP, 0>(p, plan, stream);
+        if constexpr (sizeof(T) == 2) {
+            if (p.softcap <= kShortCap) return launch_rows<T, DP, 1>(p, plan, stream);
+        }
+        return launch_rows<T, DP, 2>(p, plan, stream);
     });
 }
 

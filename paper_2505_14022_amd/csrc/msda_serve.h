@@ -85,6 +85,7 @@ struct CacheAttnParams {
     int causal;
     bool vec;                   // queries are read in 16-byte pieces
     float scale, softcap;
+    float cap_unit, cap_inverse, cap_exponent;  // softcap log2(e), 1 / softcap, 2 log2(e) / softcap
 };
 struct CacheAttnPlan {
     int rows;                   // of a workgroup: 16 or 32 that its waves share, or 128, 32 of each wave's own

@@ -379,6 +379,12 @@ msda_status_t msda_cache_attention(const msda_cache_t* cache, const void* q, con
     p.vec = token_pieces(q, q_stride, T, M, es);
     p.scale = scale;
     p.softcap = softcap;
+    if (softcap > 0.f) {
+        const float log2e = 1.4426950408889634f;
+        p.cap_unit = softcap * log2e;
+        p.cap_inverse = 1.f / softcap;
+        p.cap_exponent = 2.f * log2e / softcap;
+    }
     hipError_t e = msda::launch_cache_attn(p, plan, dtype, (hipStream_t)stream);
     if (e != hipSuccess) return fail(MSDA_ERROR_LAUNCH_FAILED, "cache attention launch: %s", hipGetErrorString(e));
     return ok();

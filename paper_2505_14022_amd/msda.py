@@ -534,7 +534,7 @@ def _workspace(workspace, nbytes, like):
     if isinstance(workspace, str):
         if workspace != "auto":
             raise ValueError(f"workspace must be 'auto' or a tensor, not {workspace!r}")
-        return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+        return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     if workspace is not None and (workspace.device != like.device or not workspace.is_contiguous()):
         raise ValueError(f"the workspace must be contiguous and on {like.device}")
     return workspace

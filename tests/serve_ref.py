@@ -203,6 +203,7 @@ def attention(q, k_cache, v_cache, k_scale, v_scale, table, length, start=None, 
                 z = raw
                 if softcap:
                     z = softcap * torch.tanh(raw / softcap)
+                    # the series, or in 16 bits the short form up to a cap of 256: an fp32 rounding or two of 1, times the cap
                     dz = dz + 8 * U * softcap
                 total = torch.logsumexp(z, 0)
                 p = torch.exp(z - total)
