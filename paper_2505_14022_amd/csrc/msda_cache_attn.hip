@@ -299,16 +299,19 @@ __device__ __forceinline__ void weigh(const float4v (&s)[NG], const float (&by)[
     }
 }
 
-// OWN: every wave has rows of its own and walks over all keys; otherwise the waves share the rows and take the 32 keys in
-// turn, and their results are joined in LDS.
-template <typename T, int DP, int NQ, bool OWN, int CAP>
-__global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAttnParams p) {
+// Waves per SIMD that a kernel's registers leave room for.
+template <typename T>
+constexpr int row_waves(int NQ) { return NQ == 2 && sizeof(T) == 2 ? 3 : 2; }
+
+// A workgroup's waves share 16 NQ rows and take the 32 keys in turn; their results are joined in LDS.
+template <typename T, int DP, int NQ, int CAP>
+__global__ __launch_bounds__(64 * kCacheWaves, row_waves<T>(NQ)) void cache_attn_kernel(CacheAttnParams p) {
     constexpr bool kTwo = std::is_same_v<T, float>;
     constexpr int kSteps = DP / 32, kBytes = DP / 16, kWords = (kBytes + 3) / 4;
-    constexpr int kRows = 16 * NQ * (OWN ? kCacheWaves : 1);
+    constexpr int kRows = 16 * NQ;
     constexpr int kStride = DP + 4;  // of a row in LDS
-    __shared__ __attribute__((aligned(16))) float joined[OWN ? 1 : kCacheWaves * kRows * kStride];
-    __shared__ float2 stats[OWN ? 1 : kCacheWaves * kRows];
+    __shared__ __attribute__((aligned(16))) float joined[kCacheWaves * 16 * kStride];
+    __shared__ float2 stats[kCacheWaves * 16];
     const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, g = lane >> 4;
     CacheWork w;
     if (!w.find(p, xcd_item(blockIdx.x, gridDim.x), lane)) return;
@@ -318,9 +321,9 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
     int limit[NQ], lowest, highest;
     float unit[NQ];
     half8 q[NQ][kSteps], q_low[kTwo ? NQ : 1][kSteps];
-    const int run0 = w.split * p.run, first_key = run0 + (OWN ? 0 : 32 * wave), most = w.limit(p, w.tokens - 1);
+    const int run0 = w.split * p.run, first_key = run0 + 32 * wave, most = w.limit(p, w.tokens - 1);
     Pages pages;
-    load_queries<T, NQ, kSteps, CAP>(p, w, OWN ? wave * 16 * NQ : 0, col,
+    load_queries<T, NQ, kSteps, CAP>(p, w, 0, col,
                                      [&](int s) { return DP == 32 ? g * 8 : (s / 2) * 64 + g * 16 + (s % 2) * 8; }, q, q_low, limit,
                                      unit, lowest, highest, [&]() { pages.load(p, w, first_key >> c.page_shift, most, lane); });
 
@@ -343,7 +346,7 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
     const uint32_t v_at = 4 * g * c.D + (col * kBytes < c.D ? col * kBytes : 0);
 
     const int run1 = (int)min((int64_t)highest, (int64_t)run0 + p.run);
-    for (int key0 = first_key; key0 < run1; key0 += OWN ? 32 : 32 * kCacheWaves) {
+    for (int key0 = first_key; key0 < run1; key0 += 32 * kCacheWaves) {
         const int columns[2] = {key0 >> c.page_shift, (key0 + 16) >> c.page_shift};
         if (columns[1] >= pages.first + 64) {
             const float turn = pages.load(p, w, columns[0], most, lane);
@@ -439,59 +442,24 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
 #pragma unroll
         for (int u = 0; u < kBytes; ++u) o[j][u] *= by;
     }
-    if constexpr (OWN) {
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-            const int row = wave * 16 * NQ + j * 16 + col, i = row / p.group, h = row - i * p.group;
-            if (i >= w.tokens || h >= w.heads) continue;
-            if (p.splits > 1) {
-                const int64_t at = ((int64_t)w.item * kRows + row) * p.splits + w.split;
+    for (int j = 0; j < NQ; ++j) {  // 16 rows at a time
+        if (j > 0) __syncthreads();  // the last ones have been read
+        float* mine = joined + (wave * 16 + col) * kStride;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int u = 0; u < kBytes; u += 2)
-                        *reinterpret_cast<float2*>(p.part + at * DP + (4 * g + r) * kBytes + u) = make_float2(o[j][u][r], o[j][u + 1][r]);
-                if (g == 0) stats_of<DP>(p, kRows)[at] = make_float2(m[j], l[j]);
-                continue;
-            }
-            const float inv = l[j] == 0.f ? 0.f : 1.f / l[j];
-            const int64_t at = (int64_t)(w.token0 + i) * p.M + w.head0 + h;
-            T* out = static_cast<T*>(p.out) + at * c.D;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = (4 * g + r) * kBytes;
-                if (d >= c.D) continue;
-                Piece<T, kBytes> y;
-#pragma unroll
-                for (int u = 0; u < kBytes; ++u) y.v[u] = (T)(o[j][u][r] * inv);
-                if constexpr (sizeof(y) <= 16) {
-                    *reinterpret_cast<Piece<T, kBytes>*>(out + d) = y;
-                } else {
-#pragma unroll
-                    for (int u = 0; u < kBytes; u += 4) *reinterpret_cast<float4*>(out + d + u) = make_float4(y.v[u], y.v[u + 1], y.v[u + 2], y.v[u + 3]);
-                }
-            }
-            if (p.lse && g == 0) p.lse[at] = lse_of(m[j], l[j]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < NQ; ++j) {
-            float* mine = joined + (wave * kRows + j * 16 + col) * kStride;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int u = 0; u < kBytes; u += 2)
-                    *reinterpret_cast<float2*>(mine + (4 * g + r) * kBytes + u) = make_float2(o[j][u][r], o[j][u + 1][r]);
-            if (g == 0) stats[wave * kRows + j * 16 + col] = make_float2(m[j], l[j]);
-        }
+            for (int u = 0; u < kBytes; u += 2)
+                *reinterpret_cast<float2*>(mine + (4 * g + r) * kBytes + u) = make_float2(o[j][u][r], o[j][u + 1][r]);
+        if (g == 0) stats[wave * 16 + col] = make_float2(m[j], l[j]);
         __syncthreads();
-        for (int k = threadIdx.x; k < kRows * (DP / 4); k += 64 * kCacheWaves) {
-            const int row = k / (DP / 4), d = k % (DP / 4) * 4, i = row / p.group, h = row - i * p.group;
+        for (int k = threadIdx.x; k < 16 * (DP / 4); k += 64 * kCacheWaves) {
+            const int in = k / (DP / 4), d = k % (DP / 4) * 4, row = j * 16 + in, i = row / p.group, h = row - i * p.group;
             if (i >= w.tokens || h >= w.heads) continue;
             Joined x;
 #pragma unroll
             for (int v = 0; v < kCacheWaves; ++v)
-                x.take(stats[v * kRows + row], *reinterpret_cast<const float4*>(joined + (v * kRows + row) * kStride + d));
+                x.take(stats[v * 16 + in], *reinterpret_cast<const float4*>(joined + (v * 16 + in) * kStride + d));
             if (p.splits > 1) {
                 const int64_t at = ((int64_t)w.item * kRows + row) * p.splits + w.split;
                 *reinterpret_cast<float4*>(p.part + at * DP + d) = make_float4(x.x[0], x.x[1], x.x[2], x.x[3]);
@@ -500,200 +468,6 @@ __global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_attn_kernel(CacheAt
                 x.template store<T>(p, (int64_t)(w.token0 + i) * p.M + w.head0 + h, d);
             }
         }
-    }
-}
-
-// ---------------------------------------------------------------- many rows
-
-// Many rows of a sequence: every wave has 32 rows of its own, and the workgroup's waves share the work of turning codes into
-// fp16. Tiles of 8192 codes of keys and of values are loaded one ahead into registers and put into LDS as operands: keys
-// as rows of channels, values as rows of keys (a thread has 4 channels of 8 keys, and a code's place in two_codes
-// turns them around for free), the keys of 32 in the order in which a lane's probabilities have them. Both are read in 16-byte pieces,
-// permuted by the row's number so that the lanes of a read, and of a write, spread over the banks.
-template <int DP>
-struct CacheTile {
-    static constexpr int kKeys = 8192 / DP;
-    static constexpr int kGroups = kKeys / 16;          // of 16 keys, each of one page
-    static constexpr int kKeyPieces = DP / 8;           // of a key's row
-    static constexpr int kValuePieces = kKeys / 8;      // of a channel's row
-    _Float16 k[kKeys * DP], v[kKeys * DP];
-    static __device__ __forceinline__ int key_at(int key, int piece) {
-        return key * DP + ((piece ^ (DP == 128 ? key & 15 : key >> 1 & 7)) << 3);
-    }
-    static __device__ __forceinline__ int value_at(int d, int piece) {
-        return d * kKeys + ((piece ^ (DP == 128 ? (d >> 1 & 7) ^ (d >> 4 & 1) : (d ^ d >> 4) & 15)) << 3);
-    }
-};
-
-template <typename T, int DP, int CAP>
-__global__ __launch_bounds__(64 * kCacheWaves, 2) void cache_tiles_kernel(CacheAttnParams p) {
-    using Tile = CacheTile<DP>;
-    constexpr int NQ = 2, kSteps = DP / 32, kBlocks = DP / 16, kRows = 16 * NQ * kCacheWaves;
-    constexpr int kKeyLoads = 2, kPerKey = DP / 16;  // 16-byte loads of keys by a thread, and of a key
-    __shared__ __attribute__((aligned(16))) Tile tile;
-    const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, g = lane >> 4;
-    CacheWork w;
-    if (!w.find(p, xcd_item(blockIdx.x, gridDim.x), lane)) return;
-    if (w.split >= max(w.runs(p), 1)) return;
-    const Cache& c = p.c;
-
-    int limit[NQ], lowest, highest;
-    float unit[NQ];
-    half8 q[NQ][kSteps];
-    const int run0 = w.split * p.run, most = w.limit(p, w.tokens - 1);  // keys that the workgroup's rows see
-    Pages pages;
-    load_queries<T, NQ, kSteps, CAP>(p, w, wave * 16 * NQ, col, [&](int s) { return s * 32 + g * 8; }, q, q, limit, unit, lowest, highest,
-                                     [&]() { pages.load(p, w, run0 >> c.page_shift, most, lane); });
-
-    float4v o[NQ][kBlocks];
-    float m[NQ], l[NQ];
-#pragma unroll
-    for (int j = 0; j < NQ; ++j) {
-        m[j] = -kInf;
-        l[j] = 0.f;
-#pragma unroll
-        for (int u = 0; u < kBlocks; ++u) o[j][u] = float4v{0.f, 0.f, 0.f, 0.f};
-    }
-    // What lane i knows of the tile's keys 16 i .. 16 i + 15: of the tile that is worked on, and of the next one.
-    struct Group {
-        int page;
-        float k_scale, bias, less;
-    } now, next;
-    uint4 kx[kKeyLoads];
-    uint32_t vx[8];
-    // the thread's keys and channels: see `stage`
-    constexpr int kLanes = DP / 4;  // threads that have 8 keys' values
-    const int v_group = (int)threadIdx.x / kLanes, v_d = (int)threadIdx.x % kLanes * 4, vg = v_group & 3;
-    const int v_pair = __builtin_amdgcn_readfirstlane(v_group >> 2);  // 32 keys
-    const uint32_t v_at = 4 * vg * c.D + (v_d < c.D ? v_d : 0);
-    const int k_part = lane % kPerKey;
-    const uint32_t k_at = lane / kPerKey * c.D + (k_part * 16 < c.D ? k_part * 16 : 0);
-    auto slab = [&](int page, int key) {
-        return (((int64_t)max(page, 0) * c.Mkv + w.kv) << c.page_shift) * c.D + (int64_t)(key & (c.page - 1)) * c.D;
-    };
-    auto fetch = [&](int key0) {
-        const int first = key0 >> c.page_shift, last = (key0 + Tile::kKeys - 16) >> c.page_shift;
-        if (last >= pages.first + 64) {
-            const float turn = pages.load(p, w, first, most, lane);
-#pragma unroll
-            for (int j = 0; j < NQ; ++j)
-#pragma unroll
-                for (int u = 0; u < kBlocks; ++u) o[j][u] *= turn;
-            now.bias = fmaxf(now.bias + __builtin_amdgcn_logf(turn), kShift - kFar);
-            now.less = exp2_of(-now.bias);
-        }
-        const int from = min(((key0 + 16 * lane) >> c.page_shift) - pages.first, 63);
-        next.page = __shfl(pages.page, from, 64);
-        next.k_scale = __shfl(pages.k_scale, from, 64);
-        next.bias = __shfl(pages.bias, from, 64);
-        next.less = __shfl(pages.less, from, 64);
-#pragma unroll
-        for (int a = 0; a < kKeyLoads; ++a) {
-            const int key = (a * kCacheWaves + wave) * (64 / kPerKey), group = key >> 4;
-            const int64_t base = slab(__builtin_amdgcn_readlane(next.page, group), key0 + 16 * group) + (key & 15) * c.D;
-            kx[a] = *reinterpret_cast<const uint4*>(c.k + base + k_at);
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int group = 2 * v_pair + t;
-            const int64_t base = slab(__builtin_amdgcn_readlane(next.page, group), key0 + 16 * group);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) vx[4 * t + i] = *reinterpret_cast<const uint32_t*>(c.v + base + i * c.D + v_at);
-        }
-    };
-    auto stage = [&]() {
-#pragma unroll
-        for (int a = 0; a < kKeyLoads; ++a) {
-            const int key = (a * kCacheWaves + wave) * (64 / kPerKey) + lane / kPerKey;
-            *reinterpret_cast<half8*>(tile.k + Tile::key_at(key, 2 * k_part)) = eight_codes(kx[a].x, kx[a].y);
-            *reinterpret_cast<half8*>(tile.k + Tile::key_at(key, 2 * k_part + 1)) = eight_codes(kx[a].z, kx[a].w);
-        }
-        auto put = [&](int j, uint32_t x, uint32_t y, uint32_t z, uint32_t u) {
-            *reinterpret_cast<uint4*>(tile.v + Tile::value_at(v_d + j, v_group)) = make_uint4(x, y, z, u);
-        };
-        put(0, two_codes<0, 0>(vx[0], vx[1]), two_codes<0, 0>(vx[2], vx[3]), two_codes<0, 0>(vx[4], vx[5]), two_codes<0, 0>(vx[6], vx[7]));
-        put(1, two_codes<1, 1>(vx[0], vx[1]), two_codes<1, 1>(vx[2], vx[3]), two_codes<1, 1>(vx[4], vx[5]), two_codes<1, 1>(vx[6], vx[7]));
-        put(2, two_codes<2, 2>(vx[0], vx[1]), two_codes<2, 2>(vx[2], vx[3]), two_codes<2, 2>(vx[4], vx[5]), two_codes<2, 2>(vx[6], vx[7]));
-        put(3, two_codes<3, 3>(vx[0], vx[1]), two_codes<3, 3>(vx[2], vx[3]), two_codes<3, 3>(vx[4], vx[5]), two_codes<3, 3>(vx[6], vx[7]));
-    };
-
-    const int run1 = (int)min((int64_t)most, (int64_t)run0 + p.run);
-    now = next = {-1, 0.f, 0.f, 0.f};
-    if (run0 < run1) fetch(run0);
-    for (int key0 = run0; key0 < run1; key0 += Tile::kKeys) {
-        __syncthreads();  // everybody has read the tile before
-        stage();
-        now = next;
-        __syncthreads();  // the tile is there
-        if (key0 + Tile::kKeys < run1) fetch(key0 + Tile::kKeys);
-        const bool there = __all(lane >= Tile::kGroups || now.page >= 0);
-#pragma unroll 1
-        for (int sub = 0; sub < Tile::kKeys && key0 + sub < highest; sub += 32) {
-            constexpr int NG = 2;
-            const bool whole = there && key0 + sub + 32 <= lowest;
-            float4v s[NQ][NG];
-            GroupScales of[NG];
-#pragma unroll
-            for (int t = 0; t < NG; ++t) {
-                const int at = sub / 16 + t;
-                of[t] = {lane_value(now.k_scale, at), lane_value(now.bias, at), lane_value(now.less, at),
-                         __builtin_amdgcn_readlane(now.page, at) >= 0};
-#pragma unroll
-                for (int j = 0; j < NQ; ++j) s[j][t] = float4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    const half8 f = *reinterpret_cast<const half8*>(tile.k + Tile::key_at(sub + 16 * t + col, 4 * k + g));
-#pragma unroll
-                    for (int j = 0; j < NQ; ++j) s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[j][k], s[j][t], 0, 0, 0);
-                }
-            }
-            half8 vf[kBlocks];
-#pragma unroll
-            for (int u = 0; u < kBlocks; ++u) vf[u] = *reinterpret_cast<const half8*>(tile.v + Tile::value_at(16 * u + col, sub / 8 + g));
-            half8 prob[NQ][1];
-#pragma unroll
-            for (int j = 0; j < NQ; ++j) {
-                float by[NG];
-                const float top = finish_scores<CAP>(p, s[j], by, unit[j], of, whole, key0 + sub + 4 * g, limit[j]);
-                if (__any(top > m[j])) {
-                    const float fade = raise(m[j], top);
-                    l[j] *= fade;
-#pragma unroll
-                    for (int u = 0; u < kBlocks; ++u) o[j][u] *= fade;
-                }
-                weigh<false>(s[j], by, of, m[j], l[j], prob[j], nullptr);
-            }
-#pragma unroll
-            for (int u = 0; u < kBlocks; ++u) {
-                const half8 v = vf[u];
-#pragma unroll
-                for (int j = 0; j < NQ; ++j) o[j][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, prob[j][0], o[j][u], 0, 0, 0);
-            }
-        }
-    }
-
-    const float by = pages.base * exp2_of(-kShift);
-#pragma unroll
-    for (int j = 0; j < NQ; ++j) {
-        l[j] = column_sum(l[j]);
-        const int row = wave * 16 * NQ + j * 16 + col, i = row / p.group, h = row - i * p.group;
-        if (i >= w.tokens || h >= w.heads) continue;
-        if (p.splits > 1) {
-            const int64_t at = ((int64_t)w.item * kRows + row) * p.splits + w.split;
-#pragma unroll
-            for (int u = 0; u < kBlocks; ++u)
-                *reinterpret_cast<float4v*>(p.part + at * DP + 16 * u + 4 * g) = o[j][u] * by;
-            if (g == 0) stats_of<DP>(p, kRows)[at] = make_float2(m[j], l[j]);
-            continue;
-        }
-        const float inv = l[j] == 0.f ? 0.f : by / l[j];
-        const int64_t at = (int64_t)(w.token0 + i) * p.M + w.head0 + h;
-#pragma unroll
-        for (int u = 0; u < kBlocks; ++u) {
-            const float y[4] = {o[j][u][0] * inv, o[j][u][1] * inv, o[j][u][2] * inv, o[j][u][3] * inv};
-            store_four(static_cast<T*>(p.out) + at * c.D, 16 * u + 4 * g, c.D, y);
-        }
-        if (p.lse && g == 0) p.lse[at] = lse_of(m[j], l[j]);
     }
 }
 
@@ -716,17 +490,12 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnParams p, int 
     }
 }
 
-// Whether many rows go through tiles in LDS: 16-bit queries of more than 32 channels.
-template <typename T, int DP>
-constexpr bool kTiled = sizeof(T) == 2 && DP > 32;
-
 template <typename T, int DP, int CAP>
 hipError_t launch_rows(const CacheAttnParams& p, const CacheAttnPlan& plan, hipStream_t stream) {
     const dim3 grid((unsigned)plan.workgroups), block(64 * kCacheWaves);
-    if (plan.rows == 16) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 1, false, CAP>), grid, block, 0, stream, p);
-    else if (plan.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 2, false, CAP>), grid, block, 0, stream, p);
-    else if constexpr (kTiled<T, DP>) hipLaunchKernelGGL((cache_tiles_kernel<T, DP, CAP>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((cache_attn_kernel<T, DP, 2, true, CAP>), grid, block, 0, stream, p);
+    if (plan.rows == 16) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 1, CAP>), grid, block, 0, stream, p);
+    else if (plan.rows == 32) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 2, CAP>), grid, block, 0, stream, p);
+    else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((cache_attn_kernel<T, DP, 3, CAP>), grid, block, 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     hipLaunchKernelGGL((cache_join_kernel<T, DP>), dim3((unsigned)((int64_t)p.blocks * p.c.Mkv * p.groups)), dim3(256), 0, stream, p,
@@ -750,19 +519,25 @@ hipError_t launch_typed(const CacheAttnParams& p, const CacheAttnPlan& plan, hip
 
 // Rows of a workgroup by what a sequence has on average, and runs so that the card is full.
 CacheAttnPlan cache_attn_plan(const CacheAttnParams& p, int dtype) {
-    (void)dtype;
     CacheAttnPlan a;
     const Cache& c = p.c;
     const int64_t mean = c.start && c.N > 0 ? (c.T + c.N - 1) / c.N : 1, G = p.G;
-    a.rows = mean * G <= 16 ? 16 : mean * G <= 64 ? 32 : 128;
-    a.group = (int)(G < a.rows ? G : a.rows);
-    a.groups = (int)((G + a.group - 1) / a.group);
-    a.tokens = a.rows / a.group;
-    a.blocks = place_count(c, a.tokens, 1);
-    const int64_t items = a.blocks * c.Mkv * a.groups, longest = (int64_t)c.width * c.page;
-    const int64_t least = a.rows == 128 ? 512 : 256;  // tokens of a run
+    auto blocks_of = [&](int rows) {
+        a.rows = rows;
+        a.group = (int)(G < rows ? G : rows);
+        a.groups = (int)((G + a.group - 1) / a.group);
+        a.tokens = a.rows / a.group;
+        a.blocks = place_count(c, a.tokens, 1);
+        return a.blocks * c.Mkv * a.groups;
+    };
+    // More rows of a wave share the codes' way to fp16, but make fewer workgroups.
+    int64_t items = mean * G <= 16 ? blocks_of(16) : blocks_of(32);
+    if (dtype != MSDA_F32 && mean * G >= 1024) {
+        items = blocks_of(48);
+        if (items < 1024) items = blocks_of(32);
+    }
+    const int64_t longest = (int64_t)c.width * c.page, least = 256;  // tokens of a run
     int64_t splits = items > 0 ? 1024 / items : 1;
-    if (a.rows == 128 && items >= 512) splits = 1;
     if (splits > longest / least) splits = longest / least;
     // the partial results have to fit into half a GB
     const int64_t row_bytes = (attn_channels(c.D) + 2) * 4, most = ((int64_t)512 << 20) / (items * a.rows * row_bytes + 1);
