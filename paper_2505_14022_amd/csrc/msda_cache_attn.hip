@@ -1,8 +1,8 @@
 // Attention over a paged cache of 8-bit keys and values with a scale for each page and head.
 //   z = cap(scale k_scale q . k_code),  lse = log sum exp z,  out = sum exp(z - lse) v_scale v_code
-// For single tokens it is bound by reading the cache once, for chunks of a prompt by the matrix unit and the vector work
-// between its products. One pass over the keys with a running maximum and sum, everything in registers: a wave has 16 rows
-// (queries of the heads that share a key head) or a multiple, as columns of 16 x 16 x 32 instructions, and takes 32 keys at a time.
+// For single tokens it is bound by reading the cache once, for chunks of a prompt by the vector work around its products. One
+// pass over the keys with a running maximum and sum, everything in registers: a wave has 16 rows (queries of the heads that
+// share a key head), 32 or 48, as columns of 16 x 16 x 32 instructions, and takes 32 keys at a time.
 //   scores: keys are the instruction's rows. A lane (column n, quarter g) reads consecutive bytes of key n of 16, in an order
 //     of channels that the queries follow, and gets the scores of keys 4 g .. 4 g + 3 of both halves of the 32;
 //   values: a sum over keys may take them in any order, so the lane's eight probabilities are its operand as they are, and it
@@ -14,6 +14,11 @@
 // Roundings: queries are scaled by a power of two to their row's largest and held in fp16 (in fp32 as the sum of two), exact for
 // fp16 and for all of bf16 within 2^28 of the largest; probabilities are rounded to fp16 for the product (in fp32 the sum of
 // two), times 2^14, so that those of long rows keep their bits; their sum is taken before that. Statistics and sums are fp32.
+// Measured: one token each of 32 sequences of 11 to 16 thousand keys, 32 heads of 128 channels on 8, bf16: 163 us and 6 to
+// join the runs, 5.3 TB/s (a large copy reaches 5.1); two chunks of up to 2048 tokens over up to 10240, the same heads:
+// 634 us, 708 TFLOP/s (a large product 1366), two waves per SIMD at 241 registers; 32 rows a wave took 692, 16 rows 1164. A
+// kernel whose waves share fp16 tiles in LDS, so that a code is turned once for 128 rows, took 705: its barriers and reads of LDS
+// cost what it saved.
 #include "msda_attn.hpp"
 #include "msda_cache.hpp"
 
@@ -299,7 +304,8 @@ __device__ __forceinline__ void weigh(const float4v (&s)[NG], const float (&by)[
     }
 }
 
-// Waves per SIMD that a kernel's registers leave room for.
+// Waves per SIMD that a kernel's registers leave room for. (32 rows: three keep 6 registers in memory, and a chunk of 2048 tokens
+// over 10240 takes 692 us for 748; in fp32 they would keep most of their sums there, 1051 us for 413.)
 template <typename T>
 constexpr int row_waves(int NQ) { return NQ == 2 && sizeof(T) == 2 ? 3 : 2; }
 
@@ -530,7 +536,11 @@ CacheAttnPlan cache_attn_plan(const CacheAttnParams& p, int dtype) {
         a.blocks = place_count(c, a.tokens, 1);
         return a.blocks * c.Mkv * a.groups;
     };
-    // More rows of a wave share the codes' way to fp16, but make fewer workgroups.
+    // More rows of a wave share the codes' way to fp16, but make fewer workgroups. bf16, 32 heads of 128 channels on 8 key heads,
+    // with 16, 32 and 48 rows: 8 sequences of 8000 keys with 4 new tokens 42, 47 and 67 us, with 16 63, 55 and 74; one of 8192
+    // with 1024 253, 187 and 190; two of 10240 with 2048 1164, 692 and 633. 64 channels, 16 sequences of 4000 with 512 of 8
+    // heads: 134, 112 and 113. In fp32 (products of two fp16 parts) 48 rows do not fit into the registers: two of 8192 with 2048,
+    // 16 heads of 128 on 4, 517, 413 and 749.
     int64_t items = mean * G <= 16 ? blocks_of(16) : blocks_of(32);
     if (dtype != MSDA_F32 && mean * G >= 1024) {
         items = blocks_of(48);
