@@ -7,8 +7,8 @@
 // sum of squares, which are found in one reduction, and the codes come from fp32 operations that do not depend on the
 // order of any sum. A NaN stays the largest, and is told with
 // the infinities by the largest's bits.
-// Measured: 9973 rows x 2568 in fp16 with a residual, its sum and 8-bit results 36 us, 5.0 TB/s (a large copy 5.1); 39894 x 1024 in
-// bf16 with a residual 47 forward, 54 backward and 5 for the sums; 16 x 4096 5.1.
+// Measured: 9973 rows x 2568 in fp16 with a residual, its sum and 8-bit results 33 to 36 us, 5.0 to 5.4 TB/s (a large copy
+// 5.1); 39894 x 1024 in bf16 with a residual 40 to 47 forward, 53 backward and 5 for the sums; 16 x 4096 5.0.
 #include "msda_codes.hpp"
 #include "msda_rows.hpp"
 #include "msda_serve.h"

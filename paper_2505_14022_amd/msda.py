@@ -485,9 +485,9 @@ def _layer_dtype(t) -> int:
 def _expect(name, t, shape, dtype, like, strided=False):
     """Checks one tensor argument: its shape and dtype, the device of `like`, and contiguity (with
     `strided`, of the channels alone). None passes."""
-    if t is None or (t.shape == shape and t.dtype is dtype and t.is_cuda and t.get_device() == like.get_device() and
+    if t is None or (t.shape == shape and t.dtype is dtype and t.get_device() == like.get_device() >= 0 and
                      (t.is_contiguous() or (strided and t.stride(-1) == 1))):
-        return
+        return  # get_device() is negative of what is not on a GPU
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} of {tuple(t.shape)}")
     if t.device != like.device:
