@@ -10,7 +10,8 @@
 // Measured: 8 tokens x 4096 by 6144 channels 9.1 us, 2.8 TB/s (bf16 results); 8192 x 4096 by 12288 380 to 396 us, 2.1 to 2.2 POP/s (the
 // library's int8 product, 32-bit results, 433; its best, 8192 cubed, 2.4 POP/s); 1019 x 1360 by 2050 in fp32 14. Sums stored from where
 // the matrix instructions leave them, 8 bytes a lane, took 584 for the second, and the builtin for loads to LDS, after which the
-// compiler waits for all of them before any read, 404.
+// compiler waits for all of them before any read, 404. Rows of 4097 codes, which start at any byte: 8 tokens by 6144 channels 26 us,
+// 4096 by 4096 95 (4096 codes 73), 8000 x 2001 by 8000 187 (1.4 POP/s).
 #include "msda_layer.hpp"
 #include "msda_serve.h"
 
@@ -26,8 +27,12 @@ __device__ __forceinline__ int4_t load_codes(const int8_t* row, int k, int K) {
     int4_t x = {0, 0, 0, 0};
     if (PIECES) {
         if (k < K) x = *reinterpret_cast<const int4_t*>(row + k);
-    } else if (k + 16 <= K) {
-        __builtin_memcpy(&x, row + k, 16);
+    } else if (K >= 16) {
+        // the row's last 16 codes, those before k shifted out, where fewer than 16 are left: no lane takes a way of its own
+        const int from = min(k, K - 16), skip = k - from;
+        unsigned __int128 codes;
+        __builtin_memcpy(&codes, row + from, 16);
+        if (skip < 16) x = __builtin_bit_cast(int4_t, codes >> (8 * skip));
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -123,8 +128,9 @@ __device__ __forceinline__ void wait_loads() {
     __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
 }
 
-// Tiles of BM tokens and BN channels, WM x WN waves, 128 bytes of every row at a time, of which NS are in LDS.
-template <typename T, int BM, int BN, int WM, int WN, int NS>
+// Tiles of BM tokens and BN channels, WM x WN waves, 128 bytes of every row at a time, of which NS are in LDS. Rows that are
+// not whole pieces (PIECES false) go through registers, since loads to LDS want their addresses aligned.
+template <typename T, int BM, int BN, int WM, int WN, int NS, bool PIECES>
 __global__ __launch_bounds__(64 * WM * WN) void product_tiles_kernel(ProductParams p, int across) {
     constexpr int kWaves = WM * WN, kTM = BM / WM / 32, kTN = BN / WN / 32;  // 32 x 32 blocks of a wave
     constexpr int kRows = BM + BN, kLoads = kRows / 8 / kWaves;              // 8 rows a load of a wave
@@ -168,20 +174,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiles_kernel(ProductPara
         return *reinterpret_cast<const int4_t*>(tile[s] + row * 128 + (((step * 2 + lh) ^ (row >> 1 & 7)) << 4));
     };
     for (int i = threadIdx.x; i < BM; i += 64 * kWaves) a_scale[i] = p.a_scale[min(t0 + i, p.T - 1)];
-#pragma unroll
-    for (int i = 0; i < NS - 1; ++i)
-        if (i * 128 < p.K) load(i * 128, i);
-    int s = 0, last = NS - 1;
-    for (int k0 = 0; k0 < p.K; k0 += 128) {
-        // the wave's pieces of this buffer are in LDS, those of the next ones may be on their way
-        if (NS > 3 && k0 + 256 < p.K) wait_loads<(NS > 3 ? 2 : 0) * kLoads>();
-        else if (NS > 2 && k0 + 128 < p.K) wait_loads<(NS > 2 ? 1 : 0) * kLoads>();
-        else wait_loads<0>();
-        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_barrier();        // everybody's are, and the buffer before it has been read
-        asm volatile("" ::: "memory");
-        if (k0 + (NS - 1) * 128 < p.K) load(k0 + (NS - 1) * 128, last);
+    auto multiply = [&](int s) {
 #pragma unroll
         for (int step = 0; step < 4; ++step) {
             int4_t x[kTN], y[kTM];
@@ -194,8 +187,51 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiles_kernel(ProductPara
 #pragma unroll
                 for (int m = 0; m < kTM; ++m) acc[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[n], y[m], acc[n][m], 0, 0, 0);
         }
-        last = s;
-        s = s + 1 == NS ? 0 : s + 1;
+    };
+    if constexpr (PIECES) {
+#pragma unroll
+        for (int i = 0; i < NS - 1; ++i)
+            if (i * 128 < p.K) load(i * 128, i);
+        int s = 0, last = NS - 1;
+        for (int k0 = 0; k0 < p.K; k0 += 128) {
+            // the wave's pieces of this buffer are in LDS, those of the next ones may be on their way
+            if (NS > 3 && k0 + 256 < p.K) wait_loads<(NS > 3 ? 2 : 0) * kLoads>();
+            else if (NS > 2 && k0 + 128 < p.K) wait_loads<(NS > 2 ? 1 : 0) * kLoads>();
+            else wait_loads<0>();
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();        // everybody's are, and the buffer before it has been read
+            asm volatile("" ::: "memory");
+            if (k0 + (NS - 1) * 128 < p.K) load(k0 + (NS - 1) * 128, last);
+            multiply(s);
+            last = s;
+            s = s + 1 == NS ? 0 : s + 1;
+        }
+    } else {
+        static_assert(NS == 2, "a buffer that is read, and one that is written");
+        int4_t held[kLoads];
+        auto take = [&](int k0) {
+            if (k0 + 128 <= p.K) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) __builtin_memcpy(&held[i], from[i] + k0, 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) held[i] = load_codes<false>(from[i] - piece[i] * 16, k0 + piece[i] * 16, p.K);
+            }
+        };
+        auto leave = [&](int s) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) *reinterpret_cast<int4_t*>(tile[s] + (wave * kLoads + i) * 1024 + lane * 16) = held[i];
+        };
+        take(0);
+        leave(0);
+        int s = 0;
+        for (int k0 = 0; k0 < p.K; k0 += 128, s ^= 1) {
+            __syncthreads();  // this buffer is written, and the other one has been read
+            if (k0 + 128 < p.K) take(k0 + 128);
+            multiply(s);
+            if (k0 + 128 < p.K) leave(s ^ 1);
+        }
     }
     // Sums change lanes through LDS, so that a lane has kPer consecutive channels (the same ones all along: their scales
     // stay in registers) and a wave stores whole pieces of rows.
@@ -257,8 +293,10 @@ void launch_rows(const ProductParams& p, int64_t workgroups, hipStream_t stream)
 
 template <typename T, int BM, int BN, int WM, int WN, int NS>
 void launch_tiles(const ProductParams& p, int64_t workgroups, hipStream_t stream) {
-    hipLaunchKernelGGL((product_tiles_kernel<T, BM, BN, WM, WN, NS>), dim3((unsigned)((workgroups + 7) / 8 * 8)), dim3(64 * WM * WN),
-                       0, stream, p, (p.O + BN - 1) / BN);
+    const dim3 grid((unsigned)((workgroups + 7) / 8 * 8)), block(64 * WM * WN);
+    const int across = (p.O + BN - 1) / BN;
+    if (p.pieces) hipLaunchKernelGGL((product_tiles_kernel<T, BM, BN, WM, WN, NS, true>), grid, block, 0, stream, p, across);
+    else hipLaunchKernelGGL((product_tiles_kernel<T, BM, BN, WM, WN, 2, false>), grid, block, 0, stream, p, across);
 }
 
 template <typename T>
@@ -294,7 +332,7 @@ ProductPlan product_plan(const ProductParams& p) {
     // Few tokens and tiles: 64 x 4096 by 4096 12.9 us against 13.6, by 1024 of 8192 20 against 24, but each 64 tokens read b again.
     // The larger tile as soon as every CU has one: 1024 x 4096 by 4096 with tiles of 64, 128 and 256 35, 27.5 and 56 us, 512
     // tokens 20, 25 and 55; 4096 tokens 111, 83 and 70, 2048 62, 42 and 58.
-    if (!p.pieces || p.T <= 64) {
+    if (p.T <= 64) {
         take(p.T <= 16 ? 16 : p.T <= 32 ? 32 : 64, 16, kRowWaves);
     } else if (tiles(256, 256) >= 256) {
         take(256, 256, 8);

@@ -70,6 +70,15 @@ def test_product_of_unaligned_codes(T, at):
     check(*make(T, 320, 70, seed=at, at=at), "bf16")
 
 
+# rows that are not whole 16-byte pieces, in tiles of each size: one short step, whole steps and a rest, a rest of one
+@pytest.mark.parametrize("T,K,O", [(65, 7, 40), (300, 777, 301), (2050, 129, 2049), (4100, 145, 4101), (4097, 383, 4098)],
+                         ids=lambda v: str(v))
+def test_product_of_odd_rows(T, K, O):
+    say(f"product of {T} x {K} and {O} x {K}")
+    check(*make(T, K, O, seed=T + K), "bf16")
+    check(*make(T, K + 1, O, seed=T + K), "f32")
+
+
 @pytest.mark.parametrize("T,O", [(5, 64), (90, 128), (5, 66)])
 def test_product_into_a_given_tensor(T, O):
     import torch
