@@ -7,7 +7,7 @@
 // straight into its registers, and the waves' sums are added in LDS. Many tokens: bound by the matrix unit. Tiles of both go to LDS past the
 // registers while the previous ones are multiplied; 16-byte pieces of a row of 128 are permuted by the row's number, so that
 // reads of one column of pieces spread over the banks.
-// Measured: 8 tokens x 4096 by 6144 channels 9.1 us, 2.8 TB/s (bf16 results); 8192 x 4096 by 12288 380 to 396 us, 2.1 to 2.2 POP/s (the
+// Measured: 8 tokens x 4096 by 6144 channels 9.1 us, 2.8 TB/s (bf16 results); 8192 x 4096 by 12288 380 to 410 us, 2.0 to 2.2 POP/s (the
 // library's int8 product, 32-bit results, 433; its best, 8192 cubed, 2.4 POP/s); 1019 x 1360 by 2050 in fp32 14. Sums stored from where
 // the matrix instructions leave them, 8 bytes a lane, took 584 for the second, and the builtin for loads to LDS, after which the
 // compiler waits for all of them before any read, 404. Rows of 4097 codes, which start at any byte: 8 tokens by 6144 channels 26 us,
