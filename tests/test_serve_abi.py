@@ -98,7 +98,8 @@ def product(L, T=4, K=64, O=32, dtype=0, a=0x1000, b=0x2000, a_scale=0x3000, b_s
     (dict(a=None), INVALID, "non-null"), (dict(b=None), INVALID, "non-null"), (dict(a_scale=None), INVALID, "non-null"),
     (dict(b_scale=None), INVALID, "non-null"), (dict(out=None), INVALID, "non-null"), (dict(a_scale=0x3001), INVALID, "misaligned"),
     (dict(bias=0x3002), INVALID, "misaligned"), (dict(out=0x5002), INVALID, "misaligned"), (dict(out=0x5001, dtype=1), INVALID, "misaligned"),
-    (dict(T=1 << 30, O=1 << 30), UNSUPPORTED, "launch"), (dict(T=1 << 24, O=1 << 10, K=7), UNSUPPORTED, "launch"),
+    (dict(T=1 << 30, O=1 << 30), UNSUPPORTED, "launch"), (dict(T=1 << 30, O=1 << 30, K=7), UNSUPPORTED, "launch"),
+    (dict(T=64, O=(1 << 31) - 2048, K=7), UNSUPPORTED, "launch"),
 ])
 def test_product_refuses(L, no_gpu, kw, status, needle):
     assert product(L, **kw) == status and needle in msda.last_error()
