@@ -1,5 +1,5 @@
 // New keys and values into a paged cache of 8 bits, the keys turned by their positions on the way.
-//   u' = max(u where tokens stood in the page, most * (1 / 127)),  old codes rne(code * (u / u')),  new ones rne(x * (1 / u'))
+//   u' = max(u where tokens stood in the page, most * (1 / 127)),  old codes rne(code * (u / u')) if u' > u,  new ones rne(x * (1 / u'))
 // Bound by memory (2 or 4 bytes read and 1 written for each channel), or by latency for single tokens. A workgroup has one page of
 // one sequence, and each of its waves one head's keys or values of that page: nothing is shared between heads
 // but the positions' cosines and sines, which the workgroup forms once, in LDS. A lane takes two 16-byte pieces at a time, a
@@ -151,8 +151,8 @@ __global__ __launch_bounds__(64 * kUnits, 4) void append_kernel(AppendParams p, 
     const bool odd = u != u || !(old >= 0.f && old < __builtin_huge_valf());
     u = old > u ? old : u;
     const float inverse = u > 0.f && !odd ? 1.f / u : 0.f;
-    if (old > 0.f && u > old && !odd) {
-        const float ratio = old / u;
+    if (u > old && !odd) {
+        const float ratio = old / u;  // of a page of scale 0, whatever its codes are, it makes zeros
         for (int i = lane * 16; i < s0 * c.D; i += 64 * 16) {
             auto x = *reinterpret_cast<const Piece<int8_t, 16>*>(codes + i);
 #pragma unroll
