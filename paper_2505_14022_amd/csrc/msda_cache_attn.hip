@@ -9,8 +9,11 @@
 //     reads DP / 16 bytes of each of its eight keys, which are the rows n DP / 16 .. of the other operand.
 // So nothing is exchanged between lanes but a maximum, and the cache goes from memory to registers. A code c becomes
 // fp16 without a conversion: byte c ^ 0x80 below the exponent of 1024 is 1152 + c, less 1152 is c.
-// A page's key scale is a factor of its scores. Its value scale goes into the exponent, relative to the largest of the
-// pages at hand, so that it costs nothing for each key.
+// A page's key scale is a factor of its scores. Its value scale goes into the exponent, so that it costs nothing for each key: an
+// operand is a probability in units of the row's largest so far, times its value scale in units of the pages' largest. That
+// keeps its digits where value scales are within 2^8 of each other. Where they are not ("apart"), a row would lose what it has to a
+// scale that it does not see, or sees with a small probability: the largest product of the two that the row has seen is the
+// unit then, and the sum of the probabilities has exponents of its own. A workgroup that meets such scales begins anew in that way.
 // Roundings: queries are scaled by a power of two to their row's largest and held in fp16 (in fp32 as the sum of two), exact for
 // fp16 and for all of bf16 within 2^28 of the largest; probabilities are rounded to fp16 for the product (in fp32 the sum of
 // two), times 2^14, so that those of long rows keep their bits; their sum is taken before that. Statistics and sums are fp32.
@@ -31,7 +34,6 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 
 constexpr int kCacheWaves = 4;
 constexpr float kShift = 14.f;  // probabilities times 2^14 as an operand
-constexpr float kFar = 74.f;    // value scales that differ by 2^74 and more count as if by that
 
 // Bytes A and B (0 .. 3) of the words x and y of codes, as two fp16 numbers.
 template <int A, int B>
@@ -108,12 +110,21 @@ struct CacheWork {
     }
 };
 
+__device__ __forceinline__ float lane_value(float x, int lane) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
 // The pages of 64 columns of the sequence's table, one to a lane.
+template <bool APART>
 struct Pages {
     int first;                  // column of lane 0
     int page;                   // -1: no tokens
-    float k_scale, bias, less;  // bias: log2 of the value scale relative to `base`, and kShift; less: 2^-bias
-    float base = 0.f;           // the largest value scale so far; sums are in units of it
+    float k_scale, bias;        // bias: log2 of the value scale in units of unit(), and kShift
+    // Without APART, the same in all lanes: the largest value scale so far, and of the first 64 pages; whether any is not within 1 / 64
+    // and 4 of the latter, so that they may be more than 2^8 from each other.
+    float most = 0.f, first_most = 0.f;
+    bool apart = false;
+    __device__ __forceinline__ float unit() const { return !APART && most > 0.f ? most : 1.f; }
     // Loads columns `column` ..; returns the factor from the old unit to the new one.
     __device__ __forceinline__ float load(const CacheAttnParams& p, const CacheWork& w, int column, int end, int lane) {
         first = column;
@@ -130,20 +141,19 @@ struct Pages {
         const bool odd = !(k_scale >= 0.f && k_scale < kInf && v_scale >= 0.f && v_scale < kInf);
         if (odd) k_scale = __builtin_nanf("");
         if (odd || v_scale < 1.17549435e-38f) v_scale = 0.f;  // logarithms are those of normal numbers
-        float top = group_max<64>(v_scale);
-        top = fmaxf(top, base);
-        const float unit = top > 0.f ? top : 1.f;
-        const float turn = base > 0.f ? base / unit : 1.f;
-        base = top;
-        // a scale below 2^-kFar of the largest, or of 0, counts as that much: its values are lost beside others in fp32
-        bias = fmaxf((v_scale > 0.f ? __builtin_amdgcn_logf(v_scale) : -kInf) - __builtin_amdgcn_logf(unit), -kFar) + kShift;
-        less = exp2_of(-bias);
+        float turn = 1.f;
+        if constexpr (!APART) {
+            const float before = most;
+            most = lane_value(fmaxf(group_max<64>(v_scale), most), 0);
+            if (before > 0.f) turn = before / most;
+            else first_most = most;
+            const bool near = v_scale > 0.f && v_scale * 64.f >= first_most && v_scale <= 4.f * first_most;
+            if (__any(page >= 0 && !near)) apart = true;
+        }
+        bias = (page >= 0 ? __builtin_amdgcn_logf(v_scale) - __builtin_amdgcn_logf(unit()) : 0.f) + kShift;
         return turn;
     }
 };
-__device__ __forceinline__ float lane_value(float x, int lane) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
-}
 
 // lse of a row's maximum (in units of log 2) and sum.
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2; }
@@ -248,18 +258,19 @@ __device__ __forceinline__ void load_queries(const CacheAttnParams& p, const Cac
     highest = __builtin_amdgcn_readfirstlane(highest);
 }
 
-// Raw scores of a lane's row with NG groups of four keys, key + 16 t .. key + 16 t + 3, made probabilities (times 2^kShift and the
-// value scale in units of the largest), in fp16 (with TWO the sum of prob and low). whole: the row sees all of them; otherwise
-// those below `limit`, of groups that have a page. The running maximum and sum follow.
+// What a group of four keys gets from its page; less: 2^-bias.
 struct GroupScales {
     float k_scale, bias, less;
     bool there;
 };
-// CAP: capped by tanh, in its short form for 16-bit results and caps up to kShortCap (a score is 2^-14 off then), else its series.
-template <int CAP, int NG>
-__device__ __forceinline__ float finish_scores(const CacheAttnParams& p, float4v (&s)[NG], float (&by)[NG], float unit,
-                                               const GroupScales (&of)[NG], bool whole, int key, int limit) {
-    float top = -kInf;
+// Raw scores of a lane's row with NG groups of four keys, key + 16 t .. key + 16 t + 3, made scores but for the factors `by`. whole: the
+// row sees all of them; otherwise those below `limit`, of groups that have a page. Returns the largest score, and with APART the
+// largest exponent of an operand. CAP: capped by tanh, in its short form for 16-bit results and caps up to kShortCap (a score is
+// 2^-14 off then), else its series.
+template <int CAP, bool APART, int NG>
+__device__ __forceinline__ float2 finish_scores(const CacheAttnParams& p, float4v (&s)[NG], float (&by)[NG], float unit,
+                                                const GroupScales (&of)[NG], bool whole, int key, int limit) {
+    float top = -kInf, weighed = -kInf;
 #pragma unroll
     for (int t = 0; t < NG; ++t) {
         by[t] = unit * of[t].k_scale;
@@ -275,9 +286,11 @@ __device__ __forceinline__ float finish_scores(const CacheAttnParams& p, float4v
             for (int r = 0; r < 4; ++r) s[t][r] = key + 16 * t + r < stop ? s[t][r] * by[t] : -kInf;
             by[t] = 1.f;
         }
-        top = fmaxf(top, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])) * by[t]);
+        const float most = fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])) * by[t];
+        top = fmaxf(top, most);
+        if constexpr (APART) weighed = fmaxf(weighed, most + of[t].bias);
     }
-    return top;
+    return make_float2(top, weighed);
 }
 // The running maximum after a lane's `top`, and the factor of what was summed before.
 __device__ __forceinline__ float raise(float& m, float top) {
@@ -286,58 +299,54 @@ __device__ __forceinline__ float raise(float& m, float top) {
     m = now;
     return fade;
 }
-template <bool TWO, int NG>
-__device__ __forceinline__ void weigh(const float4v (&s)[NG], const float (&by)[NG], const GroupScales (&of)[NG], float m, float& l,
-                                      half8 (&prob)[NG / 2], half8* low) {
-    const float base = m == -kInf ? 0.f : m;
+// Scores made operands (probabilities times 2^kShift and the value scale, see above) in fp16, with TWO the sum of prob and low; the
+// probabilities are added to l in units of 2^m, m being the row's largest score so far. Operands' exponents are relative to m too, or
+// with APART to `ref`, the largest exponent of an operand so far less kShift.
+template <bool TWO, bool APART, int NG>
+__device__ __forceinline__ void weigh(const float4v (&s)[NG], const float (&by)[NG], const GroupScales (&of)[NG], float m, float ref,
+                                      float& l, half8 (&prob)[NG / 2], half8* low) {
+    const float base = m == -kInf ? 0.f : m, from = !APART ? base : ref == -kInf ? 0.f : ref;
 #pragma unroll
     for (int t = 0; t < NG; ++t) {
         float sum = 0.f;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float x = exp2_of(__builtin_fmaf(s[t][r], by[t], of[t].bias - base));
-            sum += x;
+            const float x = exp2_of(__builtin_fmaf(s[t][r], by[t], of[t].bias - from));
+            sum += APART ? exp2_of(__builtin_fmaf(s[t][r], by[t], -base)) : x;
             prob[t / 2][4 * (t % 2) + r] = (_Float16)x;
             if constexpr (TWO) low[t / 2][4 * (t % 2) + r] = (_Float16)(x - (float)prob[t / 2][4 * (t % 2) + r]);
         }
-        l += sum * of[t].less;
+        l += APART ? sum : sum * of[t].less;
     }
 }
 
-// Waves per SIMD that a kernel's registers leave room for. (32 rows: three keep 6 registers in memory, and a chunk of 2048 tokens
-// over 10240 takes 692 us for 748; in fp32 they would keep most of their sums there, 1051 us for 413.)
-template <typename T>
-constexpr int row_waves(int NQ) { return NQ == 2 && sizeof(T) == 2 ? 3 : 2; }
-
-// A workgroup's waves share 16 NQ rows and take the 32 keys in turn; their results are joined in LDS.
-template <typename T, int DP, int NQ, int CAP>
-__global__ __launch_bounds__(64 * kCacheWaves, row_waves<T>(NQ)) void cache_attn_kernel(CacheAttnParams p) {
+// Rows row0 .. row0 + 16 NQ - 1 of a workgroup's kRows, and its run of keys. Returns false, with nothing stored, if APART has to be
+// set for them.
+template <typename T, int DP, int NQ, int CAP, bool APART, int kRows>
+__device__ __forceinline__ bool attend(const CacheAttnParams& p, int thread, int row0, float* joined, float2* stats, int* failed) {
     constexpr bool kTwo = std::is_same_v<T, float>;
     constexpr int kSteps = DP / 32, kBytes = DP / 16, kWords = (kBytes + 3) / 4;
-    constexpr int kRows = 16 * NQ;
     constexpr int kStride = DP + 4;  // of a row in LDS
-    __shared__ __attribute__((aligned(16))) float joined[kCacheWaves * 16 * kStride];
-    __shared__ float2 stats[kCacheWaves * 16];
-    const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 15, g = lane >> 4;
+    const int lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), col = lane & 15, g = lane >> 4;
     CacheWork w;
-    if (!w.find(p, xcd_item(blockIdx.x, gridDim.x), lane)) return;
-    if (w.split >= max(w.runs(p), 1)) return;
+    if (!w.find(p, xcd_item(blockIdx.x, gridDim.x), lane)) return true;
+    if (w.split >= max(w.runs(p), 1)) return true;
     const Cache& c = p.c;
 
     int limit[NQ], lowest, highest;
     float unit[NQ];
     half8 q[NQ][kSteps], q_low[kTwo ? NQ : 1][kSteps];
     const int run0 = w.split * p.run, first_key = run0 + 32 * wave, most = w.limit(p, w.tokens - 1);
-    Pages pages;
-    load_queries<T, NQ, kSteps, CAP>(p, w, 0, col,
+    Pages<APART> pages;
+    load_queries<T, NQ, kSteps, CAP>(p, w, row0, col,
                                      [&](int s) { return DP == 32 ? g * 8 : (s / 2) * 64 + g * 16 + (s % 2) * 8; }, q, q_low, limit,
                                      unit, lowest, highest, [&]() { pages.load(p, w, first_key >> c.page_shift, most, lane); });
 
     float4v o[NQ][kBytes];
-    float m[NQ], l[NQ];
+    float m[NQ], l[NQ], ref[NQ];  // ref: see weigh
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
-        m[j] = -kInf;
+        m[j] = ref[j] = -kInf;
         l[j] = 0.f;
 #pragma unroll
         for (int u = 0; u < kBytes; ++u) o[j][u] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -351,15 +360,18 @@ __global__ __launch_bounds__(64 * kCacheWaves, row_waves<T>(NQ)) void cache_attn
     }
     const uint32_t v_at = 4 * g * c.D + (col * kBytes < c.D ? col * kBytes : 0);
 
-    const int run1 = (int)min((int64_t)highest, (int64_t)run0 + p.run);
+    const int run1 = pages.apart ? 0 : (int)min((int64_t)highest, (int64_t)run0 + p.run);
     for (int key0 = first_key; key0 < run1; key0 += 32 * kCacheWaves) {
         const int columns[2] = {key0 >> c.page_shift, (key0 + 16) >> c.page_shift};
         if (columns[1] >= pages.first + 64) {
             const float turn = pages.load(p, w, columns[0], most, lane);
+            if (pages.apart) break;
+            if constexpr (!APART) {
 #pragma unroll
-            for (int j = 0; j < NQ; ++j)
+                for (int j = 0; j < NQ; ++j)
 #pragma unroll
-                for (int u = 0; u < kBytes; ++u) o[j][u] *= turn;
+                    for (int u = 0; u < kBytes; ++u) o[j][u] *= turn;
+            }
         }
         uint4 kx[2][DP == 32 ? 1 : DP / 64];
         uint32_t vx[8][kWords];
@@ -370,7 +382,8 @@ __global__ __launch_bounds__(64 * kCacheWaves, row_waves<T>(NQ)) void cache_attn
             const int at = columns[t] - pages.first, slot = (key0 + 16 * t) & (c.page - 1);
             const int page = __builtin_amdgcn_readlane(pages.page, at);
             whole = whole && page >= 0;
-            of[t] = {lane_value(pages.k_scale, at), lane_value(pages.bias, at), lane_value(pages.less, at), page >= 0};
+            const float bias = lane_value(pages.bias, at);
+            of[t] = {lane_value(pages.k_scale, at), bias, exp2_of(-bias), page >= 0};
             const int64_t base = (((int64_t)max(page, 0) * c.Mkv + w.kv) << c.page_shift) * c.D + (int64_t)slot * c.D;
 #pragma unroll
             for (int u = 0; u < (DP == 32 ? 1 : DP / 64); ++u) {
@@ -415,14 +428,23 @@ __global__ __launch_bounds__(64 * kCacheWaves, row_waves<T>(NQ)) void cache_attn
 #pragma unroll
         for (int j = 0; j < NQ; ++j) {
             float by[2];
-            const float top = finish_scores<CAP>(p, s[j], by, unit[j], of, whole, key0 + 4 * g, limit[j]);
-            if (__any(top > m[j])) {
-                const float fade = raise(m[j], top);
+            const float2 top = finish_scores<CAP, APART>(p, s[j], by, unit[j], of, whole, key0 + 4 * g, limit[j]);
+            if (__any(top.x > m[j])) {
+                const float fade = raise(m[j], top.x);
                 l[j] *= fade;
+                if constexpr (!APART) {
 #pragma unroll
-                for (int u = 0; u < kBytes; ++u) o[j][u] *= fade;
+                    for (int u = 0; u < kBytes; ++u) o[j][u] *= fade;
+                }
             }
-            weigh<kTwo>(s[j], by, of, m[j], l[j], prob[j], prob_low[kTwo ? j : 0]);
+            if constexpr (APART) {
+                if (__any(top.y - kShift > ref[j])) {
+                    const float fade = raise(ref[j], top.y - kShift);
+#pragma unroll
+                    for (int u = 0; u < kBytes; ++u) o[j][u] *= fade;
+                }
+            }
+            weigh<kTwo, APART>(s[j], by, of, m[j], ref[j], l[j], prob[j], prob_low[kTwo ? j : 0]);
         }
 #pragma unroll
         for (int u = 0; u < kBytes; ++u) {
@@ -441,12 +463,12 @@ __global__ __launch_bounds__(64 * kCacheWaves, row_waves<T>(NQ)) void cache_attn
         }
     }
 
-    const float by = pages.base * exp2_of(-kShift);
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
         l[j] = column_sum(l[j]);
+        const float by = !APART ? pages.unit() : m[j] == -kInf ? 0.f : exp2_of(ref[j] - m[j]);
 #pragma unroll
-        for (int u = 0; u < kBytes; ++u) o[j][u] *= by;
+        for (int u = 0; u < kBytes; ++u) o[j][u] = o[j][u] * exp2_of(-kShift) * by;
     }
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {  // 16 rows at a time
@@ -458,9 +480,16 @@ __global__ __launch_bounds__(64 * kCacheWaves, row_waves<T>(NQ)) void cache_attn
             for (int u = 0; u < kBytes; u += 2)
                 *reinterpret_cast<float2*>(mine + (4 * g + r) * kBytes + u) = make_float2(o[j][u][r], o[j][u + 1][r]);
         if (g == 0) stats[wave * 16 + col] = make_float2(m[j], l[j]);
+        if (!APART && j == 0 && lane == 0) failed[wave] = pages.apart;
         __syncthreads();
-        for (int k = threadIdx.x; k < 16 * (DP / 4); k += 64 * kCacheWaves) {
-            const int in = k / (DP / 4), d = k % (DP / 4) * 4, row = j * 16 + in, i = row / p.group, h = row - i * p.group;
+        if (!APART && j == 0) {
+            int any = 0;
+#pragma unroll
+            for (int v = 0; v < kCacheWaves; ++v) any |= failed[v];
+            if (any) return false;
+        }
+        for (int k = thread; k < 16 * (DP / 4); k += 64 * kCacheWaves) {
+            const int in = k / (DP / 4), d = k % (DP / 4) * 4, row = row0 + j * 16 + in, i = row / p.group, h = row - i * p.group;
             if (i >= w.tokens || h >= w.heads) continue;
             Joined x;
 #pragma unroll
@@ -474,6 +503,36 @@ __global__ __launch_bounds__(64 * kCacheWaves, row_waves<T>(NQ)) void cache_attn
                 x.template store<T>(p, (int64_t)(w.token0 + i) * p.M + w.head0 + h, d);
             }
         }
+    }
+    return true;
+}
+
+// Waves per SIMD that the registers of the kernel for 16, 32 and 48 rows leave room for, so that the part for scales that are apart
+// takes no more. (128 channels in 16 bits, 32 rows: three keep some of the queries in memory, and a chunk of 2048 tokens over 10240 takes
+// 692 us for 748; in fp32 they would keep most of their sums there, 1051 us for 413.)
+template <typename T>
+constexpr int row_waves(int DP, int NQ) {
+    constexpr int of32[3][2] = {{6, 4}, {5, 3}, {3, 2}}, of16[3][3] = {{7, 5, 4}, {5, 4, 3}, {4, 3, 2}};
+    const int width = DP == 32 ? 0 : DP == 64 ? 1 : 2;
+    return sizeof(T) == 4 ? of32[width][NQ - 1] : of16[width][NQ - 1];
+}
+
+// A workgroup's waves share 16 NQ rows and take the 32 keys in turn; their results are joined in LDS. Value scales that are apart
+// are found on the way, and the rows begun anew: sixteen at a time, and from the arguments and the thread's number as if they were
+// others, so that nothing that this needs takes registers from the first part. (With the choice made for each step of one loop, two chunks took 700 us for 640;
+// with one loop after the other, and all rows in both, 645 to 700, and a chunk of 1024 tokens 273 to 318 for 246.)
+template <typename T, int DP, int NQ, int CAP>
+__global__ __launch_bounds__(64 * kCacheWaves, row_waves<T>(DP, NQ)) void cache_attn_kernel(CacheAttnParams p) {
+    __shared__ __attribute__((aligned(16))) float joined[kCacheWaves * 16 * (DP + 4)];
+    __shared__ float2 stats[kCacheWaves * 16];
+    __shared__ int failed[kCacheWaves];
+    if (attend<T, DP, NQ, CAP, false, 16 * NQ>(p, threadIdx.x, 0, joined, stats, failed)) return;
+    for (int row0 = 0; row0 < 16 * NQ; row0 += 16) {
+        __syncthreads();  // what is in LDS has been read
+        auto* arguments = (const __attribute__((address_space(4))) CacheAttnParams*)__builtin_amdgcn_kernarg_segment_ptr();
+        int thread = threadIdx.x;
+        asm volatile("" : "+s"(arguments), "+v"(thread) : : "memory");
+        attend<T, DP, 1, CAP, true, 16 * NQ>(*(const CacheAttnParams*)arguments, thread, row0, joined, stats, failed);
     }
 }
 
