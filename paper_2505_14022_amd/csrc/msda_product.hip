@@ -189,14 +189,14 @@ __global__ __launch_bounds__(64 * WM * WN) void product_tiles_kernel(ProductPara
         }
     };
     if constexpr (PIECES) {
+        static_assert(NS == 2 || NS == 3, "at most one buffer is on its way while another is read");
 #pragma unroll
         for (int i = 0; i < NS - 1; ++i)
             if (i * 128 < p.K) load(i * 128, i);
         int s = 0, last = NS - 1;
         for (int k0 = 0; k0 < p.K; k0 += 128) {
             // the wave's pieces of this buffer are in LDS, those of the next ones may be on their way
-            if (NS > 3 && k0 + 256 < p.K) wait_loads<(NS > 3 ? 2 : 0) * kLoads>();
-            else if (NS > 2 && k0 + 128 < p.K) wait_loads<(NS > 2 ? 1 : 0) * kLoads>();
+            if (NS > 2 && k0 + 128 < p.K) wait_loads<(NS > 2 ? 1 : 0) * kLoads>();
             else wait_loads<0>();
             __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
             asm volatile("" ::: "memory");

@@ -88,7 +88,7 @@ struct CacheAttnParams {
     float cap_unit, cap_inverse, cap_exponent;  // softcap log2(e), 1 / softcap, 2 log2(e) / softcap
 };
 struct CacheAttnPlan {
-    int rows;                   // of a workgroup: 16 or 32 that its waves share, or 128, 32 of each wave's own
+    int rows;                   // of a workgroup, shared by its waves: 16, 32 or 48
     int group, groups, tokens, splits, run;
     int64_t blocks, workgroups;
     size_t bytes;               // of the workspace
