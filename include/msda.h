@@ -533,11 +533,11 @@ msda_status_t msda_cache_append(const msda_cache_t* cache, const void* k, const 
  * head m / (M / Mkv); scores are capped as in msda_attention_forward.
  *   z = cap(scale * q . k),  lse = log sum exp(z),  out = sum exp(z - lse) v
  * causal: the query of place p sees the tokens up to place p of its sequence; otherwise all length[n] of them. A query
- * that sees no token gets out = 0 and lse = -inf. A page with a scale that is negative or not finite makes NaN of the rows that see any of it;
- * a value scale below fp32's smallest normal number, 2^-126, counts as 0. What is not seen (codes and scales alike) has
- * no effect but on how small terms are rounded: a term of out is rounded in fp16 (with fp32 queries in the sum of two of them), and
- * those below 2^-20 of the row's largest product of probability and value scale to a fixed step, 2^-30 of it or less. Value scales
- * that are within 1/64 and 4 of the largest of 64 pages are the fast ones.
+ * that sees no token gets out = 0 and lse = -inf. A page with a scale that is negative or not finite makes NaN of the rows that
+ * see any of it; a value scale, or a product of one with a probability, below fp32's smallest normal number, 2^-126, counts as 0.
+ * What is not seen (codes and scales alike) has no effect but on how small terms are rounded: a term of out is rounded in fp16
+ * (with fp32 queries in the sum of two of them), and one below 2^-20 of the row's largest product of probability and value scale
+ * to a fixed step, 2^-30 of that or less. Value scales within 1/64 and 4 of the largest of a run's first 64 pages are the fast ones.
  *   q_stride  HOST array of two strides in elements (token, head), >= 0, the channels contiguous
  *   out [T, M, D] dtype contiguous, 16-byte aligned;  lse [T, M] fp32 or NULL. Rows of tokens of no sequence are left as
  *   they were.

@@ -6,7 +6,8 @@
 // pair's two where the channels of a pair lie in halves. The largest value has to be known before the first code can be
 // written: what a lane has loaded first stays in its registers (4 times two pieces, half a page of 64 tokens of 128 channels in 16
 // bits), and the rest is read again, from a cache. (Chunks of up to 2048 tokens of 16 sequences, 8 heads of 128 channels in
-// fp16: 53 us, 3.0 TB/s; with 8 times two pieces, of which the registers leave room for fewer waves, 72; with none 96.)
+// fp16: 54 us, 2.9 TB/s, the waves waiting for memory in 60 % of their time; with 8 times two pieces, of which the registers leave room
+// for fewer waves, 72; with none 96.)
 #include "msda_cache.hpp"
 #include "msda_codes.hpp"
 #include "msda_turn.hpp"

@@ -17,11 +17,12 @@
 // Roundings: queries are scaled by a power of two to their row's largest and held in fp16 (in fp32 as the sum of two), exact for
 // fp16 and for all of bf16 within 2^28 of the largest; probabilities are rounded to fp16 for the product (in fp32 the sum of
 // two), times 2^14, so that those of long rows keep their bits; their sum is taken before that. Statistics and sums are fp32.
-// Measured: one token each of 32 sequences of 11 to 16 thousand keys, 32 heads of 128 channels on 8, bf16: 163 us and 6 to
+// Measured: one token each of 32 sequences of 11 to 16 thousand keys, 32 heads of 128 channels on 8, bf16: 165 us and 5 to
 // join the runs, 5.3 TB/s (a large copy reaches 5.1); two chunks of up to 2048 tokens over up to 10240, the same heads:
-// 634 us, 708 TFLOP/s (a large product 1366), two waves per SIMD at 241 registers; 32 rows a wave took 692, 16 rows 1164. A
+// 646 us, 696 TFLOP/s (a large product 1366), two waves per SIMD at 245 registers, of which the vector unit works in 73 % of the cycles and
+// the matrix unit in 27 %. (Before it looked for scales that are apart it took 634, with 32 rows a wave 692, with 16 1164. A
 // kernel whose waves share fp16 tiles in LDS, so that a code is turned once for 128 rows, took 705: its barriers and reads of LDS
-// cost what it saved.
+// cost what it saved.)
 #include "msda_attn.hpp"
 #include "msda_cache.hpp"
 
