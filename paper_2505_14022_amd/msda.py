@@ -963,7 +963,8 @@ def cache_attention(q, k_cache, v_cache, k_scale, v_scale, table, length, start=
     msda_cache_attention.
 
     The cache's arguments as in cache_append, which has stored the new tokens' keys and values already; M is a multiple of Mkv;
-    q may be a view whose channels are contiguous. scale: D ** -0.5 when None. softcap: cap of the scores (0: none). causal:
+    q may be a view whose channels are contiguous. Long sequences are split by the table's width: a view of the columns that
+    they reach is faster than a table that is several times wider. scale: D ** -0.5 when None. softcap: cap of the scores (0: none). causal:
     a token sees those up to itself, otherwise all of its sequence. workspace: "auto" allocates it, or a caller-owned uint8
     tensor of cache_attention_workspace_size bytes.
     """
